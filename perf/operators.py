@@ -391,8 +391,9 @@ def _own(s):
     if s["op"] == "adamw8":
         if "plan" not in s:
             at = lambda t, i: ctypes.c_void_p(t.data_ptr() + i * t.element_size())  # noqa: E731
-            s["plan"] = [fx.Adamw8Tensor(at(s["w"], a), at(s["m"], a), at(s["v"], a), at(s["m_scale"], a // BLOCK), at(s["v_scale"], a // BLOCK), at(s["g"], a), at(s["wc"], a),
+            plan = [fx.Adamw8Tensor(at(s["w"], a), at(s["m"], a), at(s["v"], a), at(s["m_scale"], a // BLOCK), at(s["v_scale"], a // BLOCK), at(s["g"], a), at(s["wc"], a),
                                          n, wd, seed) for a, n, wd, seed in s["tensors"]]
+            s["plan"] = (fx.Adamw8Tensor * len(plan))(*plan)
         fx.fax_adamw8_step(ctx, s["plan"], hparams(grad_is_bf16=int(c["bf16_grad"]), **s["hp"]))
         return {k: s[k] for k in ("w", "wc", "m", "v", "m_scale", "v_scale")}
     if s["op"] == "quant":
