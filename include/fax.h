@@ -81,12 +81,14 @@ uint64_t fax_launch_count(const fax_ctx* ctx);
 /* Per-kernel profile.  Between fax_profile_begin and fax_profile_end every
  * operator launch on this context is bracketed by a pair of CUDA events on the
  * context's stream.  fax_profile_end synchronises the stream and fills `out`
- * (HOST array of n_out >= FAX_KERNEL_CLASSES entries, indexed by kernel class)
+ * (HOST array of n_out entries, indexed by kernel class: FAX_KERNEL_CLASSES for all;
+ * an array of the FAX_KERNEL_CLASSES_MIN classes of earlier versions is filled as far as it goes)
  * with, per class: operator launches, summed device milliseconds, summed
  * algorithmic FLOPs (2 per multiply-add) and summed algorithmic bytes (what the
  * operator must read and write once).  Profiling costs two event records per
  * launch, so timed runs keep it off. */
-#define FAX_KERNEL_CLASSES 10
+#define FAX_KERNEL_CLASSES 12
+#define FAX_KERNEL_CLASSES_MIN 10
 typedef struct { int64_t launches; double ms, flops, bytes; } fax_profile_entry;
 fax_status fax_profile_begin(fax_ctx* ctx);
 fax_status fax_profile_end(fax_ctx* ctx, fax_profile_entry* out, int32_t n_out);
@@ -176,6 +178,45 @@ typedef struct {
 /* `tensors` is a HOST array of n_tensors descriptors of device buffers. */
 fax_status fax_adamw_step(fax_ctx* ctx, const fax_adamw_tensor* tensors, int32_t n_tensors,
                           const fax_adamw_hparams* hp);
+
+/* AdamW over many tensors at once whose moments are held in 8 bits: m in e4m3
+ * (largest value 448, NaN 0x7f), v in e5m2 (57344, NaN 0x7f), one byte an
+ * element, with a float32 power-of-two scale for each FAX_ADAMW8_BLOCK
+ * consecutive elements: the moment is scale * value.  m, v: n bytes; m_scale,
+ * v_scale: ceil(n / FAX_ADAMW8_BLOCK) floats.  All four zero (or moments zero,
+ * any finite scale) is the state before step 1.  Per element the moments are
+ * widened, updated and used as fax_adamw_step writes it, every float32 operation
+ * rounded on its own in the order
+ *   m = b1*m + (1-b1)*g          v = b2*v + ((1-b2)*g)*g
+ *   w = (w - (lr*wd)*w) - (lr*(m*c1)) / (sqrt(v*c2) + eps)
+ * (c1 = 1/(1-b1^t), c2 = 1/(1-b2^t), taken in float64 and rounded), and stored
+ * again: the scale is the smallest power of two, at least 2^-126, that brings the
+ * largest finite moment of the block to the format's largest value at most (1 for
+ * a block of zeros), and moment / scale is rounded stochastically: to the
+ * neighbour above with the probability that makes the rounding right on average,
+ * because a step of (1-b2) is too small to ever move the nearest 8-bit value.
+ * A v above 0 stays above 0; a moment that is not finite becomes NaN, its
+ * neighbours keep theirs.  The 16 random bits of m and of v are the high and low
+ * half of h(i ^ (h(seed + step * 0x9E3779B9) + (i >> 32) * 0x85EBCA77)) for
+ * element i, all modulo 2^32, with
+ *   h(x): x ^= x>>16; x *= 0x7FEB352D; x ^= x>>15; x *= 0x846CA68B; x ^= x>>16:
+ * a step is the same bits wherever the tensor stands in a call.  Give tensors
+ * different seeds.  w and g are 16-byte, w_compute 8-byte, m, v and the scales
+ * 4-byte aligned; a tensor with n = 0 is skipped. */
+#define FAX_ADAMW8_BLOCK 128
+typedef struct {
+  float* w;
+  void* m; void* v; float* m_scale; float* v_scale;
+  const void* g;
+  void* w_compute;
+  uint64_t n;
+  float weight_decay;
+  uint32_t seed;
+} fax_adamw8_tensor;
+
+/* `tensors` is a HOST array of n_tensors descriptors of device buffers. */
+fax_status fax_adamw8_step(fax_ctx* ctx, const fax_adamw8_tensor* tensors, int32_t n_tensors,
+                           const fax_adamw_hparams* hp);
 
 /* The whole-step calls (fax_block_step*, fax_lm_step*) run the AdamW update of
  * each tensor on a second stream owned by the context as soon as that tensor's

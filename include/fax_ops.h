@@ -110,6 +110,75 @@ fax_status fax_op_attention_backward(fax_ctx* ctx, int32_t prec, int32_t batch, 
                                      const float* lse, const void* d_o, void* dqkv, void* scratch,
                                      size_t scratch_bytes);
 
+/* Token table lookup: out[i, :] = scale * table[ids[i], :], rounded once to T.
+ * ids: n_tokens int32; an id outside [0, vocab) (padding) gives a row of zeros.
+ * table [vocab, d] T, out [n_tokens, d] T.  n_tokens = 0 does nothing. */
+fax_status fax_op_embedding_forward(fax_ctx* ctx, int32_t prec, int32_t n_tokens, int32_t vocab, int32_t d,
+                                    const int32_t* ids, const void* table, float scale, void* out);
+
+/* Its reverse: dtable[v, :] = scale * sum over the tokens i with ids[i] = v of
+ * dout[i, :]  (accumulate != 0: added to what dtable holds, e.g. the output
+ * head's gradient of a tied table).  dout [n_tokens, d] T; dtable [vocab, d]
+ * float: overwritten in full, or with accumulate != 0 changed only in rows
+ * that a token touches.  Tokens with an id outside [0, vocab) add nothing.  The
+ * tokens are sorted by id first and each row is summed in float32 in a fixed
+ * order: the same inputs give the same bits.  Concurrent calls need scratch of
+ * their own.  n_tokens <= 2^30; scratch 256-byte aligned. */
+fax_status fax_op_embedding_backward_scratch_bytes(int32_t n_tokens, int32_t vocab, int32_t d, size_t* bytes);
+fax_status fax_op_embedding_backward(fax_ctx* ctx, int32_t prec, int32_t n_tokens, int32_t vocab, int32_t d,
+                                     const int32_t* ids, const void* dout, float scale, int32_t accumulate,
+                                     float* dtable, void* scratch, size_t scratch_bytes);
+
+/* ---- matrices in 8-bit floating point, and their products ----
+ * A matrix is held as one byte an element (FAX_FP8_E4M3: largest value 448;
+ * FAX_FP8_E5M2: 57344; both with NaN 0x7f) and a float32 scale for each 1 x 128
+ * (tile 1) or 128 x 128 (tile 128) block of it: element = scale * value.  Blocks
+ * begin at row 0 and column 0; those at the edges are cut off.  The scales of a
+ * matrix [R, C] are stored with the block of columns first:
+ * scale[(c / 128) * ld + r] (tile 1, ld >= R) or
+ * scale[(c / 128) * ld + r / 128] (tile 128, ld >= ceil(R / 128)). */
+enum { FAX_FP8_E4M3 = 0, FAX_FP8_E5M2 = 1 };
+#define FAX_FP8_BLOCK 128
+
+/* x [rows, cols] T with row pitch ldx -> any of
+ *   q  [rows, cols] with pitch ldq and its scales s, pitch lds     (NULL: not wanted)
+ *   qt [cols, rows], x transposed, pitch ldqt, its scales st, pitch ldst
+ *                    (blocks along x's columns: tokens, for a weight gradient)
+ * from one reading of x.  A block's scale is the smallest power of two, at least
+ * 2^-126, that brings its largest finite magnitude to the format's largest value
+ * at most (1 for a block without any above 0); values are x / scale (exact)
+ * rounded to nearest even; elements that are not finite become NaN.  ldq and
+ * ldqt are multiples of 16, q and qt 16-byte aligned; bytes between cols and ldq
+ * (rows and ldqt) are left as they were. */
+typedef struct {
+  int32_t rows, cols;
+  const void* x; int64_t ldx;
+  int32_t format, tile;
+  void* q; int64_t ldq; float* s; int64_t lds;
+  void* qt; int64_t ldqt; float* st; int64_t ldst;
+} fax_fp8_quantize_desc;
+fax_status fax_op_fp8_quantize(fax_ctx* ctx, int32_t prec, const fax_fp8_quantize_desc* desc);
+
+/* C[M, N] = A B^T of two such matrices, A [M, K] with tile 1 and B [N, K] with
+ * b_tile 1 or 128, both row-major with pitches lda, ldb (multiples of 16;
+ * 16-byte aligned bases), formats chosen for each:
+ *   C[m, n] = sum over blocks b of 128 k of sa[b, m] sb[b, n] sum_{k in b} A[m, k] B[n, k]
+ * in float32 on the tensor cores, plus bias[n] (bf16; NULL: none), rounded once
+ * to bf16, or kept as float (c_f32 != 0), or added to a float C (accumulate != 0).
+ * The forward product takes activations and transposed weights (tile 128),
+ * the input gradient output gradients and weights as stored, the weight gradient
+ * both factors transposed with tile 1.  Any M, N, K; scales may be any finite
+ * floats whose products are finite.  ldc >= N in elements; C aligned to its
+ * elements (16-byte aligned rows are stored faster).  C may not overlap A or B. */
+typedef struct {
+  int32_t M, N, K;
+  const void* A; int64_t lda; int32_t a_format; const float* a_scale; int64_t a_scale_ld;
+  const void* B; int64_t ldb; int32_t b_format; const float* b_scale; int64_t b_scale_ld; int32_t b_tile;
+  void* C; int64_t ldc; int32_t c_f32; int32_t accumulate;
+  const void* bias;
+} fax_fp8_gemm_desc;
+fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,7 @@ class FaxError(RuntimeError):
         super().__init__(f"{where}: {status_string(status)} ({status})")
 
 
-FAX_KERNEL_CLASSES = 10
+FAX_KERNEL_CLASSES = 12
 
 
 class ProfileEntry(C.Structure):
@@ -53,6 +53,12 @@ class BlockGrads(C.Structure):
 class AdamwTensor(C.Structure):
     _fields_ = [("w", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("g", C.c_void_p),
                 ("w_compute", C.c_void_p), ("n", C.c_uint64), ("weight_decay", C.c_float)]
+
+
+class Adamw8Tensor(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("g", C.c_void_p), ("w_compute", C.c_void_p), ("n", C.c_uint64),
+                ("weight_decay", C.c_float), ("seed", C.c_uint32)]
 
 
 class AdamwHparams(C.Structure):
@@ -112,6 +118,7 @@ _SIGNATURES = {
     "fax_block_backward": (C.c_int32, [_P, C.POINTER(BlockCfg), C.POINTER(BlockParams), _P, _P, C.c_size_t,
                                        _P, C.POINTER(BlockGrads), C.c_int32, _P, C.c_size_t]),
     "fax_adamw_step": (C.c_int32, [_P, C.POINTER(AdamwTensor), C.c_int32, C.POINTER(AdamwHparams)]),
+    "fax_adamw8_step": (C.c_int32, [_P, C.POINTER(Adamw8Tensor), C.c_int32, C.POINTER(AdamwHparams)]),
     "fax_block_step": (C.c_int32, [_P, C.POINTER(BlockCfg), C.POINTER(BlockState), _P, _P, _P, _P,
                                    C.POINTER(AdamwHparams)]),
     "fax_block_host_scratch_bytes": (C.c_int32, [C.POINTER(BlockCfg), C.POINTER(C.c_size_t)]),
@@ -286,6 +293,12 @@ def fax_block_backward(ctx, cfg, params, dy, saved, saved_bytes, dx, grads, accu
 def fax_adamw_step(ctx, tensors, hp: AdamwHparams):
     arr = (AdamwTensor * len(tensors))(*tensors)
     _check(load_library().fax_adamw_step(ctx, arr, len(tensors), C.byref(hp)), "fax_adamw_step")
+
+
+def fax_adamw8_step(ctx, tensors, hp: AdamwHparams):
+    """AdamW with 8-bit moments; `tensors`: Adamw8Tensor structs (a list, or a ctypes array kept by the caller)."""
+    arr = tensors if isinstance(tensors, C.Array) else (Adamw8Tensor * len(tensors))(*tensors)
+    _check(load_library().fax_adamw8_step(ctx, arr, len(arr), C.byref(hp)), "fax_adamw8_step")
 
 
 def fax_block_step(ctx, cfg, st, x, dy, y, dx, hp):

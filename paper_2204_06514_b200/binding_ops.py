@@ -17,6 +17,25 @@ class GemmDesc(C.Structure):
                 ("aux", _P), ("ldaux", C.c_int64), ("alpha", C.c_float), ("force_simt", C.c_int32)]
 
 
+FAX_FP8_E4M3, FAX_FP8_E5M2 = range(2)
+FAX_FP8_BLOCK = 128
+
+
+class Fp8QuantizeDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("x", _P), ("ldx", C.c_int64),
+                ("format", C.c_int32), ("tile", C.c_int32),
+                ("q", _P), ("ldq", C.c_int64), ("s", _P), ("lds", C.c_int64),
+                ("qt", _P), ("ldqt", C.c_int64), ("st", _P), ("ldst", C.c_int64)]
+
+
+class Fp8GemmDesc(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32),
+                ("A", _P), ("lda", C.c_int64), ("a_format", C.c_int32), ("a_scale", _P), ("a_scale_ld", C.c_int64),
+                ("B", _P), ("ldb", C.c_int64), ("b_format", C.c_int32), ("b_scale", _P), ("b_scale_ld", C.c_int64),
+                ("b_tile", C.c_int32),
+                ("C", _P), ("ldc", C.c_int64), ("c_f32", C.c_int32), ("accumulate", C.c_int32), ("bias", _P)]
+
+
 _SIGNATURES = {
     "fax_op_gemm": (C.c_int32, [_P, C.c_int32, C.POINTER(GemmDesc)]),
     "fax_op_layernorm_forward": (C.c_int32, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P, C.c_float,
@@ -31,6 +50,12 @@ _SIGNATURES = {
     "fax_op_attention_backward_scratch_bytes": (C.c_int32, [C.c_int32] * 5 + [C.POINTER(C.c_size_t)]),
     "fax_op_attention_backward": (C.c_int32, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                               _P, _P, _P, _P, _P, _P, C.c_size_t]),
+    "fax_op_embedding_forward": (C.c_int32, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_float, _P]),
+    "fax_op_embedding_backward_scratch_bytes": (C.c_int32, [C.c_int32] * 3 + [C.POINTER(C.c_size_t)]),
+    "fax_op_embedding_backward": (C.c_int32, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _P, _P, C.c_float,
+                                              C.c_int32, _P, _P, C.c_size_t]),
+    "fax_op_fp8_quantize": (C.c_int32, [_P, C.c_int32, C.POINTER(Fp8QuantizeDesc)]),
+    "fax_op_fp8_gemm": (C.c_int32, [_P, C.POINTER(Fp8GemmDesc)]),
 }
 
 _lib = None
@@ -102,3 +127,29 @@ def fax_op_attention_backward(ctx, prec, batch, seq, n_heads, head_dim, qkv, o, 
                               scratch_bytes):
     _check(_L().fax_op_attention_backward(ctx, prec, batch, seq, n_heads, head_dim, qkv, o, lse, d_o, dqkv,
                                           scratch, scratch_bytes), "fax_op_attention_backward")
+
+
+def fax_op_embedding_forward(ctx, prec, n_tokens, vocab, d, ids, table, scale, out):
+    _check(_L().fax_op_embedding_forward(ctx, prec, n_tokens, vocab, d, ids, table, scale, out),
+           "fax_op_embedding_forward")
+
+
+def fax_op_embedding_backward_scratch_bytes(n_tokens, vocab, d) -> int:
+    b = C.c_size_t()
+    _check(_L().fax_op_embedding_backward_scratch_bytes(n_tokens, vocab, d, C.byref(b)),
+           "fax_op_embedding_backward_scratch_bytes")
+    return b.value
+
+
+def fax_op_embedding_backward(ctx, prec, n_tokens, vocab, d, ids, dout, scale, accumulate, dtable, scratch,
+                              scratch_bytes):
+    _check(_L().fax_op_embedding_backward(ctx, prec, n_tokens, vocab, d, ids, dout, scale, int(bool(accumulate)),
+                                          dtable, scratch, scratch_bytes), "fax_op_embedding_backward")
+
+
+def fax_op_fp8_quantize(ctx, prec, desc: Fp8QuantizeDesc):
+    _check(_L().fax_op_fp8_quantize(ctx, prec, C.byref(desc)), "fax_op_fp8_quantize")
+
+
+def fax_op_fp8_gemm(ctx, desc: Fp8GemmDesc):
+    _check(_L().fax_op_fp8_gemm(ctx, C.byref(desc)), "fax_op_fp8_gemm")

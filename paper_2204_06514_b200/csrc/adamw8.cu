@@ -1,0 +1,238 @@
+// Multi-tensor AdamW whose moments are held in 8 bits: m in e4m3, v in e5m2, each block of 128
+// elements with a power-of-two scale of its own.
+//
+//   m = s_m q_m, v = s_v q_v                       (exact: a power of two times a value of the format)
+//   m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g^2
+//   w <- w - lr wd w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+//   s = min { 2^k >= 2^-126 : max |m| / s <= 448 } over the block, q_m = SR(m / s); v likewise with 57344
+//
+// Why the moments are rounded stochastically: one step moves v by a share (1 - b2) of itself, far less
+// than half the distance between neighbouring 8-bit floats (12 % of the value), so the nearest value
+// would never move again.  SR(y) is the neighbour above with probability (y - below) / (above -
+// below): right on average.  A v above zero never becomes zero (its smallest value is kept instead):
+// m / (sqrt(0) + eps) would be a step out of all proportion.  Why e5m2 for v: it is a square, so it
+// needs twice the exponent range of m.  Why powers of two: m / s is then exact, the rounding is the
+// only loss, and the state after a step is one well-defined bit pattern (every float operation here is
+// rounded on its own, in the order written; no contraction).
+//
+// The rounding in integers: y 2^-120 (2^-112 for e5m2) puts the format's smallest normal value on
+// float32's, so that the float's bits, cut off after the format's mantissa, are the format's code,
+// subnormals included; adding 16 random bits below the cut carries into it with the right probability.
+//
+// HBM-bound: 18 bytes per element (w 8, g 4, m 2, v 2, bf16 copy 2) against 30 with float32 moments.
+// A warp takes one block of 128 elements at a time, four elements a lane, so that a block's maximum
+// is one warp reduction (redux) and every access is a full 32-byte sector or more.
+#include "common.cuh"
+
+#include <cuda_fp8.h>
+
+namespace {
+
+constexpr int QB = FAX_ADAMW8_BLOCK;   // elements per scale
+constexpr int THREADS = 256;
+constexpr int UNROLL = 2;              // blocks of 128 a warp has in flight
+constexpr int CHUNK = THREADS / 32 * UNROLL * QB;
+constexpr int MAX_T = 40;              // tensors per launch (kernel-parameter space)
+
+struct Adam8Tensor {
+  float* w; uint8_t* m; uint8_t* v; float* ms; float* vs; const void* g; bf16* wc;
+  unsigned long long n;
+  float wd;
+  uint32_t key;                        // random key of this tensor at this step
+  unsigned int first_chunk;            // prefix sum of chunk counts
+};
+struct Adam8Batch {
+  Adam8Tensor t[MAX_T];
+  int n_tensors;
+  unsigned int total_chunks;
+};
+struct Adam8Scalars { float lr, b1, b2, eps, inv_bc1, inv_bc2; };
+
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x7feb352du;
+  x = (x ^ (x >> 15)) * 0x846ca68bu;
+  return x ^ (x >> 16);
+}
+
+// Bits of |x| for the block's maximum; what is not finite does not count.
+__device__ __forceinline__ uint32_t finite_abs_bits(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
+  return u < 0x7f800000u ? u : 0u;
+}
+// Exponent field of the scale: the smallest power of two that brings the maximum to (1.75 2^TOP_EXP).
+template <int TOP_EXP>
+__device__ __forceinline__ int scale_field(uint32_t amax_bits) {
+  const int f = (int)((amax_bits + 0x1fffffu) >> 23) - TOP_EXP;
+  return amax_bits == 0u ? 127 : (f < 1 ? 1 : f);
+}
+// Stochastic rounding of |x| 2^(127 - field) to 8 bits.  BIAS_FIELD: exponent field of the factor that
+// lays the format's smallest normal value on float32's; CUT: mantissa bits dropped; TOP: largest code.
+template <int BIAS_FIELD, int CUT, uint32_t TOP, bool KEEP_ABOVE_ZERO>
+__device__ __forceinline__ uint32_t sr_code(float x, float inv, uint32_t r16) {
+  const float y = __fmul_rn(__fmul_rn(fabsf(x), inv), __uint_as_float((uint32_t)BIAS_FIELD << 23));
+  uint32_t c = (__float_as_uint(y) + (r16 << (CUT - 16)) + (1u << (CUT - 17))) >> CUT;
+  c = c < TOP ? c : TOP;
+  if (KEEP_ABOVE_ZERO) c = (c == 0u && x > 0.f) ? 1u : c;
+  if ((__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u) c = 0x7fu;      // not finite: NaN
+  return x < 0.f ? c | 0x80u : c;
+}
+
+__device__ __forceinline__ void decode4(uint32_t q, __nv_fp8_interpretation_t fmt, float scale, float (&x)[4]) {
+  const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q & 0xffffu), fmt)));
+  const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16), fmt)));
+  x[0] = __fmul_rn(a.x, scale); x[1] = __fmul_rn(a.y, scale); x[2] = __fmul_rn(b.x, scale); x[3] = __fmul_rn(b.y, scale);
+}
+
+template <bool G_BF16>
+__global__ void __launch_bounds__(THREADS)
+adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
+  fax_grid_dependency_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float omb1 = __fsub_rn(1.f, sc.b1), omb2 = __fsub_rn(1.f, sc.b2);
+  for (unsigned int chunk = blockIdx.x; chunk < batch.total_chunks; chunk += gridDim.x) {
+    int lo = 0, hi = batch.n_tensors - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (batch.t[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
+    }
+    const Adam8Tensor& t = batch.t[lo];
+    const float lrwd = __fmul_rn(sc.lr, t.wd);
+    const unsigned long long blk0 = (unsigned long long)(chunk - t.first_chunk) * (CHUNK / QB) + warp;
+
+    float w[UNROLL][4], g[UNROLL][4];
+    uint32_t mq[UNROLL], vq[UNROLL];
+    float sm[UNROLL], sv[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const unsigned long long blk = blk0 + (unsigned long long)u * (THREADS / 32), e = blk * QB + 4 * lane;
+      if (e + 4 <= t.n) {
+        const float4 f = *reinterpret_cast<const float4*>(t.w + e);
+        w[u][0] = f.x; w[u][1] = f.y; w[u][2] = f.z; w[u][3] = f.w;
+        if (G_BF16) {
+          const uint2 raw = *reinterpret_cast<const uint2*>((const bf16*)t.g + e);
+          const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.x));
+          const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.y));
+          g[u][0] = a.x; g[u][1] = a.y; g[u][2] = b.x; g[u][3] = b.y;
+        } else {
+          const float4 h = *reinterpret_cast<const float4*>((const float*)t.g + e);
+          g[u][0] = h.x; g[u][1] = h.y; g[u][2] = h.z; g[u][3] = h.w;
+        }
+        mq[u] = *reinterpret_cast<const uint32_t*>(t.m + e);
+        vq[u] = *reinterpret_cast<const uint32_t*>(t.v + e);
+      } else {
+        mq[u] = vq[u] = 0u;                          // past the end: zeros, which leave the block's maximum alone
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool in = e + j < t.n;
+          w[u][j] = in ? t.w[e + j] : 0.f;
+          g[u][j] = in ? (G_BF16 ? __bfloat162float(((const bf16*)t.g)[e + j]) : ((const float*)t.g)[e + j]) : 0.f;
+          if (in) { mq[u] |= (uint32_t)t.m[e + j] << (8 * j); vq[u] |= (uint32_t)t.v[e + j] << (8 * j); }
+        }
+      }
+      sm[u] = blk * QB < t.n ? t.ms[blk] : 0.f;
+      sv[u] = blk * QB < t.n ? t.vs[blk] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const unsigned long long blk = blk0 + (unsigned long long)u * (THREADS / 32), e = blk * QB + 4 * lane;
+      if (blk * QB >= t.n) continue;                 // the whole warp at once
+      float m[4], v[4];
+      decode4(mq[u], __NV_E4M3, sm[u], m);
+      decode4(vq[u], __NV_E5M2, sv[u], v);
+      uint32_t am = 0u, av = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[j] = __fadd_rn(__fmul_rn(sc.b1, m[j]), __fmul_rn(omb1, g[u][j]));
+        v[j] = __fadd_rn(__fmul_rn(sc.b2, v[j]), __fmul_rn(__fmul_rn(omb2, g[u][j]), g[u][j]));
+        const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[j], sc.inv_bc2)), sc.eps);
+        const float upd = __fdiv_rn(__fmul_rn(sc.lr, __fmul_rn(m[j], sc.inv_bc1)), den);
+        w[u][j] = __fsub_rn(__fsub_rn(w[u][j], __fmul_rn(lrwd, w[u][j])), upd);
+        am = max(am, finite_abs_bits(m[j]));
+        av = max(av, finite_abs_bits(v[j]));
+      }
+      const int fm = scale_field<8>(__reduce_max_sync(0xffffffffu, am));
+      const int fv = scale_field<15>(__reduce_max_sync(0xffffffffu, av));
+      const float im = __uint_as_float((uint32_t)(254 - fm) << 23), iv = __uint_as_float((uint32_t)(254 - fv) << 23);
+      const uint32_t key = t.key + (uint32_t)(e >> 32) * 0x85ebca77u;
+      uint32_t qm = 0u, qv = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t h = mix32((uint32_t)(e + j) ^ key);
+        qm |= sr_code<7, 20, 0x7eu, false>(m[j], im, h >> 16) << (8 * j);
+        qv |= sr_code<15, 21, 0x7bu, true>(v[j], iv, h & 0xffffu) << (8 * j);
+      }
+      if (e + 4 <= t.n) {
+        *reinterpret_cast<float4*>(t.w + e) = make_float4(w[u][0], w[u][1], w[u][2], w[u][3]);
+        *reinterpret_cast<uint32_t*>(t.m + e) = qm;
+        *reinterpret_cast<uint32_t*>(t.v + e) = qv;
+        if (t.wc) {
+          uint2 o;
+          *reinterpret_cast<__nv_bfloat162*>(&o.x) = __floats2bfloat162_rn(w[u][0], w[u][1]);
+          *reinterpret_cast<__nv_bfloat162*>(&o.y) = __floats2bfloat162_rn(w[u][2], w[u][3]);
+          *reinterpret_cast<uint2*>(t.wc + e) = o;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (e + j < t.n) {
+            t.w[e + j] = w[u][j];
+            t.m[e + j] = (uint8_t)(qm >> (8 * j)); t.v[e + j] = (uint8_t)(qv >> (8 * j));
+            if (t.wc) t.wc[e + j] = __float2bfloat16_rn(w[u][j]);
+          }
+      }
+      if (lane == 0) { t.ms[blk] = __uint_as_float((uint32_t)fm << 23); t.vs[blk] = __uint_as_float((uint32_t)fv << 23); }
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" fax_status fax_adamw8_step(fax_ctx* ctx, const fax_adamw8_tensor* tensors, int32_t n, const fax_adamw_hparams* hp) {
+  if (!ctx || !hp || n < 0 || (n > 0 && !tensors)) return FAX_ERR_INVALID_ARG;
+  FAX_TRY(fax_adamw_check_hparams(hp));
+  double total = 0;
+  for (int i = 0; i < n; ++i) {
+    const fax_adamw8_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    if (!t.w || !t.m || !t.v || !t.m_scale || !t.v_scale || !t.g) return FAX_ERR_INVALID_ARG;
+    if (!fax_aligned(t.w, 16) || !fax_aligned(t.g, 16) || !fax_aligned(t.m, 4) || !fax_aligned(t.v, 4) ||
+        !fax_aligned(t.m_scale, 4) || !fax_aligned(t.v_scale, 4) || (t.w_compute && !fax_aligned(t.w_compute, 8)))
+      return FAX_ERR_INVALID_ARG;
+    if ((t.n + CHUNK - 1) / CHUNK > 0xffffffffull) return FAX_ERR_UNSUPPORTED_SHAPE;
+    total += (double)t.n;
+  }
+  Adam8Scalars sc;
+  sc.lr = hp->lr; sc.b1 = hp->beta1; sc.b2 = hp->beta2; sc.eps = hp->eps;
+  sc.inv_bc1 = (float)(1.0 / (1.0 - pow((double)hp->beta1, (double)hp->step)));
+  sc.inv_bc2 = (float)(1.0 / (1.0 - pow((double)hp->beta2, (double)hp->step)));
+  FaxProfScope prof(ctx, KC_ADAMW, 0.0, total * (hp->grad_is_bf16 ? 16.0 : 18.0));
+  int i = 0;
+  while (i < n) {
+    Adam8Batch batch;
+    int k = 0;
+    unsigned long long chunks = 0;
+    while (i < n && k < MAX_T) {
+      const fax_adamw8_tensor& t = tensors[i];
+      const unsigned long long c = (t.n + CHUNK - 1) / CHUNK;
+      if (chunks + c > 0xffffffffull) break;                 // the next launch takes it
+      ++i;
+      if (t.n == 0) continue;
+      Adam8Tensor& b = batch.t[k];
+      b.w = t.w; b.m = (uint8_t*)t.m; b.v = (uint8_t*)t.v; b.ms = t.m_scale; b.vs = t.v_scale; b.g = t.g; b.wc = (bf16*)t.w_compute;
+      b.n = t.n; b.wd = t.weight_decay;
+      b.key = mix32(t.seed + (uint32_t)hp->step * 0x9e3779b9u);
+      b.first_chunk = (unsigned int)chunks;
+      chunks += c;
+      ++k;
+    }
+    if (k == 0) continue;                                    // only empty tensors were left
+    batch.n_tensors = k;
+    batch.total_chunks = (unsigned int)chunks;
+    const unsigned long long cap = (unsigned long long)ctx->sm_count * 16;
+    const unsigned int grid = (unsigned int)(chunks < cap ? chunks : cap);
+    if (hp->grad_is_bf16) fax_launch(ctx, adamw8_kernel<true>, dim3(grid), dim3(THREADS), 0, batch, sc);
+    else fax_launch(ctx, adamw8_kernel<false>, dim3(grid), dim3(THREADS), 0, batch, sc);
+    FAX_TRY(fax_after_launch(ctx));
+  }
+  return FAX_OK;
+}

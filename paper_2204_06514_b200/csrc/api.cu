@@ -174,13 +174,14 @@ extern "C" fax_status fax_profile_begin(fax_ctx* ctx) {
 }
 
 extern "C" fax_status fax_profile_end(fax_ctx* ctx, fax_profile_entry* out, int32_t n_out) {
-  if (!ctx || !out || n_out < FAX_KERNEL_CLASSES) return FAX_ERR_INVALID_ARG;
+  if (!ctx || !out || n_out < FAX_KERNEL_CLASSES_MIN) return FAX_ERR_INVALID_ARG;
+  const int n = n_out < FAX_KERNEL_CLASSES ? n_out : FAX_KERNEL_CLASSES;
   ctx->prof_on = false;
   FAX_CUDA_TRY(ctx, cudaStreamSynchronize(ctx->stream));
-  for (int i = 0; i < FAX_KERNEL_CLASSES; ++i) { out[i].launches = 0; out[i].ms = 0; out[i].flops = 0; out[i].bytes = 0; }
+  for (int i = 0; i < n; ++i) { out[i].launches = 0; out[i].ms = 0; out[i].flops = 0; out[i].bytes = 0; }
   for (FaxProfRec& r : ctx->prof) {
     float ms = 0.f;
-    if (cudaEventElapsedTime(&ms, r.e0, r.e1) == cudaSuccess && r.cls >= 0 && r.cls < FAX_KERNEL_CLASSES) {
+    if (cudaEventElapsedTime(&ms, r.e0, r.e1) == cudaSuccess && r.cls >= 0 && r.cls < n) {
       out[r.cls].launches += 1; out[r.cls].ms += ms; out[r.cls].flops += r.flops; out[r.cls].bytes += r.bytes;
     }
     cudaEventDestroy(r.e0); cudaEventDestroy(r.e1);
@@ -191,6 +192,8 @@ extern "C" fax_status fax_profile_end(fax_ctx* ctx, fax_profile_entry* out, int3
 
 extern "C" const char* fax_kernel_class_name(int32_t cls) {
   static const char* names[FAX_KERNEL_CLASSES] = {"gemm_tcgen05", "gemm_simt", "attention_fwd", "attention_bwd",
-                                                  "layernorm_fwd", "layernorm_bwd", "adamw", "colsum", "embed", "xent"};
+                                                  "layernorm_fwd", "layernorm_bwd", "adamw", "colsum", "embed", "xent",
+                                                  "fp8_quantize", "fp8_gemm"};
+  static_assert(KC_COUNT == FAX_KERNEL_CLASSES, "class names");
   return (cls >= 0 && cls < FAX_KERNEL_CLASSES) ? names[cls] : "unknown";
 }

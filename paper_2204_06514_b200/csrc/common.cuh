@@ -16,7 +16,7 @@ typedef __nv_bfloat16 bf16;
 // Kernel classes of the per-kernel profile (order fixed by fax.h).
 enum FaxKernelClass {
   KC_GEMM_TC = 0, KC_GEMM_SIMT, KC_ATTN_FWD, KC_ATTN_BWD, KC_LN_FWD, KC_LN_BWD, KC_ADAMW, KC_COLSUM,
-  KC_EMBED, KC_XENT, KC_COUNT
+  KC_EMBED, KC_XENT, KC_FP8_QUANT, KC_FP8_GEMM, KC_COUNT
 };
 struct FaxProfRec { int cls; cudaEvent_t e0, e1; double flops, bytes; };
 
@@ -294,6 +294,11 @@ fax_status fax_embed_fwd(fax_ctx* ctx, int prec, int B, int T, int d, int vocab,
                          const void* wte, const void* wpe, void* x0);
 fax_status fax_embed_bwd(fax_ctx* ctx, int prec, int B, int T, int max_seq, int d, int vocab,
                          const int32_t* ids, const void* dx0, float* dwte, float* dwpe, bool accumulate_wpe);
+// Scaled lookup, and the table's gradient by sorted tokens (see embedding.cu); n = 0 is allowed.
+fax_status fax_embedding_lookup(fax_ctx* ctx, int prec, int n, int vocab, int d, const int32_t* ids, const void* table, float scale, void* out);
+size_t fax_embedding_grad_scratch_bytes(int n, int vocab, int d);
+fax_status fax_embedding_grad(fax_ctx* ctx, int prec, int n, int vocab, int d, const int32_t* ids, const void* dout, float scale,
+                              bool accumulate, float* dtable, void* scratch, size_t scratch_bytes);
 fax_status fax_xent(fax_ctx* ctx, int prec, int rows, int vocab, void* logits, int64_t ld,
                     const int32_t* targets, float inv_n, float* row_loss);
 fax_status fax_loss_mean(fax_ctx* ctx, int n, const float* row_loss, float* loss);
