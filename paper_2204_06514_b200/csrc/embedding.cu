@@ -13,9 +13,13 @@
 //     digit of the tile each token lands in (whole-number atomics: the sums do not depend on their order).
 //  2. embed_grad: chunks of consecutive sorted tokens.  A run of equal ids inside a chunk is summed in
 //     registers and written; a run that crosses a chunk's edge leaves partial sums (at most a first and
-//     a last one per chunk).  When the table is overwritten, further blocks of the same launch zero the rows
-//     that no token touches.
-//  3. embed_join: adds the partial sums of each run that crossed an edge, in chunk order.
+//     a last one per chunk), and the chunk it begins in is listed.
+//  3. embed_join: adds the partial sums of each listed run in chunk order.
+//
+// An overwritten table has to be zeroed where no token touches it, most of the bytes of a small batch.
+// Where the rows that can be touched are few, further blocks of the sort's launches zero the whole table
+// meanwhile (the sort is latency, the zeros are bandwidth; touched rows are written twice); where they are
+// many, the sort marks them and further blocks of embed_grad zero the others.
 #include "common.cuh"
 
 namespace {
@@ -27,7 +31,10 @@ constexpr int TILE_UNIT = 512;         // tokens per tile: a multiple of this
 constexpr int MAX_TILES = 256;         // a scatter block reads every tile's counts of its pass
 constexpr int MAX_TOKENS = 1 << 30;    // token and tile positions stay within 32 bits
 constexpr int GRAD_THREADS = 128;
-constexpr int JOIN_GROUPS = 8;
+constexpr int JOIN_WARPS = 8;
+constexpr int JOIN_SHORT = 8;          // a run over at most this many further chunks is joined by one warp per 128 columns
+// Rows of a batch that may be written twice for the zeros to run under the sort: at HBM rate about what the sort takes.
+constexpr double PREFILL_BYTES = 64e6;
 
 struct SortPlan {
   int n, tile, tiles, passes, bits;    // bits per pass
@@ -52,7 +59,8 @@ SortPlan plan_for(int n, int vocab) {
 }
 
 struct EmbedScratch {
-  uint32_t* counts;                    // [passes][tiles][DIGITS]
+  uint32_t* counts;                    // [passes][tiles][DIGITS], then the lengths of the two lists
+  uint32_t* lists;                     // [2][chunks]: chunks in which a short / long run begins that goes on
   uint8_t* touched;                    // [vocab]
   uint2* a; uint2* b;                  // (id, token) before and after a pass
   float* partial;                      // [chunks][2][d]: first run's part, last run's part
@@ -60,8 +68,9 @@ struct EmbedScratch {
 };
 
 void carve(FaxArena& ar, const SortPlan& p, int vocab, int d, EmbedScratch* s) {
-  s->count_words = (size_t)p.passes * p.tiles * DIGITS;
+  s->count_words = (size_t)p.passes * p.tiles * DIGITS + 4;
   s->counts = (uint32_t*)ar.take(s->count_words * 4);
+  s->lists = (uint32_t*)ar.take((size_t)p.chunks * 2 * 4);
   s->touched = (uint8_t*)ar.take(fax_round_up((size_t)vocab, 16));
   s->a = (uint2*)ar.take((size_t)p.n * sizeof(uint2));
   s->b = (uint2*)ar.take((size_t)p.n * sizeof(uint2));
@@ -119,38 +128,46 @@ embed_lookup_kernel(int n, int vocab, int nvec, int parts, const int32_t* __rest
 }
 
 // ---- sort ----
+// This launch's share of zeroing the table, done by the blocks behind the sort's.
+struct Fill { float4* p; unsigned long long lo, hi; };               // vectors [lo, hi)
+__device__ __forceinline__ void fill_zero(const Fill& f, unsigned int first_block) {
+  const unsigned long long step = (unsigned long long)(gridDim.x - first_block) * SORT_THREADS;
+  for (unsigned long long i = f.lo + (unsigned long long)(blockIdx.x - first_block) * SORT_THREADS + threadIdx.x; i < f.hi; i += step)
+    f.p[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
 __global__ void __launch_bounds__(SORT_THREADS)
 embed_sort_count_kernel(SortPlan p, int vocab, const int32_t* __restrict__ ids, uint32_t* __restrict__ counts,
-                        unsigned long long later_words, uint4* __restrict__ touched, unsigned long long touched_vecs) {
+                        unsigned long long later_words, uint4* __restrict__ touched, unsigned long long touched_vecs, Fill fill) {
   __shared__ uint32_t hist[DIGITS];
   for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) hist[i] = 0u;
   __syncthreads();
   fax_grid_dependency_wait();
-  const unsigned long long tid = (unsigned long long)blockIdx.x * SORT_THREADS + threadIdx.x, step = (unsigned long long)gridDim.x * SORT_THREADS;
-  uint32_t* later = counts + (size_t)p.tiles * DIGITS;              // the counts of the passes after the first
+  if (blockIdx.x >= p.tiles) { fill_zero(fill, p.tiles); return; }
+  const unsigned long long tid = (unsigned long long)blockIdx.x * SORT_THREADS + threadIdx.x, step = (unsigned long long)p.tiles * SORT_THREADS;
+  uint32_t* later = counts + (size_t)p.tiles * DIGITS;              // the counts of the passes after the first, and the lists' lengths
   for (unsigned long long i = tid; i < later_words; i += step) later[i] = 0u;
   for (unsigned long long i = tid; i < touched_vecs; i += step) touched[i] = make_uint4(0u, 0u, 0u, 0u);
-  for (int t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-    const int lo = t * p.tile, hi = min(p.n, lo + p.tile);
-    for (int i = lo + threadIdx.x; i < hi; i += SORT_THREADS)
-      atomicAdd(&hist[key_of(ids[i], vocab) & ((1u << p.bits) - 1u)], 1u);
-    __syncthreads();
-    for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) { counts[(size_t)t * DIGITS + i] = hist[i]; hist[i] = 0u; }
-    __syncthreads();
-  }
+  const int lo = blockIdx.x * p.tile, hi = min(p.n, lo + p.tile);
+  for (int i = lo + threadIdx.x; i < hi; i += SORT_THREADS)
+    atomicAdd(&hist[key_of(ids[i], vocab) & ((1u << p.bits) - 1u)], 1u);
+  __syncthreads();
+  for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) counts[(size_t)blockIdx.x * DIGITS + i] = hist[i];
 }
 
-// One tile per block.  FIRST: the tokens are read from ids, and the table rows they touch are marked.
+// One tile per block.  FIRST: the tokens are read from ids, and the table rows they touch are marked (touched not null).
 template <bool FIRST>
 __global__ void __launch_bounds__(SORT_THREADS)
 embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __restrict__ ids, const uint2* __restrict__ in,
-                          uint2* __restrict__ out, uint32_t* __restrict__ counts, uint8_t* __restrict__ touched) {
-  __shared__ uint32_t before[2][DIGITS], total[2][DIGITS];          // two halves of the tiles
+                          uint2* __restrict__ out, uint32_t* __restrict__ counts, uint8_t* __restrict__ touched, Fill fill) {
+  constexpr int QUADS = DIGITS / 4, TILE_GROUPS = SORT_THREADS / QUADS;    // a thread reads four digits of every eighth tile
+  __shared__ uint4 before[TILE_GROUPS][QUADS], total[TILE_GROUPS][QUADS];
   __shared__ uint32_t warp_total[8];
   __shared__ uint32_t off[SORT_WARPS][DIGITS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < SORT_WARPS * DIGITS; i += SORT_THREADS) (&off[0][0])[i] = 0u;
   fax_grid_dependency_wait();
+  if (blockIdx.x >= p.tiles) { fill_zero(fill, p.tiles); return; }
   const int t = blockIdx.x;
   const int shift = pass * p.bits;
   const uint32_t mask = (1u << p.bits) - 1u;
@@ -160,27 +177,30 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
 
   // counts of the tiles before this one, and of all tiles, by digit
   {
-    const uint32_t* c = counts + (size_t)pass * p.tiles * DIGITS;
-    const int dgt = threadIdx.x & (DIGITS - 1), half = threadIdx.x >> 8;
-    const int mid = (p.tiles + 1) / 2, t0 = half ? mid : 0, t1 = half ? p.tiles : mid;
-    uint32_t b = 0u, all = 0u;
+    const uint4* c = reinterpret_cast<const uint4*>(counts + (size_t)pass * p.tiles * DIGITS);
+    const int quad = threadIdx.x % QUADS, grp = threadIdx.x / QUADS;
+    uint4 b = make_uint4(0u, 0u, 0u, 0u), all = b;
 #pragma unroll 8
-    for (int i = t0; i < t1; ++i) {
-      const uint32_t x = c[(size_t)i * DIGITS + dgt];
-      b += i < t ? x : 0u;
-      all += x;
+    for (int i = grp; i < p.tiles; i += TILE_GROUPS) {
+      const uint4 x = c[(size_t)i * QUADS + quad];
+      all.x += x.x; all.y += x.y; all.z += x.z; all.w += x.w;
+      if (i < t) { b.x += x.x; b.y += x.y; b.z += x.z; b.w += x.w; }
     }
-    before[half][dgt] = b;
-    total[half][dgt] = all;
+    before[grp][quad] = b;
+    total[grp][quad] = all;
   }
   __syncthreads();
   // this tile's digits, by warp
   auto load = [&](int i) { return FIRST ? make_uint2(key_of(ids[i], vocab), (uint32_t)i) : in[i]; };
   for (int i = w_lo + lane; i < w_hi; i += 32) atomicAdd(&off[warp][(load(i).x >> shift) & mask], 1u);
   // exclusive sum of all tiles' totals over the digits
-  uint32_t x = 0u, incl = 0u;
+  uint32_t x = 0u, mine = 0u, incl = 0u;
   if (threadIdx.x < DIGITS) {
-    x = total[0][threadIdx.x] + total[1][threadIdx.x];
+#pragma unroll
+    for (int g = 0; g < TILE_GROUPS; ++g) {
+      x += reinterpret_cast<const uint32_t*>(total[g])[threadIdx.x];
+      mine += reinterpret_cast<const uint32_t*>(before[g])[threadIdx.x];
+    }
     incl = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -191,9 +211,9 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
   }
   __syncthreads();
   if (threadIdx.x < DIGITS) {
-    uint32_t add = 0u;
-    for (int w = 0; w < warp; ++w) add += warp_total[w];
-    uint32_t at = add + incl - x + before[0][threadIdx.x] + before[1][threadIdx.x];
+    uint32_t at = incl - x + mine;
+    for (int w = 0; w < warp; ++w) at += warp_total[w];
+#pragma unroll
     for (int w = 0; w < SORT_WARPS; ++w) {                           // where each warp's tokens of this digit begin
       const uint32_t c = off[w][threadIdx.x];
       off[w][threadIdx.x] = at;
@@ -217,7 +237,7 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
     if (live) {
       out[at] = kv;
       if (more) atomicAdd(next + (size_t)(at / (uint32_t)p.tile) * DIGITS + ((kv.x >> (shift + p.bits)) & mask), 1u);
-      if (FIRST && kv.x < (uint32_t)vocab) touched[kv.x] = 1;
+      if (FIRST && touched != nullptr && kv.x < (uint32_t)vocab) touched[kv.x] = 1;
     }
   }
 }
@@ -228,7 +248,8 @@ template <typename T, int V>
 __global__ void __launch_bounds__(GRAD_THREADS)
 embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices, unsigned int grad_blocks, const uint2* __restrict__ sorted,
                   const T* __restrict__ dout, float scale, int accumulate, float* __restrict__ dtable,
-                  float* __restrict__ partial, const uint8_t* __restrict__ touched) {
+                  float* __restrict__ partial, const uint8_t* __restrict__ touched, uint32_t* __restrict__ list_len,
+                  uint32_t* __restrict__ lists) {
   typedef typename Vec<T, V>::type vec;
   fax_grid_dependency_wait();
   if (blockIdx.x >= grad_blocks) {
@@ -262,6 +283,11 @@ embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices,
       float* o = partial + ((size_t)chunk * 2 + (from_before ? 0 : 1)) * d + (size_t)c * V;
 #pragma unroll
       for (int j = 0; j < V; ++j) o[j] = acc[j];
+      if (!from_before && c == 0) {
+        const size_t far = (size_t)(chunk + 1 + JOIN_SHORT) * p.chunk;
+        const int which = far < (size_t)p.n && sorted[far].x == key ? 1 : 0;
+        lists[(size_t)which * p.chunks + atomicAdd(list_len + which, 1u)] = (uint32_t)chunk;
+      }
     } else {
       float* o = dtable + (size_t)key * d + (size_t)c * V;
 #pragma unroll
@@ -311,61 +337,94 @@ embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices,
   flush(cur, first_run, true);
 }
 
-// The runs that crossed a chunk's edge: block (chunk, slice of 32 columns); nothing to do unless a run begins
-// in this chunk and goes on.  JOIN_GROUPS warps take the following chunks in turn; their sums are added in order.
-__global__ void __launch_bounds__(32 * JOIN_GROUPS)
-embed_join_kernel(SortPlan p, int vocab, int d, int slices, const uint2* __restrict__ sorted, const float* __restrict__ partial, float scale,
-                  int accumulate, float* __restrict__ dtable) {
-  __shared__ float part[JOIN_GROUPS][32];
+// The runs that crossed a chunk's edge.  Items: a listed short run and 1024 columns of it (a warp for each 128),
+// then a listed long run and 128 columns (the warps take its chunks in equal parts, whose sums are added in order).
+template <bool WIDE>
+__global__ void __launch_bounds__(32 * JOIN_WARPS)
+embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const float* __restrict__ partial, const uint32_t* __restrict__ list_len,
+                  const uint32_t* __restrict__ lists, float scale, int accumulate, float* __restrict__ dtable) {
+  __shared__ float4 part[JOIN_WARPS][32];
   fax_grid_dependency_wait();
-  const int chunk = blockIdx.x / slices, slice = blockIdx.x - chunk * slices;
-  const int lo = chunk * p.chunk, hi = lo + p.chunk;
-  if (hi >= p.n) return;                                             // the last chunk: nothing follows
-  const uint32_t key = sorted[hi - 1].x;
-  if (key >= (uint32_t)vocab || sorted[hi].x != key) return;         // its last run ends here
-  if (lo > 0 && sorted[lo - 1].x == key && sorted[lo].x == key) return;   // the run began before this chunk
-  // the run's last chunk: chunks after this one whose first token still has the key (binary search, sorted)
-  int a = chunk + 1, b = p.chunks - 1;
-  while (a < b) {
-    const int m = (a + b + 1) >> 1;
-    if (sorted[(size_t)m * p.chunk].x == key) a = m; else b = m - 1;
-  }
-  const int last = a;
-  const int col = slice * 32 + (threadIdx.x & 31), grp = threadIdx.x >> 5;
-  const int count = last - chunk, per = (count + JOIN_GROUPS - 1) / JOIN_GROUPS;
-  const int c0 = chunk + 1 + grp * per, c1 = min(last + 1, c0 + per);
-  float s = 0.f;
-  if (col < d) {
-#pragma unroll 8
-    for (int c = c0; c < c1; ++c) s += partial[(size_t)c * 2 * d + col];
-  }
-  part[grp][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (grp == 0 && col < d) {
-    float t = partial[((size_t)chunk * 2 + 1) * d + col];
-#pragma unroll
-    for (int w = 0; w < JOIN_GROUPS; ++w) t += part[w][threadIdx.x];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long slices = (d + 127) / 128, groups = (slices + JOIN_WARPS - 1) / JOIN_WARPS;
+  const long long n_short = list_len[0] * groups, n_items = n_short + list_len[1] * slices;
+  auto load = [&](const float* row, int col) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (WIDE) { if (col < d) v = *reinterpret_cast<const float4*>(row + col); }
+    else {
+      if (col < d) v.x = row[col];
+      if (col + 1 < d) v.y = row[col + 1];
+      if (col + 2 < d) v.z = row[col + 2];
+      if (col + 3 < d) v.w = row[col + 3];
+    }
+    return v;
+  };
+  auto add = [](float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; };
+  auto finish = [&](uint32_t key, int col, const float4& t) {
+    const float f[4] = {scale * t.x, scale * t.y, scale * t.z, scale * t.w};
     float* o = dtable + (size_t)key * d + col;
-    *o = accumulate ? *o + scale * t : scale * t;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (col + j < d) o[j] = accumulate ? o[j] + f[j] : f[j];
+  };
+  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const bool is_long = item >= n_short;
+    const long long k = is_long ? item - n_short : item, per = is_long ? slices : groups;
+    const int chunk = (int)lists[(is_long ? (size_t)p.chunks : 0) + (size_t)(k / per)];
+    const int slice = is_long ? (int)(k % per) : (int)(k % per) * JOIN_WARPS + warp;
+    const int col = slice * 128 + 4 * lane;
+    const uint32_t key = sorted[(size_t)(chunk + 1) * p.chunk].x;
+    // the chunks after this one that begin with the key
+    int count = 0;
+    for (int c = chunk + 1;; c += 32) {
+      const bool same = c + lane < p.chunks && sorted[(size_t)(c + lane) * p.chunk].x == key;
+      const uint32_t m = __ballot_sync(0xffffffffu, same);
+      count += __popc(m);
+      if (m != 0xffffffffu) break;
+    }
+    const float* first = partial + ((size_t)chunk * 2 + 1) * d;
+    const float* rest = partial + (size_t)(chunk + 1) * 2 * d;       // slot 0 of the next chunk
+    if (!is_long) {
+      if (slice < slices) {
+        float4 t = load(first, col);
+#pragma unroll 8
+        for (int c = 0; c < count; ++c) add(t, load(rest + (size_t)c * 2 * d, col));
+        finish(key, col, t);
+      }
+    } else {
+      const int share = (count + JOIN_WARPS - 1) / JOIN_WARPS, c1 = min(count, (warp + 1) * share);
+      float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 16
+      for (int c = warp * share; c < c1; ++c) add(t, load(rest + (size_t)c * 2 * d, col));
+      part[warp][lane] = t;
+      __syncthreads();
+      if (warp == 0) {
+        float4 u = load(first, col);
+#pragma unroll
+        for (int w = 0; w < JOIN_WARPS; ++w) add(u, part[w][lane]);
+        finish(key, col, u);
+      }
+      __syncthreads();
+    }
   }
 }
 
 template <typename T, int V>
 fax_status launch_grad(fax_ctx* ctx, const SortPlan& p, int vocab, int d, const uint2* sorted, const void* dout, float scale,
-                       int accumulate, float* dtable, const EmbedScratch& s) {
+                       int accumulate, bool fill_here, float* dtable, const EmbedScratch& s) {
   const int nvec = d / V;
   int lanes = 1;
   while (lanes < nvec && lanes < GRAD_THREADS) lanes *= 2;
   const int slices = (nvec + lanes - 1) / lanes, groups = GRAD_THREADS / lanes;
   const long long items = (long long)p.chunks * slices, gb = (items + groups - 1) / groups;
   long long zb = 0;
-  if (!accumulate) {
+  if (fill_here) {
     zb = ((long long)vocab + GRAD_THREADS / 32 - 1) / (GRAD_THREADS / 32);
     if (zb > (long long)ctx->sm_count * 16) zb = (long long)ctx->sm_count * 16;
   }
   if (gb + zb > 0x7fffffffLL) return FAX_ERR_UNSUPPORTED_SHAPE;
   fax_launch(ctx, embed_grad_kernel<T, V>, dim3((unsigned int)(gb + zb)), dim3(GRAD_THREADS), 0, p, vocab, d, nvec, lanes, slices,
-             (unsigned int)gb, sorted, (const T*)dout, scale, accumulate, dtable, s.partial, (const uint8_t*)s.touched);
+             (unsigned int)gb, sorted, (const T*)dout, scale, accumulate, dtable, s.partial, (const uint8_t*)s.touched, s.counts + s.count_words - 4, s.lists);
   return fax_after_launch(ctx);
 }
 
@@ -414,33 +473,55 @@ fax_status fax_embedding_grad(fax_ctx* ctx, int prec, int n, int vocab, int d, c
   FaxArena ar(scratch, scratch_bytes);
   EmbedScratch s;
   carve(ar, p, vocab, d, &s);
-  const unsigned long long later = s.count_words - (size_t)p.tiles * DIGITS, tv = fax_round_up((size_t)vocab, 16) / 16;
-  fax_launch(ctx, embed_sort_count_kernel, dim3(p.tiles > ctx->sm_count ? p.tiles : ctx->sm_count), dim3(SORT_THREADS), 0, p, vocab, ids, s.counts, later,
-             (uint4*)s.touched, tv);
+  const bool wide = fax_aligned(dout, 16) && fax_aligned(dtable, 16);
+  const double rows = n < vocab ? n : vocab;
+  const bool prefill = !accumulate && fax_aligned(dtable, 16) && ((size_t)vocab * d) % 4 == 0 && rows * d * 4.0 <= PREFILL_BYTES;
+  const bool mark = !accumulate && !prefill;
+  const unsigned long long later = s.count_words - (size_t)p.tiles * DIGITS, tv = mark ? fax_round_up((size_t)vocab, 16) / 16 : 0;
+  // the zeros in equal shares under the counting and each pass
+  const unsigned long long vecs = prefill ? (unsigned long long)vocab * d / 4 : 0, shares = p.passes + 1;
+  const unsigned long long share = (vecs + shares - 1) / shares;
+  auto part = [&](unsigned long long k) {
+    Fill f;
+    f.p = (float4*)dtable;
+    f.lo = k * share < vecs ? k * share : vecs;
+    f.hi = f.lo + share < vecs ? f.lo + share : vecs;
+    return f;
+  };
+  auto fill_blocks = [&](const Fill& f) {
+    const unsigned long long want = (f.hi - f.lo + 4 * SORT_THREADS - 1) / (4 * SORT_THREADS), cap = (unsigned long long)ctx->sm_count * 4;
+    return (unsigned int)(want < cap ? want : cap);
+  };
+  Fill f = part(0);
+  fax_launch(ctx, embed_sort_count_kernel, dim3(p.tiles + fill_blocks(f)), dim3(SORT_THREADS), 0, p, vocab, ids, s.counts, later, (uint4*)s.touched, tv, f);
   FAX_TRY(fax_after_launch(ctx));
   for (int pass = 0; pass < p.passes; ++pass) {
     uint2* out = (pass & 1) ? s.b : s.a;
     const uint2* in = (pass & 1) ? s.a : s.b;
+    f = part(pass + 1);
+    const dim3 grid(p.tiles + fill_blocks(f));
     if (pass == 0)
-      fax_launch(ctx, embed_sort_scatter_kernel<true>, dim3(p.tiles), dim3(SORT_THREADS), 0, p, pass, vocab, ids, in, out, s.counts, s.touched);
+      fax_launch(ctx, embed_sort_scatter_kernel<true>, grid, dim3(SORT_THREADS), 0, p, pass, vocab, ids, in, out, s.counts, mark ? s.touched : (uint8_t*)nullptr, f);
     else
-      fax_launch(ctx, embed_sort_scatter_kernel<false>, dim3(p.tiles), dim3(SORT_THREADS), 0, p, pass, vocab, ids, in, out, s.counts, s.touched);
+      fax_launch(ctx, embed_sort_scatter_kernel<false>, grid, dim3(SORT_THREADS), 0, p, pass, vocab, ids, in, out, s.counts, (uint8_t*)nullptr, f);
     FAX_TRY(fax_after_launch(ctx));
   }
   const uint2* sorted = ((p.passes - 1) & 1) ? s.b : s.a;
-  const bool wide = fax_aligned(dout, 16) && fax_aligned(dtable, 16);
   const int acc = accumulate ? 1 : 0;
   if (prec == FAX_PREC_BF16)
-    FAX_TRY((wide && d % 8 == 0 ? launch_grad<bf16, 8>(ctx, p, vocab, d, sorted, dout, scale, acc, dtable, s)
-                                : launch_grad<bf16, 1>(ctx, p, vocab, d, sorted, dout, scale, acc, dtable, s)));
+    FAX_TRY((wide && d % 8 == 0 ? launch_grad<bf16, 8>(ctx, p, vocab, d, sorted, dout, scale, acc, mark, dtable, s)
+                                : launch_grad<bf16, 1>(ctx, p, vocab, d, sorted, dout, scale, acc, mark, dtable, s)));
   else
-    FAX_TRY((wide && d % 4 == 0 ? launch_grad<float, 4>(ctx, p, vocab, d, sorted, dout, scale, acc, dtable, s)
-                                : launch_grad<float, 1>(ctx, p, vocab, d, sorted, dout, scale, acc, dtable, s)));
+    FAX_TRY((wide && d % 4 == 0 ? launch_grad<float, 4>(ctx, p, vocab, d, sorted, dout, scale, acc, mark, dtable, s)
+                                : launch_grad<float, 1>(ctx, p, vocab, d, sorted, dout, scale, acc, mark, dtable, s)));
   if (p.chunks > 1) {
-    const int slices = (d + 31) / 32;
-    if ((long long)p.chunks * slices > 0x7fffffffLL) return FAX_ERR_UNSUPPORTED_SHAPE;
-    fax_launch(ctx, embed_join_kernel, dim3((unsigned int)((long long)p.chunks * slices)), dim3(32 * JOIN_GROUPS), 0, p, vocab, d, slices, sorted,
-               (const float*)s.partial, scale, acc, dtable);
+    const long long items = (long long)p.chunks * ((d + 1023) / 1024), cap = (long long)ctx->sm_count * 8;
+    const dim3 grid((unsigned int)(items < cap ? items : cap));
+    const uint32_t* len = s.counts + s.count_words - 4;
+    if (d % 4 == 0)
+      fax_launch(ctx, embed_join_kernel<true>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint32_t*)s.lists, scale, acc, dtable);
+    else
+      fax_launch(ctx, embed_join_kernel<false>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint32_t*)s.lists, scale, acc, dtable);
     FAX_TRY(fax_after_launch(ctx));
   }
   return FAX_OK;

@@ -11,7 +11,8 @@
 //
 //   warp 0      : TMA producer (both CTAs; each loads its 128 rows of A and its half of B)
 //   warp 1      : tensor-memory allocation (both CTAs), MMA issue (even CTA)
-//   warps 2..9  : 128 rows x 256 columns of the CTA: warp w owns 32 rows and 128 columns, 128 sums a lane
+//   warps 2, 3  : none (they give their registers to the row warps)
+//   warps 4..11 : 128 rows x 256 columns of the CTA: warp w owns 32 rows and 128 columns, 128 sums a lane
 //
 // Edges: TMA fills what lies outside a matrix with zeros, the scales of rows outside are taken as 0, and
 // the stores are limited to C.  Every wait is bounded.
@@ -27,7 +28,10 @@ constexpr int BN = 256;            // columns per pair; each CTA stages 128 of B
 constexpr int BNH = 128;
 constexpr int BK = FAX_FP8_BLOCK;  // bytes = elements
 constexpr int NUM_EPI_WARPS = 8;
-constexpr int NUM_THREADS = 32 * (2 + NUM_EPI_WARPS);
+constexpr int NUM_THREADS = 32 * (4 + NUM_EPI_WARPS);
+// 168 registers a thread at launch (65536 / 384); 128 x 40 + 256 x 232 = 384 x 168
+constexpr int REGS_LOAD = 40, REGS_ROWS = 232;
+static_assert(128 * REGS_LOAD + 256 * REGS_ROWS <= 384 * 168, "register split");
 constexpr int A_BYTES = BM * BK, B_BYTES = BNH * BK, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int STAGES = 6;
 constexpr int TMEM_COLS = 512;
@@ -83,26 +87,49 @@ __device__ __forceinline__ void tc_mma_fp8_pair(uint32_t d_tmem, uint64_t adesc,
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// 16 columns of the accumulator, scaled, into the sums.  s: sa (times sb where a block of B has one scale).
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+  uint32_t a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+  lo = __uint_as_float(a); hi = __uint_as_float(b);
+}
+// Two float32 products or fused multiply-adds in one instruction.
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// 32 columns of the accumulator, scaled, into the sums.  s: sa twice (times sb where a block of B has one scale).
 template <bool B_ROWS>
-__device__ __forceinline__ void add_scaled(const uint32_t (&r)[16], float s, const float4* sb, float* acc) {
+__device__ __forceinline__ void add_scaled(const uint32_t (&r)[32], uint64_t s, const ulonglong2* sb, uint64_t* sum) {
 #pragma unroll
-  for (int j4 = 0; j4 < 4; ++j4) {
+  for (int j = 0; j < 8; ++j) {
     if (B_ROWS) {
-      const float4 b = sb[j4];
-      acc[4 * j4] = fmaf(__uint_as_float(r[4 * j4]), s * b.x, acc[4 * j4]);
-      acc[4 * j4 + 1] = fmaf(__uint_as_float(r[4 * j4 + 1]), s * b.y, acc[4 * j4 + 1]);
-      acc[4 * j4 + 2] = fmaf(__uint_as_float(r[4 * j4 + 2]), s * b.z, acc[4 * j4 + 2]);
-      acc[4 * j4 + 3] = fmaf(__uint_as_float(r[4 * j4 + 3]), s * b.w, acc[4 * j4 + 3]);
+      const ulonglong2 b = sb[j];
+      sum[2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), mul2(s, b.x), sum[2 * j]);
+      sum[2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), mul2(s, b.y), sum[2 * j + 1]);
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[4 * j4 + e] = fmaf(__uint_as_float(r[4 * j4 + e]), s, acc[4 * j4 + e]);
+      sum[2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), s, sum[2 * j]);
+      sum[2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), s, sum[2 * j + 1]);
     }
   }
 }
 
 // One lane's 128 sums of row `row`, columns col0 .. col0 + 127.
-__device__ __forceinline__ void store_row(const Fp8Params& p, const float (&acc)[128], long long row, int col0) {
+__device__ __forceinline__ void store_row(const Fp8Params& p, const uint64_t (&sum)[64], long long row, int col0) {
+  float acc[128];
+#pragma unroll
+  for (int j = 0; j < 64; ++j) unpack2(sum[j], acc[2 * j], acc[2 * j + 1]);
   if (row >= p.M || col0 >= p.N) return;
   if (p.wide && col0 + 128 <= p.N) {
 #pragma unroll
@@ -195,6 +222,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
   const uint32_t tmem_base = *tmem_base_slot;
   fax_grid_dependency_wait();    // global memory only from here
 
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LOAD));
   if (warp == 0) {
     // ---------------- TMA producer ----------------
     if (lane == 0) {
@@ -241,10 +270,12 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         }
       }
     }
+  }
   } else {
     // ---------------- row warps ----------------
-    const int q = warp & 3, half = (warp - 2) >> 2;
-    float* my_scales = scales + (warp - 2) * 2 * 128;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    float* my_scales = scales + (warp - 4) * 2 * 128;
     int acc = 0; uint32_t acc_phase = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
@@ -259,9 +290,9 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[j] = col0 + 32 * j + lane < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + col0 + 32 * j + lane) : 0.f;
       };
-      float sum[128];
+      uint64_t sum[64];
 #pragma unroll
-      for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+      for (int j = 0; j < 64; ++j) sum[j] = 0ull;
       float sa_next = load_sa(0), sb_next = 0.f, sbv[4];
       if (B_ROWS) load_sb(0, sbv); else sb_next = load_sb1(0);
       for (int kb = 0; kb < kb_total; ++kb) {
@@ -279,23 +310,22 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_co
         if (!mbar_wait_warp(tfull_bar(acc), acc_phase, abort_flag, p.status, 504)) { ok = false; break; }
         tc_fence_after();
         const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(acc * BN + half * 128);
-        uint32_t ra[16], rb[16];
-        tc_ld16(t, ra);
-#pragma unroll
-        for (int c = 0; c < 8; c += 2) {
-          tc_wait_ld();
-          tc_ld16(t + 16 * (c + 1), rb);
-          add_scaled<B_ROWS>(ra, s, reinterpret_cast<const float4*>(buf + 16 * c), sum + 16 * c);
-          tc_wait_ld();
-          if (c + 2 < 8) {
-            tc_ld16(t + 16 * (c + 2), ra);
-          } else {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(leader_addr(tempty_bar(acc)));
-          }
-          add_scaled<B_ROWS>(rb, s, reinterpret_cast<const float4*>(buf + 16 * (c + 1)), sum + 16 * (c + 1));
-        }
+        const uint64_t s2 = pack2(__float_as_uint(s), __float_as_uint(s));
+        const ulonglong2* b2 = reinterpret_cast<const ulonglong2*>(buf);
+        uint32_t ra[32], rb[32];
+        tc_ld32(t, ra);
+        tc_ld32(t + 32, rb);
+        tc_wait_ld();
+        add_scaled<B_ROWS>(ra, s2, b2, sum);
+        tc_ld32(t + 64, ra);
+        add_scaled<B_ROWS>(rb, s2, b2 + 8, sum + 16);
+        tc_ld32(t + 96, rb);
+        tc_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(leader_addr(tempty_bar(acc)));
+        add_scaled<B_ROWS>(ra, s2, b2 + 16, sum + 32);
+        add_scaled<B_ROWS>(rb, s2, b2 + 24, sum + 48);
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       if (ok) store_row(p, sum, row, col0);
