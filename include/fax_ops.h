@@ -167,8 +167,9 @@ fax_status fax_op_fp8_quantize(fax_ctx* ctx, int32_t prec, const fax_fp8_quantiz
  * to bf16, or kept as float (c_f32 != 0), or added to a float C (accumulate != 0).
  * The forward product takes activations and transposed weights (tile 128),
  * the input gradient output gradients and weights as stored, the weight gradient
- * both factors transposed with tile 1.  Any M, N, K; scales may be any finite
- * floats whose products are finite.  ldc >= N in elements; C aligned to its
+ * both factors transposed with tile 1.  Any M, N, K.  The scales are powers of
+ * two from 2^-126 to 2^127, as fax_op_fp8_quantize gives them (of any other
+ * float the exponent alone counts; infinities and NaN make NaN).  ldc >= N in elements; C aligned to its
  * elements (16-byte aligned rows are stored faster).  C may not overlap A or B. */
 typedef struct {
   int32_t M, N, K;

@@ -1,21 +1,28 @@
-// Product of two matrices in 8-bit floating point with a scale for each block of 128 along K:
+// Product of two matrices in 8-bit floating point with a power-of-two scale for each block of 128 along K:
 //
 //   C[m, n] = sum_b sa[b, m] sb[b, n] sum_{k in block b} A[m, k] B[n, k]   (+ bias[n])  (+ C[m, n])
 //
-// The tensor cores of two SMs work on one 256 x 256 tile (tcgen05.mma.cta_group::2, kind::f8f6f4).  A K
-// block is 128 bytes a row, exactly one 128-byte-swizzled operand tile and one block of scales, so the
-// pipeline runs block by block: TMA fills a stage, four MMAs (32 k each) multiply it into one of
-// two accumulators in tensor memory, and the row warps add the accumulator, times its two scales, into
-// float32 registers while the other one fills.  The scales differ from row to row and block to block,
-// so they cannot be applied after the sum over all of K.
+// The scales differ from row to row and block to block, so they cannot be applied after the sum over all of
+// K.  Applied to each block's accumulator by the row warps, they cost a hand-over of the accumulator per 128
+// k: two accumulators in flight leave 512 cycles for it and it takes about 770 (8192 x 16384 x 4096: 654 us).
+// Powers of two are the tensor core's own scale type (ue8m0, one byte): kind::mxf8f6f4 multiplies each
+// row's 32 k by the row's scale on the way in, the accumulator is handed over once a tile, and
+// a scale of 128 k is the same byte for four MMAs.
 //
-//   warp 0      : TMA producer (both CTAs; each loads its 128 rows of A and its half of B)
-//   warp 1      : tensor-memory allocation (both CTAs), MMA issue (even CTA)
-//   warps 2, 3  : none (they give their registers to the row warps)
-//   warps 4..11 : 128 rows x 256 columns of the CTA: warp w owns 32 rows and 128 columns, 128 sums a lane
+// Scales travel like this: float32 in global memory -> exponent bytes, four blocks of K in one word per row,
+// packed by warps 2..5 into shared memory -> tensor memory (tcgen05.cp, 32 x 128 bits, copied to the four
+// lane quarters) -> named by the MMA, which picks the byte of its block of K.
 //
-// Edges: TMA fills what lies outside a matrix with zeros, the scales of rows outside are taken as 0, and
-// the stores are limited to C.  Every wait is bounded.
+//   warp 0      : TMA producer
+//   warp 1      : tensor-memory allocation, scale copies and MMA issue (even CTA of a pair)
+//   warps 2..5  : scales; two teams of two warps take every other group of four K blocks
+//   warps 6..13 : epilogue; warp w reads lanes 32 (w % 4) .. and every other 32 columns
+//
+// CG = 2: a pair of SMs works on one 256 x BN tile (each CTA 128 rows of A and half of B's rows); CG = 1: one
+// SM on 128 x BN.  BN and the pipeline's depth are run-time parameters: the launcher picks them by size.
+//
+// Edges: TMA fills what lies outside a matrix with zeros (scales outside are 1), and the stores are
+// limited to C.  Every wait is bounded.
 #include "gemm_common.cuh"
 #include "../../include/fax_ops.h"
 
@@ -23,31 +30,30 @@ namespace {
 
 using namespace tc;
 
-constexpr int BM = 128;            // rows of A per CTA (256 per pair)
-constexpr int BN = 256;            // columns per pair; each CTA stages 128 of B's rows
-constexpr int BNH = 128;
+constexpr int BM = 128;            // rows of A per CTA
+constexpr int MAX_BN = 256;
 constexpr int BK = FAX_FP8_BLOCK;  // bytes = elements
-constexpr int NUM_EPI_WARPS = 8;
-constexpr int NUM_THREADS = 32 * (4 + NUM_EPI_WARPS);
-// 168 registers a thread at launch (65536 / 384); 128 x 40 + 256 x 232 = 384 x 168
-constexpr int REGS_LOAD = 40, REGS_ROWS = 232;
-static_assert(128 * REGS_LOAD + 256 * REGS_ROWS <= 384 * 168, "register split");
-constexpr int A_BYTES = BM * BK, B_BYTES = BNH * BK, STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int STAGES = 6;
-constexpr int TMEM_COLS = 512;
-constexpr int SCALE_BYTES = NUM_EPI_WARPS * 2 * 128 * 4;            // B's scales of a block, per warp, two blocks
-constexpr int BAR_BYTES = 256;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + SCALE_BYTES + 1024 + BAR_BYTES;
-static_assert(SMEM_BYTES <= 227 * 1024, "shared memory per CTA");
-static_assert(8 * (2 * STAGES + 4) + 8 <= BAR_BYTES, "barrier area");
+constexpr int GROUP = 4;           // K blocks per scale word
+constexpr int NUM_SCALE_WARPS = 4, NUM_EPI_WARPS = 8;
+constexpr int FIRST_EPI_WARP = 2 + NUM_SCALE_WARPS;
+constexpr int NUM_THREADS = 32 * (FIRST_EPI_WARP + NUM_EPI_WARPS);
+constexpr int TEAM = 64;           // threads of a scale team
+constexpr int MAX_STAGES = 12;
+constexpr int SC_SLOTS = 4;        // groups of scales in flight
+constexpr int SC_A_BYTES = 512, SC_B_BYTES = 1024, SC_BYTES = SC_A_BYTES + SC_B_BYTES;
+constexpr int BAR_BYTES = 512;
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr int TMEM_SCALE_COLS = 32;                  // two sets of 4 (A) + 8 (B) columns
+static_assert(8 * (2 * MAX_STAGES + 4 + 2 * SC_SLOTS) + 8 <= BAR_BYTES, "barrier area");
 
 struct Fp8Params {
   int M, N, K;
   uint32_t a_fmt, b_fmt;
   const float* sa; long long ldsa;
-  const float* sb; long long ldsb;
+  const float* sb; long long ldsb; int sb_shift;                    // 7: one scale per 128 rows of B
   void* C; long long ldc; int c_f32, accumulate, wide;              // wide: rows of C are 32-byte aligned
   const bf16* bias;
+  int bn, stages, tmem_cols, acc1, scale_col;                       // tile width, pipeline depth, tensor-memory columns
   int tiles_m, tiles_n, group_m, group_along_n;
   int32_t* status;
 };
@@ -67,277 +73,360 @@ __device__ __forceinline__ uint32_t leader_addr(uint32_t a) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0u));
   return r;
 }
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+  if (CG == 1)
+    tma_load_2d(dst, map, bar, c0, c1);
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrivals on a barrier of the even CTA.  Relaxed: what it orders (tensor-memory reads) has been completed;
+// release: what the warp has written to shared memory (and fenced for the asynchronous proxy) is seen first.
+template <int CG>
+__device__ __forceinline__ void arrive_leader_relaxed(uint32_t bar) {
+  if (CG == 1) mbar_arrive_relaxed(bar);
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-               ::"r"(bar), "h"((uint16_t)3) : "memory");
+template <int CG>
+__device__ __forceinline__ void arrive_leader(uint32_t bar) {
+  if (CG == 1) mbar_arrive(bar);
+  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void tc_mma_fp8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if (CG == 1)
+    tc_commit(bar);
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
-  uint32_t a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
-  lo = __uint_as_float(a); hi = __uint_as_float(b);
-}
-// Two float32 products or fused multiply-adds in one instruction.
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-// 32 columns of the accumulator, scaled, into the sums.  s: sa twice (times sb where a block of B has one scale).
-template <bool B_ROWS>
-__device__ __forceinline__ void add_scaled(const uint32_t (&r)[32], uint64_t s, const ulonglong2* sb, uint64_t* sum) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (B_ROWS) {
-      const ulonglong2 b = sb[j];
-      sum[2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), mul2(s, b.x), sum[2 * j]);
-      sum[2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), mul2(s, b.y), sum[2 * j + 1]);
-    } else {
-      sum[2 * j] = fma2(pack2(r[4 * j], r[4 * j + 1]), s, sum[2 * j]);
-      sum[2 * j + 1] = fma2(pack2(r[4 * j + 2], r[4 * j + 3]), s, sum[2 * j + 1]);
+// Bounded wait that also orders the other CTA's writes (acquire at cluster scope).
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int code) {
+  auto test = [&]() {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+  };
+  if (test()) return true;
+  const long long t0 = clock64();
+  int spins = 0;
+  while (!test()) {
+    if ((++spins & 255) == 0) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > WAIT_CYCLES) {
+        *abort_flag = 1;
+        if (atomicCAS(status, 0, 1) == 0) status[1] = code;
+        return false;
+      }
     }
   }
+  return true;
+}
+template <int CG>
+__device__ __forceinline__ void mma_scaled(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+  if (CG == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+// 128 scale words (32 rows of 16 bytes in shared memory) to four columns of tensor memory, in each lane quarter.
+template <int CG>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+  if (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// Descriptor of those 32 rows: no swizzle, groups of eight rows 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1 << 46);
 }
 
-// One lane's 128 sums of row `row`, columns col0 .. col0 + 127.
-__device__ __forceinline__ void store_row(const Fp8Params& p, const uint64_t (&sum)[64], long long row, int col0) {
-  float acc[128];
+// 32 sums of row `row` from column `col`.
+__device__ __forceinline__ void store_chunk(const Fp8Params& p, const uint32_t (&r)[32], long long row, int col) {
+  if (row >= p.M || col >= p.N) return;
+  if (p.wide && col + 32 <= p.N) {
+    float v[32];
 #pragma unroll
-  for (int j = 0; j < 64; ++j) unpack2(sum[j], acc[2 * j], acc[2 * j + 1]);
-  if (row >= p.M || col0 >= p.N) return;
-  if (p.wide && col0 + 128 <= p.N) {
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+    if (p.bias) {
 #pragma unroll
-    for (int c = 0; c < 128; c += 16) {
-      float v[16];
+      for (int j = 0; j < 32; ++j) v[j] += __bfloat162float(p.bias[col + j]);
+    }
+    if (p.c_f32) {
+      float* o = (float*)p.C + row * p.ldc + col;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = acc[c + j] + (p.bias ? __bfloat162float(p.bias[col0 + c + j]) : 0.f);
-      if (p.c_f32) {
-        float* o = (float*)p.C + row * p.ldc + col0 + c;
+      for (int j8 = 0; j8 < 4; ++j8) {
+        U8 u;
+        if (p.accumulate) {
+          const U8 old = ld_global_v8(o + 8 * j8);
 #pragma unroll
-        for (int j8 = 0; j8 < 2; ++j8) {
-          U8 u;
-          if (p.accumulate) {
-            const U8 old = ld_global_v8(o + 8 * j8);
+          for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e] + __uint_as_float(old.w[e]));
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e] + __uint_as_float(old.w[e]));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e]);
-          }
-          st_global_v8(o + 8 * j8, u);
+          for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e]);
         }
-      } else {
+        st_global_v8(o + 8 * j8, u);
+      }
+    } else {
+#pragma unroll
+      for (int j16 = 0; j16 < 2; ++j16) {
         U8 u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+          const __nv_bfloat162 h = __floats2bfloat162_rn(v[16 * j16 + 2 * e], v[16 * j16 + 2 * e + 1]);
           u.w[e] = *reinterpret_cast<const uint32_t*>(&h);
         }
-        st_global_v8((bf16*)p.C + row * p.ldc + col0 + c, u);
+        st_global_v8((bf16*)p.C + row * p.ldc + col + 16 * j16, u);
       }
     }
     return;
   }
 #pragma unroll
-  for (int c = 0; c < 128; ++c) {
-    if (col0 + c < p.N) {
-      const float v = acc[c] + (p.bias ? __bfloat162float(p.bias[col0 + c]) : 0.f);
+  for (int j = 0; j < 32; ++j) {
+    if (col + j < p.N) {
+      const float v = __uint_as_float(r[j]) + (p.bias ? __bfloat162float(p.bias[col + j]) : 0.f);
       if (p.c_f32) {
-        float* o = (float*)p.C + row * p.ldc + col0 + c;
+        float* o = (float*)p.C + row * p.ldc + col + j;
         *o = p.accumulate ? *o + v : v;
       } else {
-        ((bf16*)p.C)[row * p.ldc + col0 + c] = __float2bfloat16_rn(v);
+        ((bf16*)p.C)[row * p.ldc + col + j] = __float2bfloat16_rn(v);
       }
     }
   }
 }
 
-template <bool B_ROWS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
-fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ Fp8Params p) {
+template <int CG>
+__global__ void __launch_bounds__(NUM_THREADS, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ Fp8Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t tiles_base = (raw + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (tiles_base - raw);
-  float* scales = reinterpret_cast<float*>(gen_base + STAGES * STAGE_BYTES);
-  uint8_t* bar_mem = gen_base + STAGES * STAGE_BYTES + SCALE_BYTES;
-  const uint32_t bars = tiles_base + STAGES * STAGE_BYTES + SCALE_BYTES;
-  auto full_bar = [&](int s) { return bars + 8u * s; };                         // used in the even CTA
-  auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };             // one per CTA
-  auto tfull_bar = [&](int a) { return bars + 8u * (2 * STAGES + a); };         // one per CTA
-  auto tempty_bar = [&](int a) { return bars + 8u * (2 * STAGES + 2 + a); };    // used in the even CTA
-  volatile uint32_t* tmem_base_slot = (volatile uint32_t*)(bar_mem + 8 * (2 * STAGES + 4));
-  volatile int* abort_flag = (volatile int*)(bar_mem + 8 * (2 * STAGES + 4) + 4);
+  const uint32_t b_bytes = (uint32_t)(p.bn / CG) * BK, stage_bytes = BM * BK + b_bytes;
+  const int stages = p.stages;
+  const uint32_t sc_off = (uint32_t)stages * stage_bytes, bar_off = sc_off + SC_SLOTS * SC_BYTES;
+  const uint32_t bars = tiles_base + bar_off;
+  auto full_bar = [&](int s) { return bars + 8u * s; };                              // used in the even CTA
+  auto empty_bar = [&](int s) { return bars + 8u * (MAX_STAGES + s); };              // one per CTA
+  auto tfull_bar = [&](int a) { return bars + 8u * (2 * MAX_STAGES + a); };          // one per CTA
+  auto tempty_bar = [&](int a) { return bars + 8u * (2 * MAX_STAGES + 2 + a); };     // used in the even CTA
+  auto sfull_bar = [&](int s) { return bars + 8u * (2 * MAX_STAGES + 4 + s); };      // used in the even CTA
+  auto sempty_bar = [&](int s) { return bars + 8u * (2 * MAX_STAGES + 4 + SC_SLOTS + s); };   // one per CTA
+  volatile uint32_t* tmem_base_slot = (volatile uint32_t*)(gen_base + bar_off + 8 * (2 * MAX_STAGES + 4 + 2 * SC_SLOTS));
+  volatile int* abort_flag = (volatile int*)(tmem_base_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_ctarank();
+  const uint32_t rank = CG == 1 ? 0u : cluster_ctarank();
   const bool leader = (rank == 0);
-  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const int unit = blockIdx.x / CG, num_units = gridDim.x / CG;
   const int num_tiles = p.tiles_m * p.tiles_n;
   const int kb_total = (p.K + BK - 1) / BK;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * NUM_EPI_WARPS); }
+    for (int s = 0; s < stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), CG * NUM_EPI_WARPS); }
+    for (int s = 0; s < SC_SLOTS; ++s) { mbar_init(sfull_bar(s), CG * (TEAM / 32)); mbar_init(sempty_bar(s), 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32((const void*)tmem_base_slot)), "r"((uint32_t)TMEM_COLS) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    if (CG == 1) {
+      tmem_alloc(smem_u32((const void*)tmem_base_slot), (uint32_t)p.tmem_cols);
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                   ::"r"(smem_u32((const void*)tmem_base_slot)), "r"((uint32_t)p.tmem_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
   }
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();            // both CTAs' barriers exist before either signals the other
+  if (CG == 2) cluster_sync_all();   // both CTAs' barriers exist before either signals the other
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_slot;
-  fax_grid_dependency_wait();    // global memory only from here
+  fax_grid_dependency_wait();        // global memory only from here
 
-  if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LOAD));
   if (warp == 0) {
     // ---------------- TMA producer ----------------
     if (lane == 0) {
       int stage = 0; uint32_t phase = 0;
       bool ok = true;
-      for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+      for (int tile = unit; tile < num_tiles && ok; tile += num_units) {
         int tm, tn;
         tile_coords(tile, p.tiles_m, p.tiles_n, p.group_m, p.group_along_n, tm, tn);
-        const int m0 = tm * 2 * BM + (int)rank * BM, n0 = tn * BN + (int)rank * BNH;
+        const int m0 = tm * CG * BM + (int)rank * BM, n0 = tn * p.bn + (int)rank * (p.bn / CG);
         for (int kb = 0; kb < kb_total; ++kb) {
           if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.status, 501)) { ok = false; break; }
-          const uint32_t a_dst = tiles_base + stage * STAGE_BYTES;
-          const uint32_t fbar = leader_addr(full_bar(stage));
-          if (leader) mbar_expect_tx(full_bar(stage), 2 * STAGE_BYTES);       // both CTAs' bytes
-          tma_load_2d_pair(a_dst, &tmap_a, fbar, kb * BK, m0);
-          tma_load_2d_pair(a_dst + A_BYTES, &tmap_b, fbar, kb * BK, n0);
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          const uint32_t a_dst = tiles_base + (uint32_t)stage * stage_bytes;
+          const uint32_t fbar = CG == 1 ? full_bar(stage) : leader_addr(full_bar(stage));
+          if (leader) mbar_expect_tx(full_bar(stage), CG * stage_bytes);             // both CTAs' bytes
+          tma_load<CG>(a_dst, &tmap_a, fbar, kb * BK, m0);
+          tma_load<CG>(a_dst + BM * BK, &tmap_b, fbar, kb * BK, n0);
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
       }
       if (!ok) { const long long t0 = clock64(); while (clock64() - t0 < 2000000LL) { } }     // copies in flight land first
     }
   } else if (warp == 1) {
-    // ---------------- MMA issuer (even CTA of the pair) ----------------
+    // ---------------- scale copies and MMA issue (even CTA) ----------------
     if (leader && lane == 0) {
-      // D = f32, the two formats, both operands K-major, N = 256, M = 256 over the pair
-      const uint32_t idesc = (1u << 4) | (p.a_fmt << 7) | (p.b_fmt << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
+      // D = f32, the two formats, both K-major, N, ue8m0 scales, M over the unit; the scale bytes are named per block
+      const uint32_t idesc0 = (p.a_fmt << 7) | (p.b_fmt << 10) | ((uint32_t)(p.bn >> 3) << 17) | (1u << 23) | ((uint32_t)((CG * BM) >> 4) << 24);
+      const int b_copies = (p.bn + 127) / 128;
+      // operand descriptors: 128-byte swizzle, eight-row groups 1024 bytes apart; the low word holds the address
+      const uint32_t desc_lo0 = (uint32_t)smem_desc(tiles_base, 16u, 1024u), desc_hi = (uint32_t)(smem_desc(tiles_base, 16u, 1024u) >> 32);
+      auto desc_word = [&](uint32_t lo) { return ((uint64_t)desc_hi << 32) | lo; };
+      const bool overlap = p.acc1 < p.bn;      // the two accumulators share columns
       int stage = 0; uint32_t phase = 0;
-      int acc = 0; uint32_t acc_phase = 0;
+      int group = 0;                           // groups of four K blocks, over all tiles
+      int j = 0;                               // tiles of this unit
       bool ok = true;
-      for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
-        for (int kb = 0; kb < kb_total; ++kb) {
-          if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, p.status, 502)) { ok = false; break; }
-          if (!mbar_wait(full_bar(stage), phase, abort_flag, p.status, 503)) { ok = false; break; }
+      for (int tile = unit; tile < num_tiles && ok; tile += num_units, ++j) {
+        const int acc = j & 1;
+        // the accumulator of two tiles ago has been read; where they share columns, the previous tile's shared ones too
+        if (!overlap) { if (!mbar_wait(tempty_bar(acc), (uint32_t)((j >> 1) & 1) ^ 1u, abort_flag, p.status, 502)) { ok = false; break; } }
+        else if (j > 0) { if (!mbar_wait(tempty_bar(acc ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, p.status, 502)) { ok = false; break; } }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (acc ? (uint32_t)p.acc1 : 0u);
+        for (int kb0 = 0; kb0 < kb_total && ok; kb0 += GROUP, ++group) {
+          const int slot = group & (SC_SLOTS - 1);
+          // the MMAs of two groups ago have read the columns that these scales go to
+          if (group >= 2) {
+            const int old = group - 2;
+            if (!mbar_wait(sempty_bar(old & (SC_SLOTS - 1)), (uint32_t)(old / SC_SLOTS) & 1u, abort_flag, p.status, 507)) { ok = false; break; }
+          }
+          if (!mbar_wait_cluster(sfull_bar(slot), (uint32_t)(group / SC_SLOTS) & 1u, abort_flag, p.status, 505)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t a_src = tiles_base + stage * STAGE_BYTES, b_src = a_src + A_BYTES;
-          const uint32_t d_tmem = tmem_base + (uint32_t)(acc * BN);
+          const uint32_t sa_t = tmem_base + (uint32_t)p.scale_col + (uint32_t)(group & 1) * 16u, sb_t = sa_t + 8u;
+          const uint32_t src = tiles_base + sc_off + (uint32_t)slot * SC_BYTES;
+          copy_scales<CG>(sa_t, scale_desc(src));
+          for (int c = 0; c < b_copies; ++c) copy_scales<CG>(sb_t + 4u * c, scale_desc(src + SC_A_BYTES + 512u * c));
 #pragma unroll
-          for (int k = 0; k < BK / 32; ++k)
-            tc_mma_fp8_pair(d_tmem, smem_desc(a_src + 32u * k, 16u, 1024u), smem_desc(b_src + 32u * k, 16u, 1024u), idesc, k ? 1u : 0u);
-          tc_commit_pair(empty_bar(stage));      // frees this stage in both CTAs
-          tc_commit_pair(tfull_bar(acc));        // this block's accumulator is complete, both halves
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+          for (int b = 0; b < GROUP; ++b) {
+            if (kb0 + b >= kb_total) break;
+            if (!mbar_wait(full_bar(stage), phase, abort_flag, p.status, 503)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t idesc = idesc0 + (uint32_t)b * ((1u << 4) | (1u << 29));
+            const uint32_t a_lo = desc_lo0 + (uint32_t)stage * (stage_bytes >> 4), b_lo = a_lo + (BM * BK >> 4);
+#pragma unroll
+            for (int k = 0; k < BK / 32; ++k)                        // 32 k = two 16-byte units on
+              mma_scaled<CG>(d_tmem, desc_word(a_lo + 2u * k), desc_word(b_lo + 2u * k), idesc, sa_t, sb_t, (kb0 | b | k) ? 1u : 0u);
+            commit<CG>(empty_bar(stage));          // frees this stage (in both CTAs)
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+          }
+          commit<CG>(sempty_bar(slot));
         }
+        if (!ok) break;
+        commit<CG>(tfull_bar(acc));                // accumulator complete (both halves)
       }
     }
-  }
-  } else {
-    // ---------------- row warps ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS));
-    const int q = warp & 3, half = (warp - 4) >> 2;
-    float* my_scales = scales + (warp - 4) * 2 * 128;
-    int acc = 0; uint32_t acc_phase = 0;
+  } else if (warp < FIRST_EPI_WARP) {
+    // ---------------- scales ----------------
+    const int team = (warp - 2) >> 1, t = (threadIdx.x - 64) & (TEAM - 1);
+    const int rows_b = (p.bn + TEAM - 1) / TEAM;                     // of B per thread, 1 .. 4
+    const int groups_k = (kb_total + GROUP - 1) / GROUP;
+    int group = 0;
     bool ok = true;
-    for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+    for (int tile = unit; tile < num_tiles && ok; tile += num_units) {
       int tm, tn;
       tile_coords(tile, p.tiles_m, p.tiles_n, p.group_m, p.group_along_n, tm, tn);
-      const long long row = (long long)tm * 2 * BM + (int)rank * BM + 32 * q + lane;
-      const int col0 = tn * BN + half * 128;
-      const bool row_in = row < p.M;
-      auto load_sa = [&](int kb) { return row_in ? __ldg(p.sa + (long long)kb * p.ldsa + row) : 0.f; };
-      auto load_sb1 = [&](int kb) { return col0 < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + (col0 >> 7)) : 0.f; };
-      auto load_sb = [&](int kb, float (&b)[4]) {
+      const int m0 = tm * CG * BM + (int)rank * BM, n0 = tn * p.bn;
+      for (int g = 0; g < groups_k; ++g, ++group) {
+        if ((group & 1) != team) continue;
+        // exponent bytes of four K blocks; 127 (a scale of 1) outside the matrices.  Every load is issued, from a
+        // place inside, so that none waits for another
+        uint32_t wa[BM / TEAM], wb[MAX_BN / TEAM];
+        long long at[GROUP];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = col0 + 32 * j + lane < p.N ? __ldg(p.sb + (long long)kb * p.ldsb + col0 + 32 * j + lane) : 0.f;
-      };
-      uint64_t sum[64];
+        for (int b = 0; b < GROUP; ++b) at[b] = min(g * GROUP + b, kb_total - 1);
+        float fa[BM / TEAM][GROUP], fb[MAX_BN / TEAM][GROUP];
 #pragma unroll
-      for (int j = 0; j < 64; ++j) sum[j] = 0ull;
-      float sa_next = load_sa(0), sb_next = 0.f, sbv[4];
-      if (B_ROWS) load_sb(0, sbv); else sb_next = load_sb1(0);
-      for (int kb = 0; kb < kb_total; ++kb) {
-        const float s = B_ROWS ? sa_next : sa_next * sb_next;
-        float* buf = my_scales + (kb & 1) * 128;
-        if (B_ROWS) {
+        for (int i = 0; i < BM / TEAM; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) buf[32 * j + lane] = sbv[j];
-          __syncwarp();                          // the buffer of two blocks ago has been read by every lane before this one's turn
-        }
-        if (kb + 1 < kb_total) {
-          sa_next = load_sa(kb + 1);
-          if (B_ROWS) load_sb(kb + 1, sbv); else sb_next = load_sb1(kb + 1);
-        }
-        if (!mbar_wait_warp(tfull_bar(acc), acc_phase, abort_flag, p.status, 504)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(acc * BN + half * 128);
-        const uint64_t s2 = pack2(__float_as_uint(s), __float_as_uint(s));
-        const ulonglong2* b2 = reinterpret_cast<const ulonglong2*>(buf);
-        uint32_t ra[32], rb[32];
-        tc_ld32(t, ra);
-        tc_ld32(t + 32, rb);
-        tc_wait_ld();
-        add_scaled<B_ROWS>(ra, s2, b2, sum);
-        tc_ld32(t + 64, ra);
-        add_scaled<B_ROWS>(rb, s2, b2 + 8, sum + 16);
-        tc_ld32(t + 96, rb);
-        tc_wait_ld();
+          for (int b = 0; b < GROUP; ++b) fa[i][b] = __ldg(p.sa + at[b] * p.ldsa + min(m0 + t + TEAM * i, p.M - 1));
+#pragma unroll
+        for (int i = 0; i < MAX_BN / TEAM; ++i)
+          if (i < rows_b) {
+#pragma unroll
+            for (int b = 0; b < GROUP; ++b) fb[i][b] = __ldg(p.sb + at[b] * p.ldsb + (min(n0 + t + TEAM * i, p.N - 1) >> p.sb_shift));
+          }
+        auto word = [](const float (&f)[GROUP], bool in) {
+          uint32_t w = 0u;
+#pragma unroll
+          for (int b = 0; b < GROUP; ++b) w |= ((__float_as_uint(f[b]) >> 23) & 0xffu) << (8 * b);
+          return in ? w : 0x7f7f7f7fu;
+        };
+#pragma unroll
+        for (int i = 0; i < BM / TEAM; ++i) wa[i] = word(fa[i], m0 + t + TEAM * i < p.M);
+#pragma unroll
+        for (int i = 0; i < MAX_BN / TEAM; ++i) wb[i] = word(fb[i], n0 + t + TEAM * i < p.N);
+        const int slot = group & (SC_SLOTS - 1);
+        if (!mbar_wait(sempty_bar(slot), ((uint32_t)(group / SC_SLOTS) & 1u) ^ 1u, abort_flag, p.status, 506)) { ok = false; break; }
+        uint8_t* dst = gen_base + sc_off + slot * SC_BYTES;
+        auto place = [](int r) { return (r >> 7) * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4; };
+#pragma unroll
+        for (int i = 0; i < BM / TEAM; ++i) *reinterpret_cast<uint32_t*>(dst + place(t + TEAM * i)) = wa[i];
+#pragma unroll
+        for (int i = 0; i < MAX_BN / TEAM; ++i)
+          if (i < rows_b) *reinterpret_cast<uint32_t*>(dst + SC_A_BYTES + place(t + TEAM * i)) = wb[i];
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) arrive_leader<CG>(sfull_bar(slot));
+      }
+    }
+  } else {
+    // ---------------- epilogue: this CTA's 128 rows of the tile ----------------
+    const int q = warp & 3, half = (warp - FIRST_EPI_WARP) >> 2;
+    const bool overlap = p.acc1 < p.bn;
+    const int chunks = (p.bn / 32 - half + 1) / 2;                   // this warp's 32-column chunks: half, half + 2, ...
+    int j = 0;
+    for (int tile = unit; tile < num_tiles; tile += num_units, ++j) {
+      int tm, tn;
+      tile_coords(tile, p.tiles_m, p.tiles_n, p.group_m, p.group_along_n, tm, tn);
+      const long long row = (long long)tm * CG * BM + (int)rank * BM + 32 * q + lane;
+      const int n0 = tn * p.bn, acc = j & 1;
+      if (!mbar_wait_warp(tfull_bar(acc), (uint32_t)(j >> 1) & 1u, abort_flag, p.status, 504)) break;
+      tc_fence_after();
+      const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (acc ? (uint32_t)p.acc1 : 0u);
+      auto release = [&]() {
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(leader_addr(tempty_bar(acc)));
-        add_scaled<B_ROWS>(ra, s2, b2 + 16, sum + 32);
-        add_scaled<B_ROWS>(rb, s2, b2 + 24, sum + 48);
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        if (lane == 0) arrive_leader_relaxed<CG>(tempty_bar(acc));
+      };
+      if (chunks == 0) release();
+      // where the accumulators share columns (the first one's last chunk, the second one's first), those are read first
+      for (int i = 0; i < chunks; ++i) {
+        const int c = 32 * (half + 2 * (acc ? i : chunks - 1 - i));
+        uint32_t r[32];
+        tc_ld32(t + c, r);
+        tc_wait_ld();
+        if (i == (overlap ? 0 : chunks - 1)) release();
+        store_chunk(p, r, row, n0 + c);
       }
-      if (ok) store_row(p, sum, row, col0);
     }
   }
 
   tc_fence_before();
   __syncthreads();
-  cluster_sync_all();            // neither CTA leaves (or frees tensor memory) while the other may still signal it
+  if (CG == 2) cluster_sync_all();   // neither CTA leaves (or frees tensor memory) while the other may still signal it
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)TMEM_COLS) : "memory");
+    if (CG == 1) tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)p.tmem_cols) : "memory");
   }
 }
 
@@ -349,6 +438,28 @@ bool make_map_u8(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inne
   return ((EncodeTiledFn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, estr,
                                             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// fax_launch with a cluster of `cluster` CTAs.
+void launch_cluster(fax_ctx* ctx, void (*kernel)(CUtensorMap, CUtensorMap, Fp8Params), int grid, int cluster, int smem, const CUtensorMap& ma,
+                    const CUtensorMap& mb, const Fp8Params& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctx->use_pdl ? 2 : 1;
+  (void)cudaLaunchKernelEx(&cfg, kernel, ma, mb, p);                 // errors surface in fax_after_launch
+}
+
+struct TileChoice { int cg, bn; };
+TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K) {
+  (void)ctx; (void)K;
+  if (M > 128 && N > 128) return {2, 256};
+  return {1, N > 64 ? 64 : 32};
 }
 
 }  // namespace
@@ -367,26 +478,40 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
     return FAX_ERR_INVALID_ARG;
   if (d->lda >= (1LL << 40) || d->ldb >= (1LL << 40)) return FAX_ERR_UNSUPPORTED_SHAPE;        // the pitch a tensor map can hold
   if (d->M > 0x7fffff00 || d->N > 0x7fffff00 || d->K > 0x7fffff00) return FAX_ERR_UNSUPPORTED_SHAPE;
+  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K);
   CUtensorMap ma, mb;
-  if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, BNH)) return FAX_ERR_INVALID_ARG;
+  if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, (uint32_t)(t.bn / t.cg))) return FAX_ERR_INVALID_ARG;
   Fp8Params p;
   p.M = d->M; p.N = d->N; p.K = d->K;
   p.a_fmt = (uint32_t)d->a_format; p.b_fmt = (uint32_t)d->b_format;
-  p.sa = d->a_scale; p.ldsa = d->a_scale_ld; p.sb = d->b_scale; p.ldsb = d->b_scale_ld;
+  p.sa = d->a_scale; p.ldsa = d->a_scale_ld; p.sb = d->b_scale; p.ldsb = d->b_scale_ld; p.sb_shift = d->b_tile == 1 ? 0 : 7;
   p.C = d->C; p.ldc = d->ldc; p.c_f32 = d->c_f32 != 0; p.accumulate = d->accumulate != 0;
   p.wide = fax_aligned(d->C, 32) && ((size_t)d->ldc * es) % 32 == 0;
   p.bias = (const bf16*)d->bias;
-  p.tiles_m = (d->M + 2 * BM - 1) / (2 * BM); p.tiles_n = (d->N + BN - 1) / BN;
+  p.bn = t.bn;
+  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES;
+  p.stages = (SMEM_MAX - fixed) / stage_bytes;
+  if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
+  const int smem = p.stages * stage_bytes + fixed;
+  // two accumulators and the scales; at 256 columns the accumulators share the columns that the scales take
+  p.tmem_cols = 64;
+  while (p.tmem_cols < 2 * t.bn + TMEM_SCALE_COLS && p.tmem_cols < 512) p.tmem_cols *= 2;
+  p.scale_col = p.tmem_cols - TMEM_SCALE_COLS;
+  p.acc1 = t.bn < p.scale_col - t.bn ? t.bn : p.scale_col - t.bn;
+  p.tiles_m = (int)(((int64_t)d->M + t.cg * BM - 1) / (t.cg * BM)); p.tiles_n = (int)(((int64_t)d->N + t.bn - 1) / t.bn);
   p.group_m = 8; p.group_along_n = 0;
   p.status = ctx->dev_status;
   if ((long long)p.tiles_m * p.tiles_n > 0x7fff0000LL) return FAX_ERR_UNSUPPORTED_SHAPE;
   FaxProfScope prof(ctx, KC_FP8_GEMM, 2.0 * d->M * (double)d->N * d->K, 0.0);
+  const int tiles = p.tiles_m * p.tiles_n, max_units = ctx->sm_count / t.cg;
+  const int units = tiles < max_units ? tiles : max_units;
   static bool done[2][FAX_MAX_DEVICES] = {};
-  FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_pair_kernel<false>, SMEM_BYTES, done[0]));
-  FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_pair_kernel<true>, SMEM_BYTES, done[1]));
-  const int tiles = p.tiles_m * p.tiles_n, max_pairs = ctx->sm_count / 2;
-  const int pairs = tiles < max_pairs ? tiles : max_pairs;
-  if (d->b_tile == 1) fax_launch(ctx, fp8_gemm_pair_kernel<true>, dim3(2 * pairs), dim3(NUM_THREADS), SMEM_BYTES, ma, mb, p);
-  else fax_launch(ctx, fp8_gemm_pair_kernel<false>, dim3(2 * pairs), dim3(NUM_THREADS), SMEM_BYTES, ma, mb, p);
+  if (t.cg == 2) {
+    FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<2>, SMEM_MAX, done[1]));
+    launch_cluster(ctx, fp8_gemm_kernel<2>, 2 * units, 2, smem, ma, mb, p);
+  } else {
+    FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<1>, SMEM_MAX, done[0]));
+    fax_launch(ctx, fp8_gemm_kernel<1>, dim3(units), dim3(NUM_THREADS), smem, ma, mb, p);
+  }
   return fax_after_launch(ctx);
 }
