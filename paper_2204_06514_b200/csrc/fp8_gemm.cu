@@ -34,6 +34,13 @@ constexpr int BM = 128;            // rows of A per CTA
 constexpr int MAX_BN = 256;
 constexpr int BK = FAX_FP8_BLOCK;  // bytes = elements
 constexpr int GROUP = 4;           // K blocks per scale word
+// Float outputs: the tensor core cuts off what falls below its accumulator's last digit, a bias that grows with the
+// number of MMAs (2.4e-6 of the result's norm at K = 5000, where float32 sums are off by 4e-7), so the sums of
+// 1024 k are handed over and added in registers.  Three 32-column chunks a warp: tiles of 192 columns at most,
+// which also leaves two whole accumulators room.  A bf16 output is rounded far more coarsely: one sum over all of K.
+constexpr int SEGMENT = 8;         // K blocks
+constexpr int SUM_CHUNKS = 3, SUM_BN = 64 * SUM_CHUNKS;
+static_assert(SEGMENT % GROUP == 0, "scales are grouped by four blocks within a segment");
 constexpr int NUM_SCALE_WARPS = 4, NUM_EPI_WARPS = 8;
 constexpr int FIRST_EPI_WARP = 2 + NUM_SCALE_WARPS;
 constexpr int NUM_THREADS = 32 * (FIRST_EPI_WARP + NUM_EPI_WARPS);
@@ -208,7 +215,7 @@ __device__ __forceinline__ void store_chunk(const Fp8Params& p, const uint32_t (
   }
 }
 
-template <int CG>
+template <int CG, bool SUMS>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ Fp8Params p) {
   extern __shared__ uint8_t smem_raw[];
@@ -234,6 +241,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   const int unit = blockIdx.x / CG, num_units = gridDim.x / CG;
   const int num_tiles = p.tiles_m * p.tiles_n;
   const int kb_total = (p.K + BK - 1) / BK;
+  const int seg_len = SUMS ? SEGMENT : kb_total, segments = (kb_total + seg_len - 1) / seg_len;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -286,52 +294,63 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     if (leader && lane == 0) {
       // D = f32, the two formats, both K-major, N, ue8m0 scales, M over the unit; the scale bytes are named per block
       const uint32_t idesc0 = (p.a_fmt << 7) | (p.b_fmt << 10) | ((uint32_t)(p.bn >> 3) << 17) | (1u << 23) | ((uint32_t)((CG * BM) >> 4) << 24);
-      const int b_copies = (p.bn + 127) / 128;
       // operand descriptors: 128-byte swizzle, eight-row groups 1024 bytes apart; the low word holds the address
       const uint32_t desc_lo0 = (uint32_t)smem_desc(tiles_base, 16u, 1024u), desc_hi = (uint32_t)(smem_desc(tiles_base, 16u, 1024u) >> 32);
       auto desc_word = [&](uint32_t lo) { return ((uint64_t)desc_hi << 32) | lo; };
       const bool overlap = p.acc1 < p.bn;      // the two accumulators share columns
       int stage = 0; uint32_t phase = 0;
       int group = 0;                           // groups of four K blocks, over all tiles
-      int j = 0;                               // tiles of this unit
-      bool ok = true;
-      for (int tile = unit; tile < num_tiles && ok; tile += num_units, ++j) {
-        const int acc = j & 1;
-        // the accumulator of two tiles ago has been read; where they share columns, the previous tile's shared ones too
-        if (!overlap) { if (!mbar_wait(tempty_bar(acc), (uint32_t)((j >> 1) & 1) ^ 1u, abort_flag, p.status, 502)) { ok = false; break; } }
-        else if (j > 0) { if (!mbar_wait(tempty_bar(acc ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, p.status, 502)) { ok = false; break; } }
+      const int num_groups = unit < num_tiles ? ((num_tiles - unit + num_units - 1) / num_units) * ((kb_total + GROUP - 1) / GROUP) : 0;
+      auto scale_cols = [&](int g) { return tmem_base + (uint32_t)p.scale_col + (uint32_t)(g & 1) * 16u; };
+      // copies the scales of group g to tensor memory, once the MMAs of group g - 2 have read what they replace
+      auto scales_of = [&](int g) {
+        const int slot = g & (SC_SLOTS - 1), old = g - 2;
+        if (old >= 0 && !mbar_wait(sempty_bar(old & (SC_SLOTS - 1)), (uint32_t)(old / SC_SLOTS) & 1u, abort_flag, p.status, 507)) return false;
+        if (!mbar_wait_cluster(sfull_bar(slot), (uint32_t)(g / SC_SLOTS) & 1u, abort_flag, p.status, 505)) return false;
         tc_fence_after();
-        const uint32_t d_tmem = tmem_base + (acc ? (uint32_t)p.acc1 : 0u);
-        for (int kb0 = 0; kb0 < kb_total && ok; kb0 += GROUP, ++group) {
-          const int slot = group & (SC_SLOTS - 1);
-          // the MMAs of two groups ago have read the columns that these scales go to
-          if (group >= 2) {
-            const int old = group - 2;
-            if (!mbar_wait(sempty_bar(old & (SC_SLOTS - 1)), (uint32_t)(old / SC_SLOTS) & 1u, abort_flag, p.status, 507)) { ok = false; break; }
-          }
-          if (!mbar_wait_cluster(sfull_bar(slot), (uint32_t)(group / SC_SLOTS) & 1u, abort_flag, p.status, 505)) { ok = false; break; }
+        const uint32_t src = tiles_base + sc_off + (uint32_t)slot * SC_BYTES, t = scale_cols(g);
+        copy_scales<CG>(t, scale_desc(src));
+        copy_scales<CG>(t + 8u, scale_desc(src + SC_A_BYTES));
+        if (p.bn > 128) copy_scales<CG>(t + 12u, scale_desc(src + SC_A_BYTES + 512u));
+        return true;
+      };
+      bool ready = false;                      // the stage at hand has been seen full
+      int j = 0;                               // accumulators handed over
+      bool ok = true;
+      for (int tile = unit; tile < num_tiles && ok; tile += num_units) {
+        for (int seg = 0; seg < segments && ok; ++seg, ++j) {
+          const int acc = j & 1;
+          // the accumulator before the last has been read; where the two share columns, the last one's shared ones too
+          if (!overlap) { if (!mbar_wait(tempty_bar(acc), (uint32_t)((j >> 1) & 1) ^ 1u, abort_flag, p.status, 502)) { ok = false; break; } }
+          else if (j > 0) { if (!mbar_wait(tempty_bar(acc ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, p.status, 502)) { ok = false; break; } }
           tc_fence_after();
-          const uint32_t sa_t = tmem_base + (uint32_t)p.scale_col + (uint32_t)(group & 1) * 16u, sb_t = sa_t + 8u;
-          const uint32_t src = tiles_base + sc_off + (uint32_t)slot * SC_BYTES;
-          copy_scales<CG>(sa_t, scale_desc(src));
-          for (int c = 0; c < b_copies; ++c) copy_scales<CG>(sb_t + 4u * c, scale_desc(src + SC_A_BYTES + 512u * c));
+          const uint32_t d_tmem = tmem_base + (acc ? (uint32_t)p.acc1 : 0u);
+          const int first = seg * seg_len, end = min(kb_total, first + seg_len);
+          for (int kb0 = first; kb0 < end && ok; kb0 += GROUP, ++group) {
+            if (group == 0 && !scales_of(0)) { ok = false; break; }
+            const uint32_t sa_t = scale_cols(group), sb_t = sa_t + 8u;
 #pragma unroll
-          for (int b = 0; b < GROUP; ++b) {
-            if (kb0 + b >= kb_total) break;
-            if (!mbar_wait(full_bar(stage), phase, abort_flag, p.status, 503)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t idesc = idesc0 + (uint32_t)b * ((1u << 4) | (1u << 29));
-            const uint32_t a_lo = desc_lo0 + (uint32_t)stage * (stage_bytes >> 4), b_lo = a_lo + (BM * BK >> 4);
+            for (int b = 0; b < GROUP; ++b) {
+              if (kb0 + b >= end) break;
+              if (!ready && !mbar_wait(full_bar(stage), phase, abort_flag, p.status, 503)) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t idesc = idesc0 + (uint32_t)b * ((1u << 4) | (1u << 29));
+              const uint32_t a_lo = desc_lo0 + (uint32_t)stage * (stage_bytes >> 4), b_lo = a_lo + (BM * BK >> 4);
+              const uint32_t ebar = empty_bar(stage);
+              if (++stage == stages) { stage = 0; phase ^= 1u; }
+              ready = mbar_try_wait(full_bar(stage), phase);         // the next stage is looked at while this one is issued
 #pragma unroll
-            for (int k = 0; k < BK / 32; ++k)                        // 32 k = two 16-byte units on
-              mma_scaled<CG>(d_tmem, desc_word(a_lo + 2u * k), desc_word(b_lo + 2u * k), idesc, sa_t, sb_t, (kb0 | b | k) ? 1u : 0u);
-            commit<CG>(empty_bar(stage));          // frees this stage (in both CTAs)
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
+              for (int k = 0; k < BK / 32; ++k)                      // 32 k = two 16-byte units on
+                mma_scaled<CG>(d_tmem, desc_word(a_lo + 2u * k), desc_word(b_lo + 2u * k), idesc, sa_t, sb_t, ((kb0 - first) | b | k) ? 1u : 0u);
+              commit<CG>(ebar);                    // frees this stage (in both CTAs)
+              // the next group's scales, under the MMAs of this one
+              if (b == 0 && group + 1 < num_groups && !scales_of(group + 1)) { ok = false; break; }
+            }
+            commit<CG>(sempty_bar(group & (SC_SLOTS - 1)));
           }
-          commit<CG>(sempty_bar(slot));
+          if (!ok) break;
+          commit<CG>(tfull_bar(acc));              // accumulator complete (both halves)
         }
-        if (!ok) break;
-        commit<CG>(tfull_bar(acc));                // accumulator complete (both halves)
       }
     }
   } else if (warp < FIRST_EPI_WARP) {
@@ -394,28 +413,61 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     const bool overlap = p.acc1 < p.bn;
     const int chunks = (p.bn / 32 - half + 1) / 2;                   // this warp's 32-column chunks: half, half + 2, ...
     int j = 0;
-    for (int tile = unit; tile < num_tiles; tile += num_units, ++j) {
+    bool ok = true;
+    for (int tile = unit; tile < num_tiles && ok; tile += num_units) {
       int tm, tn;
       tile_coords(tile, p.tiles_m, p.tiles_n, p.group_m, p.group_along_n, tm, tn);
       const long long row = (long long)tm * CG * BM + (int)rank * BM + 32 * q + lane;
-      const int n0 = tn * p.bn, acc = j & 1;
-      if (!mbar_wait_warp(tfull_bar(acc), (uint32_t)(j >> 1) & 1u, abort_flag, p.status, 504)) break;
-      tc_fence_after();
-      const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (acc ? (uint32_t)p.acc1 : 0u);
-      auto release = [&]() {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_leader_relaxed<CG>(tempty_bar(acc));
-      };
-      if (chunks == 0) release();
-      // where the accumulators share columns (the first one's last chunk, the second one's first), those are read first
-      for (int i = 0; i < chunks; ++i) {
-        const int c = 32 * (half + 2 * (acc ? i : chunks - 1 - i));
-        uint32_t r[32];
-        tc_ld32(t + c, r);
-        tc_wait_ld();
-        if (i == (overlap ? 0 : chunks - 1)) release();
-        store_chunk(p, r, row, n0 + c);
+      const int n0 = tn * p.bn;
+      uint32_t sum[SUMS ? SUM_CHUNKS : 1][32];
+      if (SUMS) {
+#pragma unroll
+        for (int i = 0; i < SUM_CHUNKS; ++i)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[SUMS ? i : 0][e] = 0u;
+      }
+      for (int seg = 0; seg < segments; ++seg, ++j) {
+        const int acc = j & 1;
+        if (!mbar_wait_warp(tfull_bar(acc), (uint32_t)(j >> 1) & 1u, abort_flag, p.status, 504)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (acc ? (uint32_t)p.acc1 : 0u);
+        auto release = [&]() {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_leader_relaxed<CG>(tempty_bar(acc));
+        };
+        if (chunks == 0) release();
+        if (SUMS) {
+#pragma unroll
+          for (int i = 0; i < SUM_CHUNKS; ++i)
+            if (i < chunks) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t r[16];
+                tc_ld16(t + 32 * (half + 2 * i) + 16 * h, r);
+                tc_wait_ld();
+                if (h == 1 && i == chunks - 1) release();
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  sum[SUMS ? i : 0][16 * h + e] = __float_as_uint(__uint_as_float(sum[SUMS ? i : 0][16 * h + e]) + __uint_as_float(r[e]));
+              }
+            }
+        } else {
+          // where the accumulators share columns (the first one's last chunk, the second one's first), those are read first
+          for (int i = 0; i < chunks; ++i) {
+            const int c = 32 * (half + 2 * (acc ? i : chunks - 1 - i));
+            uint32_t r[32];
+            tc_ld32(t + c, r);
+            tc_wait_ld();
+            if (i == (overlap ? 0 : chunks - 1)) release();
+            store_chunk(p, r, row, n0 + c);
+          }
+        }
+      }
+      if (SUMS && ok) {
+#pragma unroll
+        for (int i = 0; i < SUM_CHUNKS; ++i)
+          if (i < chunks) store_chunk(p, sum[SUMS ? i : 0], row, n0 + 32 * (half + 2 * i));
       }
     }
   }
@@ -440,25 +492,31 @@ bool make_map_u8(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inne
                                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// fax_launch with a cluster of `cluster` CTAs.
-void launch_cluster(fax_ctx* ctx, void (*kernel)(CUtensorMap, CUtensorMap, Fp8Params), int grid, int cluster, int smem, const CUtensorMap& ma,
-                    const CUtensorMap& mb, const Fp8Params& p) {
+// fax_launch, with clusters of CG CTAs.
+template <int CG, bool SUMS>
+fax_status launch(fax_ctx* ctx, int units, int smem, const CUtensorMap& ma, const CUtensorMap& mb, const Fp8Params& p) {
+  static bool done[FAX_MAX_DEVICES] = {};
+  FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<CG, SUMS>, SMEM_MAX, done));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
+  cfg.gridDim = dim3(CG * units); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = CG; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ctx->use_pdl ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, ma, mb, p);                 // errors surface in fax_after_launch
+  (void)cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<CG, SUMS>, ma, mb, p);      // errors surface in fax_after_launch
+  return fax_after_launch(ctx);
 }
 
 struct TileChoice { int cg, bn; };
-TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K) {
+TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
   (void)ctx; (void)K;
-  if (M > 128 && N > 128) return {2, 256};
+#ifdef FORCE_CG
+  return {FORCE_CG, FORCE_BN};
+#endif
+  if (M > 128 && N > 128) return {2, sums ? SUM_BN : 256};
   return {1, N > 64 ? 64 : 32};
 }
 
@@ -478,7 +536,8 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
     return FAX_ERR_INVALID_ARG;
   if (d->lda >= (1LL << 40) || d->ldb >= (1LL << 40)) return FAX_ERR_UNSUPPORTED_SHAPE;        // the pitch a tensor map can hold
   if (d->M > 0x7fffff00 || d->N > 0x7fffff00 || d->K > 0x7fffff00) return FAX_ERR_UNSUPPORTED_SHAPE;
-  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K);
+  const bool sums = d->c_f32 && d->K > SEGMENT * BK;      // otherwise one segment holds all of K
+  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K, sums);
   CUtensorMap ma, mb;
   if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, (uint32_t)(t.bn / t.cg))) return FAX_ERR_INVALID_ARG;
   Fp8Params p;
@@ -505,13 +564,6 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   FaxProfScope prof(ctx, KC_FP8_GEMM, 2.0 * d->M * (double)d->N * d->K, 0.0);
   const int tiles = p.tiles_m * p.tiles_n, max_units = ctx->sm_count / t.cg;
   const int units = tiles < max_units ? tiles : max_units;
-  static bool done[2][FAX_MAX_DEVICES] = {};
-  if (t.cg == 2) {
-    FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<2>, SMEM_MAX, done[1]));
-    launch_cluster(ctx, fp8_gemm_kernel<2>, 2 * units, 2, smem, ma, mb, p);
-  } else {
-    FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<1>, SMEM_MAX, done[0]));
-    fax_launch(ctx, fp8_gemm_kernel<1>, dim3(units), dim3(NUM_THREADS), smem, ma, mb, p);
-  }
-  return fax_after_launch(ctx);
+  if (t.cg == 2) return sums ? launch<2, true>(ctx, units, smem, ma, mb, p) : launch<2, false>(ctx, units, smem, ma, mb, p);
+  return sums ? launch<1, true>(ctx, units, smem, ma, mb, p) : launch<1, false>(ctx, units, smem, ma, mb, p);
 }
