@@ -10,13 +10,14 @@
 // a scale of 128 k is the same byte for four MMAs.
 //
 // Scales travel like this: float32 in global memory -> exponent bytes, four blocks of K in one word per row,
-// packed by warps 2..5 into shared memory -> tensor memory (tcgen05.cp, 32 x 128 bits, copied to the four
+// packed by the scale warps into shared memory -> tensor memory (tcgen05.cp, 32 x 128 bits, copied to the four
 // lane quarters) -> named by the MMA, which picks the byte of its block of K.
 //
 //   warp 0      : TMA producer
 //   warp 1      : tensor-memory allocation, scale copies and MMA issue (even CTA of a pair)
-//   warps 2..5  : scales; two teams of two warps take every other group of four K blocks
-//   warps 6..13 : epilogue; warp w reads lanes 32 (w % 4) .. and every other 32 columns
+//   warps 2, 3  : scales of every other group of four K blocks; warps 12, 13: of the groups between
+//   warps 4..11 : epilogue; warp w reads lanes 32 (w % 4) .. and every other 32 columns
+//   warps 14, 15: none (registers are split by groups of four warps)
 //
 // CG = 2: a pair of SMs works on one 256 x BN tile (each CTA 128 rows of A and half of B's rows); CG = 1: one
 // SM on 128 x BN.  BN and the pipeline's depth are run-time parameters: the launcher picks them by size.
@@ -36,14 +37,16 @@ constexpr int BK = FAX_FP8_BLOCK;  // bytes = elements
 constexpr int GROUP = 4;           // K blocks per scale word
 // Float outputs: the tensor core cuts off what falls below its accumulator's last digit, a bias that grows with the
 // number of MMAs (2.4e-6 of the result's norm at K = 5000, where float32 sums are off by 4e-7), so the sums of
-// 1024 k are handed over and added in registers.  Three 32-column chunks a warp: tiles of 192 columns at most,
-// which also leaves two whole accumulators room.  A bf16 output is rounded far more coarsely: one sum over all of K.
-constexpr int SEGMENT = 8;         // K blocks
-constexpr int SUM_CHUNKS = 3, SUM_BN = 64 * SUM_CHUNKS;
+// 512 k are handed over and added in registers (128 sums a lane at 256 columns, for which the other warps
+// give up registers).  A bf16 output is rounded far more coarsely: one sum over all of K.
+constexpr int SEGMENT = 4;         // K blocks
+constexpr int SUM_CHUNKS = MAX_BN / 64;
 static_assert(SEGMENT % GROUP == 0, "scales are grouped by four blocks within a segment");
-constexpr int NUM_SCALE_WARPS = 4, NUM_EPI_WARPS = 8;
-constexpr int FIRST_EPI_WARP = 2 + NUM_SCALE_WARPS;
-constexpr int NUM_THREADS = 32 * (FIRST_EPI_WARP + NUM_EPI_WARPS);
+constexpr int NUM_EPI_WARPS = 8;
+constexpr int NUM_THREADS = 512;
+// 128 registers a thread at launch; 256 x 64 + 256 x 192 = 512 x 128
+constexpr int REGS_OTHER = 64, REGS_SUMS = 192;
+static_assert(256 * REGS_OTHER + 256 * REGS_SUMS <= NUM_THREADS * 128, "register split");
 constexpr int TEAM = 64;           // threads of a scale team
 constexpr int MAX_STAGES = 12;
 constexpr int SC_SLOTS = 4;        // groups of scales in flight
@@ -58,7 +61,8 @@ struct Fp8Params {
   uint32_t a_fmt, b_fmt;
   const float* sa; long long ldsa;
   const float* sb; long long ldsb; int sb_shift;                    // 7: one scale per 128 rows of B
-  void* C; long long ldc; int c_f32, accumulate, wide;              // wide: rows of C are 32-byte aligned
+  void* C; long long ldc; int c_f32, accumulate;
+  int wide, reduce, staged;                                         // C's rows are 32-byte aligned; added by bulk reductions; chunks may be staged
   const bf16* bias;
   int bn, stages, tmem_cols, acc1, scale_col;                       // tile width, pipeline depth, tensor-memory columns
   int tiles_m, tiles_n, group_m, group_along_n;
@@ -161,30 +165,62 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1 << 46);
 }
 
-// 32 sums of row `row` from column `col`.
-__device__ __forceinline__ void store_chunk(const Fp8Params& p, const uint32_t (&r)[32], long long row, int col) {
-  if (row >= p.M || col >= p.N) return;
+// A warp's 32 x 32 sums: row `row` (one a lane) from column `col`, to C.  Rows of C that are 32-byte aligned take
+// whole sectors from each lane; others go through shared memory (stg, 32 x 33 floats a warp), so that the lanes
+// write along a row (8000 x 200 x 2000, bf16: 29.8 us with a lane's row element by element, 12.0 us staged).
+// A product that is added to C is staged in the swizzled layout of the tensor map and added at L2 by a bulk reduction:
+// nothing waits for C (4096 x 1024 x 5120: REDUCE_US, with C read into the sums 35.4 us, without adding 30.0 us).
+constexpr int STG_BYTES = 5120;        // per warp: 32 x 33 floats, or the 4096 bytes of a swizzled box; a multiple of 1024
+__device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMap* mc, const uint32_t (&r)[32], long long row, int col, float* stg,
+                                            uint32_t stg_addr, int lane) {
+  if (col >= p.N) return;
+  const long long row0 = row - lane;
+  if (p.reduce) {
+    if (row0 >= p.M) return;
+    float bias = 0.f;
+    if (p.bias) bias = col + lane < p.N ? __bfloat162float(p.bias[col + lane]) : 0.f;
+    if (lane == 0) bulk_wait_read_all();                             // the previous chunk's reduction has read the buffer
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(r[4 * u + e]);
+      if (p.bias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __shfl_sync(0xffffffffu, bias, 4 * u + e);
+      }
+      st_shared_v4(stg_addr + epi_sw128(lane, u), __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      tma_reduce_add_2d(mc, stg_addr, col, (int)row0);
+      bulk_commit_group();
+    }
+    return;
+  }
   if (p.wide && col + 32 <= p.N) {
+    if (row >= p.M) return;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
     if (p.bias) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += __bfloat162float(p.bias[col + j]);
+      for (int j8 = 0; j8 < 4; ++j8) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.bias + col) + j8);
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(h[e]); v[8 * j8 + 2 * e] += f.x; v[8 * j8 + 2 * e + 1] += f.y; }
+      }
     }
     if (p.c_f32) {
       float* o = (float*)p.C + row * p.ldc + col;
 #pragma unroll
       for (int j8 = 0; j8 < 4; ++j8) {
         U8 u;
-        if (p.accumulate) {
-          const U8 old = ld_global_v8(o + 8 * j8);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e] + __uint_as_float(old.w[e]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e]);
-        }
+        for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e]);
         st_global_v8(o + 8 * j8, u);
       }
     } else {
@@ -201,30 +237,42 @@ __device__ __forceinline__ void store_chunk(const Fp8Params& p, const uint32_t (
     }
     return;
   }
+  __syncwarp();                                                      // the previous chunk has been read
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    if (col + j < p.N) {
-      const float v = __uint_as_float(r[j]) + (p.bias ? __bfloat162float(p.bias[col + j]) : 0.f);
-      if (p.c_f32) {
-        float* o = (float*)p.C + row * p.ldc + col + j;
-        *o = p.accumulate ? *o + v : v;
-      } else {
-        ((bf16*)p.C)[row * p.ldc + col + j] = __float2bfloat16_rn(v);
+  for (int j = 0; j < 32; ++j) stg[lane * 33 + j] = __uint_as_float(r[j]);
+  __syncwarp();
+  const int rows = (int)(p.M - row0 < 32 ? p.M - row0 : 32);
+  if (col + lane < p.N) {
+    const float bias = p.bias ? __bfloat162float(p.bias[col + lane]) : 0.f;
+    if (p.c_f32) {
+      float* o = (float*)p.C + row0 * p.ldc + col + lane;
+      for (int i0 = 0; i0 < rows; i0 += 8) {
+        float old[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) old[i] = p.accumulate && i0 + i < rows ? o[(i0 + i) * p.ldc] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i0 + i < rows) o[(i0 + i) * p.ldc] = old[i] + (stg[(i0 + i) * 33 + lane] + bias);
       }
+    } else {
+      bf16* o = (bf16*)p.C + row0 * p.ldc + col + lane;
+#pragma unroll 8
+      for (int i = 0; i < rows; ++i) o[i * p.ldc] = __float2bfloat16_rn(stg[i * 33 + lane] + bias);
     }
   }
 }
 
 template <int CG, bool SUMS>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
-fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ Fp8Params p) {
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_c,
+                const __grid_constant__ Fp8Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t tiles_base = (raw + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (tiles_base - raw);
   const uint32_t b_bytes = (uint32_t)(p.bn / CG) * BK, stage_bytes = BM * BK + b_bytes;
   const int stages = p.stages;
-  const uint32_t sc_off = (uint32_t)stages * stage_bytes, bar_off = sc_off + SC_SLOTS * SC_BYTES;
+  const uint32_t sc_off = (uint32_t)stages * stage_bytes, bar_off = sc_off + SC_SLOTS * SC_BYTES + (p.staged ? NUM_EPI_WARPS * STG_BYTES : 0);
   const uint32_t bars = tiles_base + bar_off;
   auto full_bar = [&](int s) { return bars + 8u * s; };                              // used in the even CTA
   auto empty_bar = [&](int s) { return bars + 8u * (MAX_STAGES + s); };              // one per CTA
@@ -251,6 +299,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
+    if (p.reduce) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_c) : "memory");
   }
   if (warp == 1) {
     if (CG == 1) {
@@ -268,6 +317,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   const uint32_t tmem_base = *tmem_base_slot;
   fax_grid_dependency_wait();        // global memory only from here
 
+  if (warp < 4 || warp >= 12) {
+  if (SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
   if (warp == 0) {
     // ---------------- TMA producer ----------------
     if (lane == 0) {
@@ -353,9 +404,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         }
       }
     }
-  } else if (warp < FIRST_EPI_WARP) {
+  } else if (warp < 14) {
     // ---------------- scales ----------------
-    const int team = (warp - 2) >> 1, t = (threadIdx.x - 64) & (TEAM - 1);
+    const int team = warp < 4 ? 0 : 1, t = threadIdx.x & (TEAM - 1);
     const int rows_b = (p.bn + TEAM - 1) / TEAM;                     // of B per thread, 1 .. 4
     const int groups_k = (kb_total + GROUP - 1) / GROUP;
     int group = 0;
@@ -407,9 +458,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         if (lane == 0) arrive_leader<CG>(sfull_bar(slot));
       }
     }
+  }
   } else {
     // ---------------- epilogue: this CTA's 128 rows of the tile ----------------
-    const int q = warp & 3, half = (warp - FIRST_EPI_WARP) >> 2;
+    if (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SUMS));
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t stg_off = sc_off + SC_SLOTS * SC_BYTES + (uint32_t)(p.staged ? (warp - 4) * STG_BYTES : 0);
+    float* stg = reinterpret_cast<float*>(gen_base + stg_off);
+    const uint32_t stg_addr = tiles_base + stg_off;
     const bool overlap = p.acc1 < p.bn;
     const int chunks = (p.bn / 32 - half + 1) / 2;                   // this warp's 32-column chunks: half, half + 2, ...
     int j = 0;
@@ -437,39 +493,47 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
           if (lane == 0) arrive_leader_relaxed<CG>(tempty_bar(acc));
         };
         if (chunks == 0) release();
+        // where the accumulators share columns (the first one's last chunk, the second one's first), those are read first
         if (SUMS) {
+          auto add = [&](int i, bool last) {
 #pragma unroll
-          for (int i = 0; i < SUM_CHUNKS; ++i)
-            if (i < chunks) {
+            for (int h = 0; h < 2; ++h) {
+              uint32_t r[16];
+              tc_ld16(t + 32 * (half + 2 * i) + 16 * h, r);
+              tc_wait_ld();
+              if (h == 1 && last) release();
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                uint32_t r[16];
-                tc_ld16(t + 32 * (half + 2 * i) + 16 * h, r);
-                tc_wait_ld();
-                if (h == 1 && i == chunks - 1) release();
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  sum[SUMS ? i : 0][16 * h + e] = __float_as_uint(__uint_as_float(sum[SUMS ? i : 0][16 * h + e]) + __uint_as_float(r[e]));
-              }
+              for (int e = 0; e < 16; ++e)
+                sum[SUMS ? i : 0][16 * h + e] = __float_as_uint(__uint_as_float(sum[SUMS ? i : 0][16 * h + e]) + __uint_as_float(r[e]));
             }
+          };
+          if (acc) {
+#pragma unroll
+            for (int i = 0; i < SUM_CHUNKS; ++i)
+              if (i < chunks) add(i, overlap ? i == 0 : i == chunks - 1);
+          } else {
+#pragma unroll
+            for (int i = SUM_CHUNKS - 1; i >= 0; --i)
+              if (i < chunks) add(i, overlap ? i == chunks - 1 : i == 0);
+          }
         } else {
-          // where the accumulators share columns (the first one's last chunk, the second one's first), those are read first
           for (int i = 0; i < chunks; ++i) {
             const int c = 32 * (half + 2 * (acc ? i : chunks - 1 - i));
             uint32_t r[32];
             tc_ld32(t + c, r);
             tc_wait_ld();
             if (i == (overlap ? 0 : chunks - 1)) release();
-            store_chunk(p, r, row, n0 + c);
+            store_chunk(p, &tmap_c, r, row, n0 + c, stg, stg_addr, lane);
           }
         }
       }
       if (SUMS && ok) {
 #pragma unroll
         for (int i = 0; i < SUM_CHUNKS; ++i)
-          if (i < chunks) store_chunk(p, sum[SUMS ? i : 0], row, n0 + 32 * (half + 2 * i));
+          if (i < chunks) store_chunk(p, &tmap_c, sum[SUMS ? i : 0], row, n0 + 32 * (half + 2 * i), stg, stg_addr, lane);
       }
     }
+    if (p.reduce && lane == 0) bulk_wait_all();                      // the additions are complete
   }
 
   tc_fence_before();
@@ -494,7 +558,7 @@ bool make_map_u8(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inne
 
 // fax_launch, with clusters of CG CTAs.
 template <int CG, bool SUMS>
-fax_status launch(fax_ctx* ctx, int units, int smem, const CUtensorMap& ma, const CUtensorMap& mb, const Fp8Params& p) {
+fax_status launch(fax_ctx* ctx, int units, int smem, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Fp8Params& p) {
   static bool done[FAX_MAX_DEVICES] = {};
   FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<CG, SUMS>, SMEM_MAX, done));
   cudaLaunchConfig_t cfg = {};
@@ -506,18 +570,29 @@ fax_status launch(fax_ctx* ctx, int units, int smem, const CUtensorMap& ma, cons
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ctx->use_pdl ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<CG, SUMS>, ma, mb, p);      // errors surface in fax_after_launch
+  (void)cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<CG, SUMS>, ma, mb, mc, p);  // errors surface in fax_after_launch
   return fax_after_launch(ctx);
 }
 
 struct TileChoice { int cg, bn; };
+// Time of a tile shape in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's end),
+// the paces as measured with all SMs busy.  A pair of SMs loads each operand byte for twice the work and runs best
+// where there are tiles for all pairs; a narrower tile has about the pace of the 128-column one (the issue of
+// its MMAs bounds it), so it pays only where it brings more SMs to work.
 TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
-  (void)ctx; (void)K;
-#ifdef FORCE_CG
-  return {FORCE_CG, FORCE_BN};
-#endif
-  if (M > 128 && N > 128) return {2, sums ? SUM_BN : 256};
-  return {1, N > 64 ? 64 : 32};
+  struct Shape { int cg, bn; double pace, end; };
+  static const Shape shapes[] = {{2, 256, 0.40, 1.5}, {2, 192, 0.33, 1.3}, {1, 256, 0.42, 1.2}, {1, 128, 0.31, 0.8}, {1, 64, 0.29, 0.6}};
+  const double kb = (K + BK - 1) / BK;
+  TileChoice best = {2, 256};
+  double least = 1e30;
+  for (const Shape& s : shapes) {
+    const double tiles = (double)((M + s.cg * BM - 1) / (s.cg * BM)) * ((N + s.bn - 1) / s.bn);
+    const double waves = (double)(long long)((tiles + ctx->sm_count / s.cg - 1) / (ctx->sm_count / s.cg));
+    const double pace = s.pace + (sums && s.bn == 256 ? 0.09 : 0.0);        // the accumulators share columns: a pause per segment
+    const double t = waves * (kb * pace + s.end) + (s.cg == 2 ? 0.5 : 0.0);
+    if (t < least) { least = t; best = {s.cg, s.bn}; }
+  }
+  return best;
 }
 
 }  // namespace
@@ -536,7 +611,7 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
     return FAX_ERR_INVALID_ARG;
   if (d->lda >= (1LL << 40) || d->ldb >= (1LL << 40)) return FAX_ERR_UNSUPPORTED_SHAPE;        // the pitch a tensor map can hold
   if (d->M > 0x7fffff00 || d->N > 0x7fffff00 || d->K > 0x7fffff00) return FAX_ERR_UNSUPPORTED_SHAPE;
-  const bool sums = d->c_f32 && d->K > SEGMENT * BK;      // otherwise one segment holds all of K
+  const bool sums = d->c_f32 && d->K > SEGMENT * BK;         // otherwise one segment holds all of K
   const TileChoice t = choose_tile(ctx, d->M, d->N, d->K, sums);
   CUtensorMap ma, mb;
   if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, (uint32_t)(t.bn / t.cg))) return FAX_ERR_INVALID_ARG;
@@ -545,10 +620,14 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   p.a_fmt = (uint32_t)d->a_format; p.b_fmt = (uint32_t)d->b_format;
   p.sa = d->a_scale; p.ldsa = d->a_scale_ld; p.sb = d->b_scale; p.ldsb = d->b_scale_ld; p.sb_shift = d->b_tile == 1 ? 0 : 7;
   p.C = d->C; p.ldc = d->ldc; p.c_f32 = d->c_f32 != 0; p.accumulate = d->accumulate != 0;
-  p.wide = fax_aligned(d->C, 32) && ((size_t)d->ldc * es) % 32 == 0;
+  p.reduce = p.accumulate && fax_aligned(d->C, 16) && d->ldc % 4 == 0 && d->ldc < (1LL << 36);
+  CUtensorMap mc = ma;                                               // read only by the reductions
+  if (p.reduce && !make_map_f32(ctx, &mc, d->C, d->N, d->M, d->ldc, 32, 32)) return FAX_ERR_INVALID_ARG;
+  p.wide = !p.accumulate && fax_aligned(d->C, 32) && ((size_t)d->ldc * es) % 32 == 0 && fax_aligned(d->bias, 16);
+  p.staged = !(p.wide && d->N % 32 == 0);
   p.bias = (const bf16*)d->bias;
   p.bn = t.bn;
-  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES;
+  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + (p.staged ? NUM_EPI_WARPS * STG_BYTES : 0);
   p.stages = (SMEM_MAX - fixed) / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   const int smem = p.stages * stage_bytes + fixed;
@@ -564,6 +643,6 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   FaxProfScope prof(ctx, KC_FP8_GEMM, 2.0 * d->M * (double)d->N * d->K, 0.0);
   const int tiles = p.tiles_m * p.tiles_n, max_units = ctx->sm_count / t.cg;
   const int units = tiles < max_units ? tiles : max_units;
-  if (t.cg == 2) return sums ? launch<2, true>(ctx, units, smem, ma, mb, p) : launch<2, false>(ctx, units, smem, ma, mb, p);
-  return sums ? launch<1, true>(ctx, units, smem, ma, mb, p) : launch<1, false>(ctx, units, smem, ma, mb, p);
+  if (t.cg == 2) return sums ? launch<2, true>(ctx, units, smem, ma, mb, mc, p) : launch<2, false>(ctx, units, smem, ma, mb, mc, p);
+  return sums ? launch<1, true>(ctx, units, smem, ma, mb, mc, p) : launch<1, false>(ctx, units, smem, ma, mb, mc, p);
 }
