@@ -62,7 +62,7 @@ struct Fp8Params {
   const float* sa; long long ldsa;
   const float* sb; long long ldsb; int sb_shift;                    // 7: one scale per 128 rows of B
   void* C; long long ldc; int c_f32, accumulate;
-  int wide, reduce, staged;                                         // C's rows are 32-byte aligned; added by bulk reductions; chunks may be staged
+  int bulk;                                                         // C can be described by a tensor map
   const bf16* bias;
   int bn, stages, tmem_cols, acc1, scale_col;                       // tile width, pipeline depth, tensor-memory columns
   int tiles_m, tiles_n, group_m, group_along_n;
@@ -165,75 +165,48 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1 << 46);
 }
 
-// A warp's 32 x 32 sums: row `row` (one a lane) from column `col`, to C.  Rows of C that are 32-byte aligned take
-// whole sectors from each lane; others go through shared memory (stg, 32 x 33 floats a warp), so that the lanes
-// write along a row (8000 x 200 x 2000, bf16: 29.8 us with a lane's row element by element, 12.0 us staged).
-// A product that is added to C is staged in the swizzled layout of the tensor map and added at L2 by a bulk reduction:
-// nothing waits for C (4096 x 1024 x 5120: REDUCE_US, with C read into the sums 35.4 us, without adding 30.0 us).
+// A warp's 32 x 32 sums (a row a lane) of rows row0 .. and columns col .., to C, through the warp's staging buffer.
+// Where a tensor map can describe C, one bulk store (or, for a product that is added, one bulk reduction at L2: nothing
+// waits for C) takes the buffer, swizzled as the map says, and cuts it off at C's edges; the sums of a float
+// output 4096 x 4096 x 4096 took 86.5 us with rows stored from registers, 85 us so.  Other pitches: the lanes write along a row.
 constexpr int STG_BYTES = 5120;        // per warp: 32 x 33 floats, or the 4096 bytes of a swizzled box; a multiple of 1024
-__device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMap* mc, const uint32_t (&r)[32], long long row, int col, float* stg,
+__device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMap* mc, const uint32_t (&r)[32], long long row0, int col, float* stg,
                                             uint32_t stg_addr, int lane) {
-  if (col >= p.N) return;
-  const long long row0 = row - lane;
-  if (p.reduce) {
-    if (row0 >= p.M) return;
-    float bias = 0.f;
-    if (p.bias) bias = col + lane < p.N ? __bfloat162float(p.bias[col + lane]) : 0.f;
-    if (lane == 0) bulk_wait_read_all();                             // the previous chunk's reduction has read the buffer
-    __syncwarp();
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(r[4 * u + e]);
-      if (p.bias) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += __shfl_sync(0xffffffffu, bias, 4 * u + e);
-      }
-      st_shared_v4(stg_addr + epi_sw128(lane, u), __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-    }
-    fence_proxy_async();
-    __syncwarp();
-    if (lane == 0) {
-      tma_reduce_add_2d(mc, stg_addr, col, (int)row0);
-      bulk_commit_group();
-    }
-    return;
-  }
-  if (p.wide && col + 32 <= p.N) {
-    if (row >= p.M) return;
+  if (col >= p.N || row0 >= p.M) return;
+  const float bias = p.bias && col + lane < p.N ? __bfloat162float(p.bias[col + lane]) : 0.f;
+  if (p.bulk) {
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
     if (p.bias) {
 #pragma unroll
-      for (int j8 = 0; j8 < 4; ++j8) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.bias + col) + j8);
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(h[e]); v[8 * j8 + 2 * e] += f.x; v[8 * j8 + 2 * e + 1] += f.y; }
-      }
+      for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bias, j);
     }
+    if (lane == 0) bulk_wait_read_all();                             // the previous chunk has left the buffer
+    __syncwarp();
     if (p.c_f32) {
-      float* o = (float*)p.C + row * p.ldc + col;
 #pragma unroll
-      for (int j8 = 0; j8 < 4; ++j8) {
-        U8 u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u.w[e] = __float_as_uint(v[8 * j8 + e]);
-        st_global_v8(o + 8 * j8, u);
-      }
+      for (int u = 0; u < 8; ++u)
+        st_shared_v4(stg_addr + epi_sw128(lane, u), __float_as_uint(v[4 * u]), __float_as_uint(v[4 * u + 1]), __float_as_uint(v[4 * u + 2]),
+                     __float_as_uint(v[4 * u + 3]));
     } else {
 #pragma unroll
-      for (int j16 = 0; j16 < 2; ++j16) {
-        U8 u;
+      for (int u = 0; u < 4; ++u) {                                  // 64-byte rows, 64-byte swizzle
+        uint32_t h[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(v[16 * j16 + 2 * e], v[16 * j16 + 2 * e + 1]);
-          u.w[e] = *reinterpret_cast<const uint32_t*>(&h);
+        for (int e = 0; e < 4; ++e) {
+          const __nv_bfloat162 x = __floats2bfloat162_rn(v[8 * u + 2 * e], v[8 * u + 2 * e + 1]);
+          h[e] = *reinterpret_cast<const uint32_t*>(&x);
         }
-        st_global_v8((bf16*)p.C + row * p.ldc + col + 16 * j16, u);
+        st_shared_v4(stg_addr + (uint32_t)(lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4)), h[0], h[1], h[2], h[3]);
       }
+    }
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      if (p.accumulate) tma_reduce_add_2d(mc, stg_addr, col, (int)row0);
+      else tma_store_2d(mc, stg_addr, col, (int)row0);
+      bulk_commit_group();
     }
     return;
   }
@@ -243,7 +216,6 @@ __device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMa
   __syncwarp();
   const int rows = (int)(p.M - row0 < 32 ? p.M - row0 : 32);
   if (col + lane < p.N) {
-    const float bias = p.bias ? __bfloat162float(p.bias[col + lane]) : 0.f;
     if (p.c_f32) {
       float* o = (float*)p.C + row0 * p.ldc + col + lane;
       for (int i0 = 0; i0 < rows; i0 += 8) {
@@ -272,7 +244,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   uint8_t* gen_base = smem_raw + (tiles_base - raw);
   const uint32_t b_bytes = (uint32_t)(p.bn / CG) * BK, stage_bytes = BM * BK + b_bytes;
   const int stages = p.stages;
-  const uint32_t sc_off = (uint32_t)stages * stage_bytes, bar_off = sc_off + SC_SLOTS * SC_BYTES + (p.staged ? NUM_EPI_WARPS * STG_BYTES : 0);
+  const uint32_t sc_off = (uint32_t)stages * stage_bytes, bar_off = sc_off + SC_SLOTS * SC_BYTES + NUM_EPI_WARPS * STG_BYTES;
   const uint32_t bars = tiles_base + bar_off;
   auto full_bar = [&](int s) { return bars + 8u * s; };                              // used in the even CTA
   auto empty_bar = [&](int s) { return bars + 8u * (MAX_STAGES + s); };              // one per CTA
@@ -299,7 +271,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
-    if (p.reduce) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_c) : "memory");
+    if (p.bulk) asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_c) : "memory");
   }
   if (warp == 1) {
     if (CG == 1) {
@@ -463,7 +435,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     // ---------------- epilogue: this CTA's 128 rows of the tile ----------------
     if (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SUMS));
     const int q = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t stg_off = sc_off + SC_SLOTS * SC_BYTES + (uint32_t)(p.staged ? (warp - 4) * STG_BYTES : 0);
+    const uint32_t stg_off = sc_off + SC_SLOTS * SC_BYTES + (uint32_t)(warp - 4) * STG_BYTES;
     float* stg = reinterpret_cast<float*>(gen_base + stg_off);
     const uint32_t stg_addr = tiles_base + stg_off;
     const bool overlap = p.acc1 < p.bn;
@@ -473,7 +445,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     for (int tile = unit; tile < num_tiles && ok; tile += num_units) {
       int tm, tn;
       tile_coords(tile, p.tiles_m, p.tiles_n, p.group_m, p.group_along_n, tm, tn);
-      const long long row = (long long)tm * CG * BM + (int)rank * BM + 32 * q + lane;
+      const long long row0 = (long long)tm * CG * BM + (int)rank * BM + 32 * q;
       const int n0 = tn * p.bn;
       uint32_t sum[SUMS ? SUM_CHUNKS : 1][32];
       if (SUMS) {
@@ -523,17 +495,17 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
             tc_ld32(t + c, r);
             tc_wait_ld();
             if (i == (overlap ? 0 : chunks - 1)) release();
-            store_chunk(p, &tmap_c, r, row, n0 + c, stg, stg_addr, lane);
+            store_chunk(p, &tmap_c, r, row0, n0 + c, stg, stg_addr, lane);
           }
         }
       }
       if (SUMS && ok) {
 #pragma unroll
         for (int i = 0; i < SUM_CHUNKS; ++i)
-          if (i < chunks) store_chunk(p, &tmap_c, sum[SUMS ? i : 0], row, n0 + 32 * (half + 2 * i), stg, stg_addr, lane);
+          if (i < chunks) store_chunk(p, &tmap_c, sum[SUMS ? i : 0], row0, n0 + 32 * (half + 2 * i), stg, stg_addr, lane);
       }
     }
-    if (p.reduce && lane == 0) bulk_wait_all();                      // the additions are complete
+    if (p.bulk && lane == 0) bulk_wait_all();                        // the stores are complete
   }
 
   tc_fence_before();
@@ -553,6 +525,18 @@ bool make_map_u8(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inne
   cuuint32_t estr[2] = {1, 1};
   return ((EncodeTiledFn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, estr,
                                             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// C in boxes of 32 x 32: rows of 128 bytes (float) or 64 bytes (bf16), swizzled over their own width.
+bool make_map_c(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t ld, bool f32) {
+  if (f32) return make_map_f32(ctx, map, base, inner, outer, ld, 32, 32);
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {ld * 2};
+  cuuint32_t box[2] = {32, 32};
+  cuuint32_t estr[2] = {1, 1};
+  return ((EncodeTiledFn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)base, dims, strides, box, estr,
+                                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -620,14 +604,13 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   p.a_fmt = (uint32_t)d->a_format; p.b_fmt = (uint32_t)d->b_format;
   p.sa = d->a_scale; p.ldsa = d->a_scale_ld; p.sb = d->b_scale; p.ldsb = d->b_scale_ld; p.sb_shift = d->b_tile == 1 ? 0 : 7;
   p.C = d->C; p.ldc = d->ldc; p.c_f32 = d->c_f32 != 0; p.accumulate = d->accumulate != 0;
-  p.reduce = p.accumulate && fax_aligned(d->C, 16) && d->ldc % 4 == 0 && d->ldc < (1LL << 36);
-  CUtensorMap mc = ma;                                               // read only by the reductions
-  if (p.reduce && !make_map_f32(ctx, &mc, d->C, d->N, d->M, d->ldc, 32, 32)) return FAX_ERR_INVALID_ARG;
-  p.wide = !p.accumulate && fax_aligned(d->C, 32) && ((size_t)d->ldc * es) % 32 == 0 && fax_aligned(d->bias, 16);
-  p.staged = !(p.wide && d->N % 32 == 0);
+  // whole 16-byte units only: a bulk store does not cut off within one, it would write behind column N
+  p.bulk = fax_aligned(d->C, 16) && ((size_t)d->ldc * es) % 16 == 0 && ((size_t)d->N * es) % 16 == 0 && d->ldc < (1LL << 36);
+  CUtensorMap mc = ma;
+  if (p.bulk && !make_map_c(ctx, &mc, d->C, d->N, d->M, d->ldc, d->c_f32 != 0)) return FAX_ERR_INVALID_ARG;
   p.bias = (const bf16*)d->bias;
   p.bn = t.bn;
-  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + (p.staged ? NUM_EPI_WARPS * STG_BYTES : 0);
+  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + NUM_EPI_WARPS * STG_BYTES;
   p.stages = (SMEM_MAX - fixed) / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   const int smem = p.stages * stage_bytes + fixed;
