@@ -185,16 +185,18 @@ fax_status fax_adamw_step(fax_ctx* ctx, const fax_adamw_tensor* tensors, int32_t
  * consecutive elements: the moment is scale * value.  m, v: n bytes; m_scale,
  * v_scale: ceil(n / FAX_ADAMW8_BLOCK) floats.  All four zero (or moments zero,
  * any finite scale) is the state before step 1.  Per element the moments are
- * widened, updated and used as fax_adamw_step writes it, every float32 operation
- * rounded on its own in the order
+ * widened, updated and used as fax_adamw_step writes it:
  *   m = b1*m + (1-b1)*g          v = b2*v + ((1-b2)*g)*g
  *   w = (w - (lr*wd)*w) - (lr*(m*c1)) / (sqrt(v*c2) + eps)
+ * Every float32 operation of m and v is rounded on its own in this order, so the
+ * stored moments are the same bits everywhere; quotient and root are the hardware's.
  * (c1 = 1/(1-b1^t), c2 = 1/(1-b2^t), taken in float64 and rounded), and stored
  * again: the scale is the smallest power of two, at least 2^-126, that brings the
  * largest finite moment of the block to the format's largest value at most (1 for
  * a block of zeros), and moment / scale is rounded stochastically: to the
  * neighbour above with the probability that makes the rounding right on average,
  * because a step of (1-b2) is too small to ever move the nearest 8-bit value.
+ * (That leaves a spread: for steady gradients about a third of v at b2 = 0.999.)
  * A v above 0 stays above 0; a moment that is not finite becomes NaN, its
  * neighbours keep theirs.  The 16 random bits of m and of v are the high and low
  * half of h(i ^ (h(seed + step * 0x9E3779B9) + (i >> 32) * 0x85EBCA77)) for

@@ -12,16 +12,20 @@
 // below): right on average.  A v above zero never becomes zero (its smallest value is kept instead):
 // m / (sqrt(0) + eps) would be a step out of all proportion.  Why e5m2 for v: it is a square, so it
 // needs twice the exponent range of m.  Why powers of two: m / s is then exact, the rounding is the
-// only loss, and the state after a step is one well-defined bit pattern (every float operation here is
-// rounded on its own, in the order written; no contraction).
+// only loss, and the moments after a step are one well-defined bit pattern (their float operations are each
+// rounded on its own, in the order written; no contraction).  The update of w uses the hardware's
+// reciprocal and square root (each within 2 units of the last place): its relative error is far below w's rounding.
 //
 // The rounding in integers: y 2^-120 (2^-112 for e5m2) puts the format's smallest normal value on
 // float32's, so that the float's bits, cut off after the format's mantissa, are the format's code,
 // subnormals included; adding 16 random bits below the cut carries into it with the right probability.
+// The largest moment is at most the format's largest value times the scale, which is where the cut falls, so
+// that the sum never carries past the last code.
 //
-// HBM-bound: 18 bytes per element (w 8, g 4, m 2, v 2, bf16 copy 2) against 30 with float32 moments.
-// A warp takes one block of 128 elements at a time, four elements a lane, so that a block's maximum
-// is one warp reduction (redux) and every access is a full 32-byte sector or more.
+// HBM-bound if the instructions are few: 18 bytes per element (w 8, g 4, m 2, v 2, bf16 copy 2) against 30 with
+// float32 moments.  A warp takes one block of 128 elements at a time, four elements a lane, so that a block's
+// maximum is one warp reduction (redux) and every access is a full 32-byte sector or more.  Moments that are
+// not finite are looked for once a block (their bits are the largest), not element by element.
 #include "common.cuh"
 
 #include <cuda_fp8.h>
@@ -54,29 +58,40 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-// Bits of |x| for the block's maximum; what is not finite does not count.
-__device__ __forceinline__ uint32_t finite_abs_bits(float x) {
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
 // Exponent field of the scale: the smallest power of two that brings the maximum to (1.75 2^TOP_EXP).
 template <int TOP_EXP>
 __device__ __forceinline__ int scale_field(uint32_t amax_bits) {
   const int f = (int)((amax_bits + 0x1fffffu) >> 23) - TOP_EXP;
   return amax_bits == 0u ? 127 : (f < 1 ? 1 : f);
 }
-// Stochastic rounding of |x| 2^(127 - field) to 8 bits.  BIAS_FIELD: exponent field of the factor that
-// lays the format's smallest normal value on float32's; CUT: mantissa bits dropped; TOP: largest code.
-template <int BIAS_FIELD, int CUT, uint32_t TOP, bool KEEP_ABOVE_ZERO>
-__device__ __forceinline__ uint32_t sr_code(float x, float inv, uint32_t r16) {
-  const float y = __fmul_rn(__fmul_rn(fabsf(x), inv), __uint_as_float((uint32_t)BIAS_FIELD << 23));
-  uint32_t c = (__float_as_uint(y) + (r16 << (CUT - 16)) + (1u << (CUT - 17))) >> CUT;
-  c = c < TOP ? c : TOP;
-  if (KEEP_ABOVE_ZERO) c = (c == 0u && x > 0.f) ? 1u : c;
-  if ((__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u) c = 0x7fu;      // not finite: NaN
-  return x < 0.f ? c | 0x80u : c;
+// Stochastic rounding of x 2^(127 - field): the codes are the top bytes of the words returned.
+// e4m3: sign, then bits 26 .. 20 of the float's magnitude; e5m2 (never negative): bits 28 .. 21.
+__device__ __forceinline__ uint32_t sr_e4m3(float x, float inv, uint32_t h) {
+  const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), __uint_as_float(7u << 23)));
+  const uint32_t t = y + ((h >> 12) & 0xffff0u) + 8u;
+  return (t & 0x80000000u) | ((t << 4) & 0x7f000000u);
 }
+__device__ __forceinline__ uint32_t sr_e5m2(float x, float inv, uint32_t h) {
+  const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), __uint_as_float(15u << 23)));
+  const uint32_t t = y + ((h & 0xffffu) << 5) + 16u;
+  return max(t, x > 0.f ? 1u << 21 : 0u) << 3;
+}
+__device__ __forceinline__ uint32_t top_bytes(const uint32_t (&c)[4]) {
+  return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
+}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
+__device__ __forceinline__ uint32_t max4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return max(__vimax3_u32(a, b, c), d); }
 
+__device__ __forceinline__ float sqrt_fast(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ void decode4(uint32_t q, __nv_fp8_interpretation_t fmt, float scale, float (&x)[4]) {
   const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q & 0xffffu), fmt)));
   const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16), fmt)));
@@ -139,28 +154,40 @@ adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
       float m[4], v[4];
       decode4(mq[u], __NV_E4M3, sm[u], m);
       decode4(vq[u], __NV_E5M2, sv[u], v);
-      uint32_t am = 0u, av = 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         m[j] = __fadd_rn(__fmul_rn(sc.b1, m[j]), __fmul_rn(omb1, g[u][j]));
         v[j] = __fadd_rn(__fmul_rn(sc.b2, v[j]), __fmul_rn(__fmul_rn(omb2, g[u][j]), g[u][j]));
-        const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[j], sc.inv_bc2)), sc.eps);
-        const float upd = __fdiv_rn(__fmul_rn(sc.lr, __fmul_rn(m[j], sc.inv_bc1)), den);
-        w[u][j] = __fsub_rn(__fsub_rn(w[u][j], __fmul_rn(lrwd, w[u][j])), upd);
-        am = max(am, finite_abs_bits(m[j]));
-        av = max(av, finite_abs_bits(v[j]));
+        const float den = sqrt_fast(v[j] * sc.inv_bc2) + sc.eps;
+        w[u][j] = (w[u][j] - lrwd * w[u][j]) - sc.lr * (m[j] * sc.inv_bc1) * rcp_fast(den);
       }
-      const int fm = scale_field<8>(__reduce_max_sync(0xffffffffu, am));
-      const int fv = scale_field<15>(__reduce_max_sync(0xffffffffu, av));
+      uint32_t am = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(m[0]) & 0x7fffffffu, __float_as_uint(m[1]) & 0x7fffffffu,
+                                                        __float_as_uint(m[2]) & 0x7fffffffu, __float_as_uint(m[3]) & 0x7fffffffu));
+      uint32_t av = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+      uint32_t bad_m = 0u, bad_v = 0u;                             // bytes that become NaN
+      if (max(am, av) >= 0x7f800000u) {                            // the whole warp: leave them out of the maxima
+        am = av = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (finite(m[j])) am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
+          else { bad_m |= (m[j] < 0.f ? 0xffu : 0x7fu) << (8 * j); m[j] = 0.f; }
+          if (finite(v[j])) av = max(av, __float_as_uint(v[j]));
+          else { bad_v |= 0x7fu << (8 * j); v[j] = 0.f; }
+        }
+        am = __reduce_max_sync(0xffffffffu, am);
+        av = __reduce_max_sync(0xffffffffu, av);
+      }
+      const int fm = scale_field<8>(am), fv = scale_field<15>(av);
       const float im = __uint_as_float((uint32_t)(254 - fm) << 23), iv = __uint_as_float((uint32_t)(254 - fv) << 23);
       const uint32_t key = t.key + (uint32_t)(e >> 32) * 0x85ebca77u;
-      uint32_t qm = 0u, qv = 0u;
+      uint32_t cm[4], cv[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t h = mix32((uint32_t)(e + j) ^ key);
-        qm |= sr_code<7, 20, 0x7eu, false>(m[j], im, h >> 16) << (8 * j);
-        qv |= sr_code<15, 21, 0x7bu, true>(v[j], iv, h & 0xffffu) << (8 * j);
+        cm[j] = sr_e4m3(m[j], im, h);
+        cv[j] = sr_e5m2(v[j], iv, h);
       }
+      const uint32_t qm = top_bytes(cm) | bad_m, qv = top_bytes(cv) | bad_v;
       if (e + 4 <= t.n) {
         *reinterpret_cast<float4*>(t.w + e) = make_float4(w[u][0], w[u][1], w[u][2], w[u][3]);
         *reinterpret_cast<uint32_t*>(t.m + e) = qm;

@@ -11,7 +11,11 @@
 // row, the weight gradient wants them along the tokens, i.e. blocks down a column, transposed).  A thread
 // block takes a 128 x 128 tile: 16 lanes hold a row's 128 elements, so that a row's maximum is four
 // shuffles and each row is written as 128 consecutive bytes; the tile is kept in shared memory and
-// read again down its columns for the transposed output.
+// read again down its columns, 32 rows of a word a thread, for the transposed output.
+//
+// What costs is instructions: maxima are taken on the raw words (two bf16 at a time), and elements that are not
+// finite are looked for once a tile (their bits are the largest); only a tile that holds one runs the code that
+// leaves them out of the maximum and makes them NaN.
 #include "common.cuh"
 #include "../../include/fax_ops.h"
 
@@ -28,83 +32,86 @@ struct QuantParams {
   uint8_t* q; long long ldq; float* s; long long lds;
   uint8_t* qt; long long ldqt; float* st; long long ldst;
   int square;                          // one scale for the whole tile
+  int wide_t;                          // rows of qt are 32-byte aligned
   int tiles_c;
 };
 
-__device__ __forceinline__ uint32_t finite_abs_bits(float x) {
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
-}
 template <int FMT> __device__ __forceinline__ uint32_t scale_field(uint32_t amax) {
   const int f = (int)((amax + 0x1fffffu) >> 23) - (FMT == FAX_FP8_E4M3 ? 8 : 15);
   return amax == 0u ? 127u : (f < 1 ? 1u : (uint32_t)f);
 }
 __device__ __forceinline__ float pow2_field(uint32_t f) { return __uint_as_float(f << 23); }
 
-// Two values already divided by their scale -> two codes.
-template <int FMT> __device__ __forceinline__ uint32_t code2(float a, float b) {
+// Two values already divided by their scale -> two codes.  The conversion saturates: where elements may not be
+// finite (BAD), infinities are made NaN before it.
+template <int FMT, bool BAD> __device__ __forceinline__ uint32_t code2(float a, float b) {
+  if (BAD) {
+    a = a - a == 0.f ? a : __uint_as_float(0x7fffffffu);
+    b = b - b == 0.f ? b : __uint_as_float(0x7fffffffu);
+  }
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, FMT == FAX_FP8_E4M3 ? __NV_E4M3 : __NV_E5M2);
 }
-// The conversion saturates: an infinite element is made NaN before it.
-__device__ __forceinline__ float inf_to_nan(float x) { return x - x == 0.f ? x : __uint_as_float(0x7fffffffu); }
+template <int FMT, bool BAD> __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
+  return code2<FMT, BAD>(a, b) | (code2<FMT, BAD>(c, d) << 16);
+}
 
-template <typename T> struct Row8;     // eight consecutive elements
-template <> struct Row8<bf16> {
-  static __device__ __forceinline__ void load(const bf16* p, float (&v)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { const float2 f = __bfloat1622float2(h[e]); v[2 * e] = f.x; v[2 * e + 1] = f.y; }
+// A 32-bit word of the matrix: two bf16 or one float.  Maxima are kept as words too (both halves of a bf16 word).
+template <typename T> struct Word;
+template <> struct Word<bf16> {
+  static constexpr int N = 2;
+  static constexpr uint32_t INF_BITS = 0x7f80u;
+  template <bool BAD> static __device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
+    w &= 0x7fff7fffu;
+    if (BAD) w = ((w & 0xffffu) < INF_BITS ? w & 0xffffu : 0u) | ((w >> 16) < INF_BITS ? w & 0xffff0000u : 0u);
+    return __vmaxu2(m, w);
   }
+  static __device__ __forceinline__ uint32_t join(uint32_t m) { return max(m & 0xffffu, m >> 16); }       // over both halves
+  static __device__ __forceinline__ uint32_t half(uint32_t m, int i) { return i ? m >> 16 : m & 0xffffu; }
+  static __device__ __forceinline__ uint32_t float_bits(uint32_t m) { return m << 16; }
+  static __device__ __forceinline__ float value(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
 };
-template <> struct Row8<float> {
-  static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+template <> struct Word<float> {
+  static constexpr int N = 1;
+  static constexpr uint32_t INF_BITS = 0x7f800000u;
+  template <bool BAD> static __device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
+    w &= 0x7fffffffu;
+    if (BAD) w = w < INF_BITS ? w : 0u;
+    return max(m, w);
   }
+  static __device__ __forceinline__ uint32_t join(uint32_t m) { return m; }
+  static __device__ __forceinline__ uint32_t half(uint32_t m, int) { return m; }
+  static __device__ __forceinline__ uint32_t float_bits(uint32_t m) { return m; }
+  static __device__ __forceinline__ float value(uint32_t w, int) { return __uint_as_float(w); }
 };
 
-// VEC: x is 16-byte aligned with a pitch of whole 16-byte vectors.  Outputs: pitches are multiples of 16.
-template <typename T, int FMT, bool VEC, bool STRAIGHT, bool TRANSPOSED>
-__global__ void __launch_bounds__(THREADS)
-fp8_quantize_kernel(const QuantParams p) {
-  extern __shared__ uint4 tile_raw[];              // TRANSPOSED: the tile [128][128] of T
-  T* tile = reinterpret_cast<T*>(tile_raw);
-  __shared__ uint32_t red[THREADS / 32];
-  __shared__ uint32_t col_max[TRANSPOSED ? 2 : 1][QT];
-  fax_grid_dependency_wait();
-  const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
+__device__ __forceinline__ void store32(uint8_t* dst, const uint32_t (&w)[8], bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                 "r"(w[6]), "r"(w[7]) : "memory");
+  } else {
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
+// Eight consecutive elements of a row are RW words; the tile has WPR words a row.
+template <typename T> constexpr int RW = 8 * (int)sizeof(T) / 4;
+template <typename T> constexpr int WPR = QT * (int)sizeof(T) / 4;
+
+template <typename T, int FMT, bool STRAIGHT, bool TRANSPOSED, bool BAD>
+__device__ __forceinline__ void quantize_tile(const QuantParams& p, const uint32_t (&v)[8][RW<T>], const uint32_t* tile, uint32_t* red,
+                                              uint32_t* col_max, int tr, int tc) {
+  typedef Word<T> W;
   const int r0 = tr * QT, c0 = tc * QT;
-  const int sub = threadIdx.x & 15, grp = threadIdx.x >> 4;          // 16 lanes a row, 16 rows at a time
-  const int c = c0 + 8 * sub;
-  float v[8][8];
+  const int sub = threadIdx.x & 15, grp = threadIdx.x >> 4;
   uint32_t am[8];
+  if (STRAIGHT || p.square) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = r0 + grp + 16 * i;
-    const T* src = (const T*)p.x + (size_t)r * p.ldx + c;
-    if (r < p.rows && VEC && c + 8 <= p.cols) {
-      Row8<T>::load(src, v[i]);
-    } else {
+    for (int i = 0; i < 8; ++i) {
+      uint32_t m = 0u;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = (r < p.rows && c + j < p.cols) ? to_f32(src[j]) : 0.f;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint32_t m = 0u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, finite_abs_bits(v[i][j]));
-    am[i] = m;
-    if (TRANSPOSED) {
-#pragma unroll
-      for (int j = 0; j < 8; j += 16 / (int)sizeof(T)) {
-        uint4 u;
-        T* e = reinterpret_cast<T*>(&u);
-#pragma unroll
-        for (int k = 0; k < 16 / (int)sizeof(T); ++k) e[k] = from_f32<T>(v[i][j + k]);
-        *reinterpret_cast<uint4*>(tile + (grp + 16 * i) * QT + 8 * sub + j) = u;
-      }
+      for (int j = 0; j < RW<T>; ++j) m = W::template max_abs<BAD>(m, v[i][j]);
+      am[i] = W::join(m);
     }
   }
   uint32_t all = 0u;                                                 // maximum of the whole tile
@@ -118,6 +125,7 @@ fp8_quantize_kernel(const QuantParams p) {
     for (int w = 0; w < THREADS / 32; ++w) all = max(all, red[w]);
   }
   if (STRAIGHT) {
+    const int c = c0 + 8 * sub;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int r = r0 + grp + 16 * i;
@@ -128,70 +136,129 @@ fp8_quantize_kernel(const QuantParams p) {
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
       }
-      const uint32_t f = scale_field<FMT>(m);
+      const uint32_t f = scale_field<FMT>(W::float_bits(m));
       const float inv = pow2_field(254u - f);
       if (r >= p.rows) continue;
       if (sub == 0 && !p.square) p.s[(size_t)tc * p.lds + r] = pow2_field(f);
-      uint2 o;
-      uint32_t h[4];
+      float y[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = code2<FMT>(inf_to_nan(v[i][2 * j]) * inv, inf_to_nan(v[i][2 * j + 1]) * inv);
-      o.x = h[0] | (h[1] << 16); o.y = h[2] | (h[3] << 16);
+      for (int j = 0; j < 8; ++j) y[j] = W::value(v[i][j / W::N], j % W::N) * inv;
+      const uint32_t lo = code4<FMT, BAD>(y[0], y[1], y[2], y[3]), hi = code4<FMT, BAD>(y[4], y[5], y[6], y[7]);
       uint8_t* dst = p.q + (size_t)r * p.ldq + c;
       if (c + 8 <= p.cols) {
-        *reinterpret_cast<uint2*>(dst) = o;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) dst[j] = (uint8_t)((j < 4 ? o.x : o.y) >> (8 * (j & 3)));
+          if (c + j < p.cols) dst[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
       }
     }
-    if (p.square && threadIdx.x == 0) p.s[(size_t)tc * p.lds + tr] = pow2_field(scale_field<FMT>(all));
+    if (p.square && threadIdx.x == 0) p.s[(size_t)tc * p.lds + tr] = pow2_field(scale_field<FMT>(W::float_bits(all)));
   }
   if (TRANSPOSED) {
-    __syncthreads();
-    // a thread takes one column and 16 consecutive rows of it at a time: 16 bytes of the transposed row
-    const int col = threadIdx.x & 127, part = threadIdx.x >> 7;      // part 0: row groups 0..3, part 1: 4..7
-    float x[4][16];
-    uint32_t cm = 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        x[k][j] = to_f32(tile[(16 * (4 * part + k) + j) * QT + col]);
-        cm = max(cm, finite_abs_bits(x[k][j]));
-      }
+    // a thread takes one word of each of 32 rows at a time: the columns in it, 32 bytes of their transposed rows
+    constexpr int GROUPS = THREADS / WPR<T>, ROWS = QT / GROUPS;
+    const int word = threadIdx.x % WPR<T>, group = threadIdx.x / WPR<T>;
+    const uint32_t* src = tile + (size_t)group * ROWS * WPR<T> + word;
+    uint32_t m = 0u;
     if (!p.square) {
-      col_max[part][col] = cm;
+#pragma unroll 32
+      for (int r = 0; r < ROWS; ++r) m = W::template max_abs<BAD>(m, src[r * WPR<T>]);
+      col_max[group * WPR<T> + word] = m;
       __syncthreads();
-      cm = max(col_max[0][col], col_max[1][col]);
-    } else {
-      cm = all;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) m = W::template max_abs<false>(m, col_max[g * WPR<T> + word]);
     }
-    const uint32_t f = scale_field<FMT>(cm);
-    const float inv = pow2_field(254u - f);
-    if (c0 + col < p.cols) {
-      if (part == 0 && !p.square) p.st[(size_t)tr * p.ldst + c0 + col] = pow2_field(f);
+    float inv[W::N];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = r0 + 16 * (4 * part + k);
-        uint32_t w[4];
+    for (int k = 0; k < W::N; ++k) {
+      const uint32_t f = scale_field<FMT>(W::float_bits(p.square ? all : W::half(m, k)));
+      const int c = c0 + word * W::N + k;
+      inv[k] = pow2_field(254u - f);
+      if (group == 0 && !p.square && c < p.cols) p.st[(size_t)tr * p.ldst + c] = pow2_field(f);
+    }
+#pragma unroll 1
+    for (int piece = 0; piece < ROWS / 32; ++piece) {
+      const int r = r0 + group * ROWS + piece * 32;
+      uint32_t w[32];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = code2<FMT>(inf_to_nan(x[k][4 * j]) * inv, inf_to_nan(x[k][4 * j + 1]) * inv) |
-                 (code2<FMT>(inf_to_nan(x[k][4 * j + 2]) * inv, inf_to_nan(x[k][4 * j + 3]) * inv) << 16);
-        uint8_t* dst = p.qt + (size_t)(c0 + col) * p.ldqt + r;
-        if (r + 16 <= p.rows) {
-          *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int j = 0; j < 32; ++j) w[j] = src[(piece * 32 + j) * WPR<T>];
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) {
+        const int c = c0 + word * W::N + k;
+        if (c >= p.cols) continue;
+        uint32_t o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          o[j] = code4<FMT, BAD>(W::value(w[4 * j], k) * inv[k], W::value(w[4 * j + 1], k) * inv[k], W::value(w[4 * j + 2], k) * inv[k],
+                                 W::value(w[4 * j + 3], k) * inv[k]);
+        uint8_t* dst = p.qt + (size_t)c * p.ldqt + r;
+        if (r + 32 <= p.rows) {
+          store32(dst, o, p.wide_t);
         } else {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (r + j < p.rows) dst[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+          for (int j = 0; j < 32; ++j)
+            if (r + j < p.rows) dst[j] = (uint8_t)(o[j >> 2] >> (8 * (j & 3)));
         }
       }
     }
-    if (p.square && threadIdx.x == 0) p.st[(size_t)tr * p.ldst + tc] = pow2_field(scale_field<FMT>(all));
+    if (p.square && threadIdx.x == 0) p.st[(size_t)tr * p.ldst + tc] = pow2_field(scale_field<FMT>(W::float_bits(all)));
   }
+}
+
+// VEC: x is 16-byte aligned with a pitch of whole 16-byte vectors.  Outputs: pitches are multiples of 16.
+template <typename T, int FMT, bool VEC, bool STRAIGHT, bool TRANSPOSED>
+__global__ void __launch_bounds__(THREADS)
+fp8_quantize_kernel(const QuantParams p) {
+  typedef Word<T> W;
+  extern __shared__ uint4 tile_raw[];              // TRANSPOSED: the tile [128][128] of T
+  __shared__ uint32_t red[THREADS / 32];
+  __shared__ uint32_t col_max[TRANSPOSED ? THREADS : 1];
+  fax_grid_dependency_wait();
+  const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
+  const int sub = threadIdx.x & 15, grp = threadIdx.x >> 4;          // 16 lanes a row, 16 rows at a time
+  const int c = tc * QT + 8 * sub;
+  uint32_t v[8][RW<T>];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = tr * QT + grp + 16 * i;
+    const T* src = (const T*)p.x + (size_t)r * p.ldx + c;
+    if (VEC && r < p.rows && c + 8 <= p.cols) {
+#pragma unroll
+      for (int j = 0; j < RW<T>; j += 4) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(src) + j / 4);
+        v[i][j] = u.x; v[i][j + 1] = u.y; v[i][j + 2] = u.z; v[i][j + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < RW<T>; ++j) {
+        uint32_t w = 0u;
+#pragma unroll
+        for (int k = 0; k < W::N; ++k)
+          if (r < p.rows && c + j * W::N + k < p.cols) {
+            if (W::N == 2) w |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[j * W::N + k] << (16 * k);
+            else w = reinterpret_cast<const uint32_t*>(src)[j];
+          }
+        v[i][j] = w;
+      }
+    }
+  }
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int j = 0; j < RW<T>; ++j) m = W::template max_abs<false>(m, v[i][j]);
+    if (TRANSPOSED) {
+#pragma unroll
+      for (int j = 0; j < RW<T>; j += 4)
+        tile_raw[((grp + 16 * i) * WPR<T> + sub * RW<T> + j) / 4] = make_uint4(v[i][j], v[i][j + 1], v[i][j + 2], v[i][j + 3]);
+    }
+  }
+  // also the barrier between writing the tile and reading it
+  const bool bad = __syncthreads_or(W::join(m) >= W::INF_BITS) != 0;
+  const uint32_t* tile = reinterpret_cast<const uint32_t*>(tile_raw);
+  if (!bad) quantize_tile<T, FMT, STRAIGHT, TRANSPOSED, false>(p, v, tile, red, col_max, tr, tc);
+  else quantize_tile<T, FMT, STRAIGHT, TRANSPOSED, true>(p, v, tile, red, col_max, tr, tc);
 }
 
 template <typename T, int FMT, bool VEC>
@@ -231,6 +298,7 @@ extern "C" fax_status fax_op_fp8_quantize(fax_ctx* ctx, int32_t prec, const fax_
   p.q = (uint8_t*)d->q; p.ldq = d->ldq; p.s = d->s; p.lds = d->lds;
   p.qt = (uint8_t*)d->qt; p.ldqt = d->ldqt; p.st = d->st; p.ldst = d->ldst;
   p.square = square ? 1 : 0;
+  p.wide_t = fax_aligned(d->qt, 32) && d->ldqt % 32 == 0;
   p.tiles_c = (int)cb;
   const size_t es = fax_elem_size(prec);
   FaxProfScope prof(ctx, KC_FP8_QUANT, 0.0, (double)d->rows * d->cols * (es + (d->q ? 1.0 : 0.0) + (d->qt ? 1.0 : 0.0)));
