@@ -52,7 +52,7 @@ struct Adam8Batch {
 };
 struct Adam8Scalars { float lr, b1, b2, eps, inv_bc1, inv_bc2; };
 
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+static inline uint32_t mix32(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x7feb352du;
   x = (x ^ (x >> 15)) * 0x846ca68bu;
   return x ^ (x >> 16);
@@ -64,17 +64,15 @@ __device__ __forceinline__ int scale_field(uint32_t amax_bits) {
   const int f = (int)((amax_bits + 0x1fffffu) >> 23) - TOP_EXP;
   return amax_bits == 0u ? 127 : (f < 1 ? 1 : f);
 }
-// Stochastic rounding of x 2^(127 - field): the codes are the top bytes of the words returned.
-// e4m3: sign, then bits 26 .. 20 of the float's magnitude; e5m2 (never negative): bits 28 .. 21.
-__device__ __forceinline__ uint32_t sr_e4m3(float x, float inv, uint32_t h) {
-  const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), __uint_as_float(7u << 23)));
-  const uint32_t t = y + ((h >> 12) & 0xffff0u) + 8u;
+// Stochastic rounding: y is the moment times 2^(127 - field) 2^-120 (2^-112 for e5m2); the codes are the top bytes
+// of the words returned.  e4m3: sign, then bits 26 .. 20 of the float's magnitude; e5m2 (never negative): bits 28 .. 21.
+__device__ __forceinline__ uint32_t sr_e4m3(float y, uint32_t h) {
+  const uint32_t t = __float_as_uint(y) + ((h >> 12) & 0xffff0u) + 8u;
   return (t & 0x80000000u) | ((t << 4) & 0x7f000000u);
 }
-__device__ __forceinline__ uint32_t sr_e5m2(float x, float inv, uint32_t h) {
-  const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(x, inv), __uint_as_float(15u << 23)));
-  const uint32_t t = y + ((h & 0xffffu) << 5) + 16u;
-  return max(t, x > 0.f ? 1u << 21 : 0u) << 3;
+__device__ __forceinline__ uint32_t sr_e5m2(float y, bool above_zero, uint32_t h) {
+  const uint32_t t = __float_as_uint(y) + ((h & 0xffffu) << 5) + 16u;
+  return max(t, above_zero ? 1u << 21 : 0u) << 3;
 }
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&c)[4]) {
   return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
@@ -82,14 +80,15 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&c)[4]) {
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
 __device__ __forceinline__ uint32_t max4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return max(__vimax3_u32(a, b, c), d); }
 
+// Square root and reciprocal of the hardware.  They take numbers below 2^-126 for zero: x is kept above (a NaN stays).
 __device__ __forceinline__ float sqrt_fast(float x) {
   float y;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0f00800000;\n\tsqrt.approx.ftz.f32 %0, t;\n\t}" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float rcp_fast(float x) {
   float y;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ void decode4(uint32_t q, __nv_fp8_interpretation_t fmt, float scale, float (&x)[4]) {
@@ -98,12 +97,144 @@ __device__ __forceinline__ void decode4(uint32_t q, __nv_fp8_interpretation_t fm
   x[0] = __fmul_rn(a.x, scale); x[1] = __fmul_rn(a.y, scale); x[2] = __fmul_rn(b.x, scale); x[3] = __fmul_rn(b.y, scale);
 }
 
+// One warp's UNROLL blocks of a chunk.  FULL: the chunk lies wholly inside its tensor.
+template <bool G_BF16, bool FULL>
+__device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8Scalars& sc, unsigned long long blk0, int lane) {
+  constexpr int WARPS = THREADS / 32, NEXT = WARPS * QB;           // blocks, elements from one of the warp's blocks to its next
+  const float omb1 = __fsub_rn(1.f, sc.b1), omb2 = __fsub_rn(1.f, sc.b2);
+  const float lrwd = sc.lr * t.wd, lrc1 = sc.lr * sc.inv_bc1;
+  const unsigned long long e0 = blk0 * QB + 4 * lane;
+  float* const wp = t.w + e0;
+  uint8_t* const mp = t.m + e0;
+  uint8_t* const vp = t.v + e0;
+  bf16* const cp = t.wc + e0;
+  float* const msp = t.ms + blk0;
+  float* const vsp = t.vs + blk0;
+  const float* const gp = (const float*)t.g + e0;
+  const bf16* const hp = (const bf16*)t.g + e0;
+  // elements of this lane's group that are inside (only the last block's group can be cut)
+  auto inside = [&](int u) { return FULL ? 4 : (e0 + u * NEXT >= t.n ? 0 : (t.n - (e0 + u * NEXT) < 4 ? (int)(t.n - (e0 + u * NEXT)) : 4)); };
+  auto block_in = [&](int u) { return FULL || (blk0 + u * WARPS) * QB < t.n; };
+
+  float w[UNROLL][4], g[UNROLL][4];
+  uint32_t mq[UNROLL], vq[UNROLL];
+  float sm[UNROLL], sv[UNROLL];
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    const int in = inside(u);
+    if (in == 4) {
+      const float4 f = *reinterpret_cast<const float4*>(wp + u * NEXT);
+      w[u][0] = f.x; w[u][1] = f.y; w[u][2] = f.z; w[u][3] = f.w;
+      if (G_BF16) {
+        const uint2 raw = *reinterpret_cast<const uint2*>(hp + u * NEXT);
+        g[u][0] = __uint_as_float(raw.x << 16); g[u][1] = __uint_as_float(raw.x & 0xffff0000u);
+        g[u][2] = __uint_as_float(raw.y << 16); g[u][3] = __uint_as_float(raw.y & 0xffff0000u);
+      } else {
+        const float4 h = *reinterpret_cast<const float4*>(gp + u * NEXT);
+        g[u][0] = h.x; g[u][1] = h.y; g[u][2] = h.z; g[u][3] = h.w;
+      }
+      mq[u] = *reinterpret_cast<const uint32_t*>(mp + u * NEXT);
+      vq[u] = *reinterpret_cast<const uint32_t*>(vp + u * NEXT);
+    } else {
+      mq[u] = vq[u] = 0u;                            // past the end: zeros, which leave the block's maximum alone
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[u][j] = j < in ? wp[u * NEXT + j] : 0.f;
+        g[u][j] = j < in ? (G_BF16 ? __bfloat162float(hp[u * NEXT + j]) : gp[u * NEXT + j]) : 0.f;
+        if (j < in) { mq[u] |= (uint32_t)mp[u * NEXT + j] << (8 * j); vq[u] |= (uint32_t)vp[u * NEXT + j] << (8 * j); }
+      }
+    }
+    sm[u] = block_in(u) ? msp[u * WARPS] : 0.f;
+    sv[u] = block_in(u) ? vsp[u * WARPS] : 0.f;
+  }
+#pragma unroll
+  for (int u = 0; u < UNROLL; ++u) {
+    if (!block_in(u)) continue;                      // the whole warp at once
+    float m[4], v[4];
+    decode4(mq[u], __NV_E4M3, sm[u], m);
+    decode4(vq[u], __NV_E5M2, sv[u], v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = __fadd_rn(__fmul_rn(sc.b1, m[j]), __fmul_rn(omb1, g[u][j]));
+      v[j] = __fadd_rn(__fmul_rn(sc.b2, v[j]), __fmul_rn(__fmul_rn(omb2, g[u][j]), g[u][j]));
+      const float den = sqrt_fast(v[j] * sc.inv_bc2) + sc.eps;
+      w[u][j] = fmaf(-lrwd, w[u][j], w[u][j]);
+      w[u][j] = fmaf(-(m[j] * lrc1), rcp_fast(den), w[u][j]);
+    }
+    uint32_t am = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(m[0]) & 0x7fffffffu, __float_as_uint(m[1]) & 0x7fffffffu,
+                                                      __float_as_uint(m[2]) & 0x7fffffffu, __float_as_uint(m[3]) & 0x7fffffffu));
+    uint32_t av = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+    uint32_t bad_m = 0u, bad_v = 0u;                 // bytes that become NaN
+    if (max(am, av) >= 0x7f800000u) {                // the whole warp: leave them out of the maxima
+      am = av = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (finite(m[j])) am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
+        else { bad_m |= (m[j] < 0.f ? 0xffu : 0x7fu) << (8 * j); m[j] = 0.f; }
+        if (finite(v[j])) av = max(av, __float_as_uint(v[j]));
+        else { bad_v |= 0x7fu << (8 * j); v[j] = 0.f; }
+      }
+      am = __reduce_max_sync(0xffffffffu, am);
+      av = __reduce_max_sync(0xffffffffu, av);
+    }
+    const int fm = scale_field<8>(am), fv = scale_field<15>(av);
+    // moment times 2^(127 - field), then 2^-120 or 2^-112: one factor unless it is below 2^-126 itself
+    float ym[4], yv[4];
+    if (fm <= 133 && fv <= 141) {
+      const float km = __uint_as_float((uint32_t)(134 - fm) << 23), kv = __uint_as_float((uint32_t)(142 - fv) << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { ym[j] = __fmul_rn(m[j], km); yv[j] = __fmul_rn(v[j], kv); }
+    } else {
+      const float im = __uint_as_float((uint32_t)(254 - fm) << 23), iv = __uint_as_float((uint32_t)(254 - fv) << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ym[j] = __fmul_rn(__fmul_rn(m[j], im), __uint_as_float(7u << 23));
+        yv[j] = __fmul_rn(__fmul_rn(v[j], iv), __uint_as_float(15u << 23));
+      }
+    }
+    // mix32 of (element index ^ key): the index ends in two bits j, which the first shift leaves alone
+    const unsigned long long e = e0 + u * NEXT;
+    uint32_t x0 = (uint32_t)e ^ (t.key + (uint32_t)(e >> 32) * 0x85ebca77u);
+    x0 ^= x0 >> 16;
+    uint32_t cm[4], cv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t h = (x0 ^ (uint32_t)j) * 0x7feb352du;
+      h = (h ^ (h >> 15)) * 0x846ca68bu;
+      h ^= h >> 16;
+      cm[j] = sr_e4m3(ym[j], h);
+      cv[j] = sr_e5m2(yv[j], v[j] > 0.f, h);
+    }
+    const uint32_t qm = top_bytes(cm) | bad_m, qv = top_bytes(cv) | bad_v;
+    const int in = inside(u);
+    if (in == 4) {
+      *reinterpret_cast<float4*>(wp + u * NEXT) = make_float4(w[u][0], w[u][1], w[u][2], w[u][3]);
+      *reinterpret_cast<uint32_t*>(mp + u * NEXT) = qm;
+      *reinterpret_cast<uint32_t*>(vp + u * NEXT) = qv;
+      if (t.wc) {
+        uint2 o;
+        *reinterpret_cast<__nv_bfloat162*>(&o.x) = __floats2bfloat162_rn(w[u][0], w[u][1]);
+        *reinterpret_cast<__nv_bfloat162*>(&o.y) = __floats2bfloat162_rn(w[u][2], w[u][3]);
+        *reinterpret_cast<uint2*>(cp + u * NEXT) = o;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < in) {
+          wp[u * NEXT + j] = w[u][j];
+          mp[u * NEXT + j] = (uint8_t)(qm >> (8 * j)); vp[u * NEXT + j] = (uint8_t)(qv >> (8 * j));
+          if (t.wc) cp[u * NEXT + j] = __float2bfloat16_rn(w[u][j]);
+        }
+    }
+    if (lane == 0) { msp[u * WARPS] = __uint_as_float((uint32_t)fm << 23); vsp[u * WARPS] = __uint_as_float((uint32_t)fv << 23); }
+  }
+}
+
 template <bool G_BF16>
 __global__ void __launch_bounds__(THREADS)
 adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
   fax_grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float omb1 = __fsub_rn(1.f, sc.b1), omb2 = __fsub_rn(1.f, sc.b2);
   for (unsigned int chunk = blockIdx.x; chunk < batch.total_chunks; chunk += gridDim.x) {
     int lo = 0, hi = batch.n_tensors - 1;
     while (lo < hi) {
@@ -111,104 +242,9 @@ adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
       if (batch.t[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
     }
     const Adam8Tensor& t = batch.t[lo];
-    const float lrwd = __fmul_rn(sc.lr, t.wd);
-    const unsigned long long blk0 = (unsigned long long)(chunk - t.first_chunk) * (CHUNK / QB) + warp;
-
-    float w[UNROLL][4], g[UNROLL][4];
-    uint32_t mq[UNROLL], vq[UNROLL];
-    float sm[UNROLL], sv[UNROLL];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const unsigned long long blk = blk0 + (unsigned long long)u * (THREADS / 32), e = blk * QB + 4 * lane;
-      if (e + 4 <= t.n) {
-        const float4 f = *reinterpret_cast<const float4*>(t.w + e);
-        w[u][0] = f.x; w[u][1] = f.y; w[u][2] = f.z; w[u][3] = f.w;
-        if (G_BF16) {
-          const uint2 raw = *reinterpret_cast<const uint2*>((const bf16*)t.g + e);
-          const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.x));
-          const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&raw.y));
-          g[u][0] = a.x; g[u][1] = a.y; g[u][2] = b.x; g[u][3] = b.y;
-        } else {
-          const float4 h = *reinterpret_cast<const float4*>((const float*)t.g + e);
-          g[u][0] = h.x; g[u][1] = h.y; g[u][2] = h.z; g[u][3] = h.w;
-        }
-        mq[u] = *reinterpret_cast<const uint32_t*>(t.m + e);
-        vq[u] = *reinterpret_cast<const uint32_t*>(t.v + e);
-      } else {
-        mq[u] = vq[u] = 0u;                          // past the end: zeros, which leave the block's maximum alone
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool in = e + j < t.n;
-          w[u][j] = in ? t.w[e + j] : 0.f;
-          g[u][j] = in ? (G_BF16 ? __bfloat162float(((const bf16*)t.g)[e + j]) : ((const float*)t.g)[e + j]) : 0.f;
-          if (in) { mq[u] |= (uint32_t)t.m[e + j] << (8 * j); vq[u] |= (uint32_t)t.v[e + j] << (8 * j); }
-        }
-      }
-      sm[u] = blk * QB < t.n ? t.ms[blk] : 0.f;
-      sv[u] = blk * QB < t.n ? t.vs[blk] : 0.f;
-    }
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const unsigned long long blk = blk0 + (unsigned long long)u * (THREADS / 32), e = blk * QB + 4 * lane;
-      if (blk * QB >= t.n) continue;                 // the whole warp at once
-      float m[4], v[4];
-      decode4(mq[u], __NV_E4M3, sm[u], m);
-      decode4(vq[u], __NV_E5M2, sv[u], v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        m[j] = __fadd_rn(__fmul_rn(sc.b1, m[j]), __fmul_rn(omb1, g[u][j]));
-        v[j] = __fadd_rn(__fmul_rn(sc.b2, v[j]), __fmul_rn(__fmul_rn(omb2, g[u][j]), g[u][j]));
-        const float den = sqrt_fast(v[j] * sc.inv_bc2) + sc.eps;
-        w[u][j] = (w[u][j] - lrwd * w[u][j]) - sc.lr * (m[j] * sc.inv_bc1) * rcp_fast(den);
-      }
-      uint32_t am = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(m[0]) & 0x7fffffffu, __float_as_uint(m[1]) & 0x7fffffffu,
-                                                        __float_as_uint(m[2]) & 0x7fffffffu, __float_as_uint(m[3]) & 0x7fffffffu));
-      uint32_t av = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-      uint32_t bad_m = 0u, bad_v = 0u;                             // bytes that become NaN
-      if (max(am, av) >= 0x7f800000u) {                            // the whole warp: leave them out of the maxima
-        am = av = 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (finite(m[j])) am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
-          else { bad_m |= (m[j] < 0.f ? 0xffu : 0x7fu) << (8 * j); m[j] = 0.f; }
-          if (finite(v[j])) av = max(av, __float_as_uint(v[j]));
-          else { bad_v |= 0x7fu << (8 * j); v[j] = 0.f; }
-        }
-        am = __reduce_max_sync(0xffffffffu, am);
-        av = __reduce_max_sync(0xffffffffu, av);
-      }
-      const int fm = scale_field<8>(am), fv = scale_field<15>(av);
-      const float im = __uint_as_float((uint32_t)(254 - fm) << 23), iv = __uint_as_float((uint32_t)(254 - fv) << 23);
-      const uint32_t key = t.key + (uint32_t)(e >> 32) * 0x85ebca77u;
-      uint32_t cm[4], cv[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t h = mix32((uint32_t)(e + j) ^ key);
-        cm[j] = sr_e4m3(m[j], im, h);
-        cv[j] = sr_e5m2(v[j], iv, h);
-      }
-      const uint32_t qm = top_bytes(cm) | bad_m, qv = top_bytes(cv) | bad_v;
-      if (e + 4 <= t.n) {
-        *reinterpret_cast<float4*>(t.w + e) = make_float4(w[u][0], w[u][1], w[u][2], w[u][3]);
-        *reinterpret_cast<uint32_t*>(t.m + e) = qm;
-        *reinterpret_cast<uint32_t*>(t.v + e) = qv;
-        if (t.wc) {
-          uint2 o;
-          *reinterpret_cast<__nv_bfloat162*>(&o.x) = __floats2bfloat162_rn(w[u][0], w[u][1]);
-          *reinterpret_cast<__nv_bfloat162*>(&o.y) = __floats2bfloat162_rn(w[u][2], w[u][3]);
-          *reinterpret_cast<uint2*>(t.wc + e) = o;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (e + j < t.n) {
-            t.w[e + j] = w[u][j];
-            t.m[e + j] = (uint8_t)(qm >> (8 * j)); t.v[e + j] = (uint8_t)(qv >> (8 * j));
-            if (t.wc) t.wc[e + j] = __float2bfloat16_rn(w[u][j]);
-          }
-      }
-      if (lane == 0) { t.ms[blk] = __uint_as_float((uint32_t)fm << 23); t.vs[blk] = __uint_as_float((uint32_t)fv << 23); }
-    }
+    const unsigned long long c = chunk - t.first_chunk;
+    if ((c + 1) * CHUNK <= t.n) update_blocks<G_BF16, true>(t, sc, c * (CHUNK / QB) + warp, lane);
+    else update_blocks<G_BF16, false>(t, sc, c * (CHUNK / QB) + warp, lane);
   }
 }
 

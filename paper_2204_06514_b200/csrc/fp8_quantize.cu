@@ -9,7 +9,7 @@
 //
 // HBM-bound: one reading of x serves both outputs (a forward product wants activations in blocks along a
 // row, the weight gradient wants them along the tokens, i.e. blocks down a column, transposed).  A thread
-// block takes a 128 x 128 tile: 16 lanes hold a row's 128 elements, so that a row's maximum is four
+// block takes a 128 x 128 tile: 8 lanes hold a row's 128 elements, so that a row's maximum is three
 // shuffles and each row is written as 128 consecutive bytes; the tile is kept in shared memory and
 // read again down its columns, 32 rows of a word a thread, for the transposed output.
 //
@@ -24,7 +24,8 @@
 namespace {
 
 constexpr int QT = FAX_FP8_BLOCK;      // tile edge
-constexpr int THREADS = 256;
+// Threads of a tile: each has 64 (bf16) or 32 (float) elements, 32 registers of them.
+template <typename T> constexpr int THREADS = 128 * (int)sizeof(T);
 
 struct QuantParams {
   int rows, cols;
@@ -42,17 +43,21 @@ template <int FMT> __device__ __forceinline__ uint32_t scale_field(uint32_t amax
 }
 __device__ __forceinline__ float pow2_field(uint32_t f) { return __uint_as_float(f << 23); }
 
-// Two values already divided by their scale -> two codes.  The conversion saturates: where elements may not be
+// Four values already divided by their scale -> four codes.  The conversion saturates: where elements may not be
 // finite (BAD), infinities are made NaN before it.
-template <int FMT, bool BAD> __device__ __forceinline__ uint32_t code2(float a, float b) {
-  if (BAD) {
-    a = a - a == 0.f ? a : __uint_as_float(0x7fffffffu);
-    b = b - b == 0.f ? b : __uint_as_float(0x7fffffffu);
-  }
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, FMT == FAX_FP8_E4M3 ? __NV_E4M3 : __NV_E5M2);
-}
 template <int FMT, bool BAD> __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d) {
-  return code2<FMT, BAD>(a, b) | (code2<FMT, BAD>(c, d) << 16);
+  if (BAD) {
+    const float nan = __uint_as_float(0x7fffffffu);
+    a = a - a == 0.f ? a : nan; b = b - b == 0.f ? b : nan; c = c - c == 0.f ? c : nan; d = d - d == 0.f ? d : nan;
+  }
+  uint32_t r;
+  if (FMT == FAX_FP8_E4M3)
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+  else
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e5m2x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
 }
 
 // A 32-bit word of the matrix: two bf16 or one float.  Maxima are kept as words too (both halves of a bf16 word).
@@ -61,12 +66,13 @@ template <> struct Word<bf16> {
   static constexpr int N = 2;
   static constexpr uint32_t INF_BITS = 0x7f80u;
   template <bool BAD> static __device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
-    w &= 0x7fff7fffu;
-    if (BAD) w = ((w & 0xffffu) < INF_BITS ? w & 0xffffu : 0u) | ((w >> 16) < INF_BITS ? w & 0xffff0000u : 0u);
-    return __vmaxu2(m, w);
+    if (BAD) w = ((w & 0x7fffu) < INF_BITS ? w & 0x7fffu : 0u) | (((w >> 16) & 0x7fffu) < INF_BITS ? w & 0x7fff0000u : 0u);
+    uint32_t d;                                    // the larger magnitudes, with signs that nobody reads; a NaN stays
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(w));
+    return d;
   }
-  static __device__ __forceinline__ uint32_t join(uint32_t m) { return max(m & 0xffffu, m >> 16); }       // over both halves
-  static __device__ __forceinline__ uint32_t half(uint32_t m, int i) { return i ? m >> 16 : m & 0xffffu; }
+  static __device__ __forceinline__ uint32_t join(uint32_t m) { return max(m & 0x7fffu, (m >> 16) & 0x7fffu); }       // over both halves
+  static __device__ __forceinline__ uint32_t half(uint32_t m, int i) { return (i ? m >> 16 : m) & 0x7fffu; }
   static __device__ __forceinline__ uint32_t float_bits(uint32_t m) { return m << 16; }
   static __device__ __forceinline__ float value(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
 };
@@ -94,136 +100,142 @@ __device__ __forceinline__ void store32(uint8_t* dst, const uint32_t (&w)[8], bo
   }
 }
 
-// Eight consecutive elements of a row are RW words; the tile has WPR words a row.
-template <typename T> constexpr int RW = 8 * (int)sizeof(T) / 4;
+// A lane holds 16 consecutive elements (RW words) of PASSES rows, ROW_STEP apart; the tile has WPR words a row.
+template <typename T> constexpr int PASSES = QT * QT / (THREADS<T> * 16);
+template <typename T> constexpr int ROW_STEP = THREADS<T> / 8;
+template <typename T> constexpr int RW = 16 * (int)sizeof(T) / 4;
 template <typename T> constexpr int WPR = QT * (int)sizeof(T) / 4;
 
-template <typename T, int FMT, bool STRAIGHT, bool TRANSPOSED, bool BAD>
-__device__ __forceinline__ void quantize_tile(const QuantParams& p, const uint32_t (&v)[8][RW<T>], const uint32_t* tile, uint32_t* red,
-                                              uint32_t* col_max, int tr, int tc) {
+// Place of a row's 16-byte unit in shared memory: eight lanes that write units 2 or 4 apart hit eight different bank groups,
+// and 32 lanes that read consecutive words still do.
+__device__ __forceinline__ int unit_at(int u) { return u ^ (u >> 3); }
+
+// The rows of the tile in v, quantised; am: their lanes' maxima (taken again where some are not finite).  Returns the
+// maximum of the whole tile (square blocks).
+template <typename T, int FMT, bool STRAIGHT, bool BAD>
+__device__ __forceinline__ uint32_t quantize_rows(const QuantParams& p, const uint32_t (&v)[PASSES<T>][RW<T>], uint32_t (&am)[PASSES<T>], uint32_t* red, int tr, int tc) {
   typedef Word<T> W;
-  const int r0 = tr * QT, c0 = tc * QT;
-  const int sub = threadIdx.x & 15, grp = threadIdx.x >> 4;
-  uint32_t am[8];
-  if (STRAIGHT || p.square) {
+  const int sub = threadIdx.x & 7;
+  if (BAD) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < PASSES<T>; ++i) {
       uint32_t m = 0u;
 #pragma unroll
-      for (int j = 0; j < RW<T>; ++j) m = W::template max_abs<BAD>(m, v[i][j]);
+      for (int j = 0; j < RW<T>; ++j) m = W::template max_abs<true>(m, v[i][j]);
       am[i] = W::join(m);
     }
   }
-  uint32_t all = 0u;                                                 // maximum of the whole tile
+  uint32_t all = 0u;
   if (p.square) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) all = max(all, am[i]);
+    for (int i = 0; i < PASSES<T>; ++i) all = max(all, am[i]);
     all = __reduce_max_sync(0xffffffffu, all);
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = all;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) all = max(all, red[w]);
+    for (int w = 0; w < THREADS<T> / 32; ++w) all = max(all, red[w]);
   }
   if (STRAIGHT) {
-    const int c = c0 + 8 * sub;
+    const int c = tc * QT + 16 * sub, r0 = tr * QT + (threadIdx.x >> 3);
+    uint8_t* dst = p.q + (size_t)r0 * p.ldq + c;
+    float* sc = p.s + (size_t)tc * p.lds + r0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = r0 + grp + 16 * i;
+    for (int i = 0; i < PASSES<T>; ++i, dst += ROW_STEP<T> * p.ldq) {
       uint32_t m = am[i];
       if (p.square) {
         m = all;
       } else {
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
       }
       const uint32_t f = scale_field<FMT>(W::float_bits(m));
       const float inv = pow2_field(254u - f);
-      if (r >= p.rows) continue;
-      if (sub == 0 && !p.square) p.s[(size_t)tc * p.lds + r] = pow2_field(f);
-      float y[8];
+      if (r0 + ROW_STEP<T> * i >= p.rows) continue;
+      if (sub == 0 && !p.square) sc[ROW_STEP<T> * i] = pow2_field(f);
+      uint32_t o[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = W::value(v[i][j / W::N], j % W::N) * inv;
-      const uint32_t lo = code4<FMT, BAD>(y[0], y[1], y[2], y[3]), hi = code4<FMT, BAD>(y[4], y[5], y[6], y[7]);
-      uint8_t* dst = p.q + (size_t)r * p.ldq + c;
-      if (c + 8 <= p.cols) {
-        *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+      for (int j = 0; j < 4; ++j) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = W::value(v[i][(4 * j + e) / W::N], e % W::N) * inv;
+        o[j] = code4<FMT, BAD>(y[0], y[1], y[2], y[3]);
+      }
+      if (c + 16 <= p.cols) {
+        *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < p.cols) dst[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+        for (int j = 0; j < 16; ++j)
+          if (c + j < p.cols) dst[j] = (uint8_t)(o[j >> 2] >> (8 * (j & 3)));
       }
     }
     if (p.square && threadIdx.x == 0) p.s[(size_t)tc * p.lds + tr] = pow2_field(scale_field<FMT>(W::float_bits(all)));
   }
-  if (TRANSPOSED) {
-    // a thread takes one word of each of 32 rows at a time: the columns in it, 32 bytes of their transposed rows
-    constexpr int GROUPS = THREADS / WPR<T>, ROWS = QT / GROUPS;
-    const int word = threadIdx.x % WPR<T>, group = threadIdx.x / WPR<T>;
-    const uint32_t* src = tile + (size_t)group * ROWS * WPR<T> + word;
-    uint32_t m = 0u;
-    if (!p.square) {
-#pragma unroll 32
-      for (int r = 0; r < ROWS; ++r) m = W::template max_abs<BAD>(m, src[r * WPR<T>]);
-      col_max[group * WPR<T> + word] = m;
-      __syncthreads();
+  return all;
+}
+
+// The columns of the tile in shared memory: a thread takes one word of each of 32 rows, and writes 32 bytes of the
+// transposed row of each column in it.
+template <typename T, int FMT, bool BAD>
+__device__ __forceinline__ void quantize_columns(const QuantParams& p, const uint32_t* tile, uint32_t* col_max, uint32_t all, int tr, int tc) {
+  typedef Word<T> W;
+  constexpr int GROUPS = QT / 32;
+  static_assert(THREADS<T> == GROUPS * WPR<T>, "a word of 32 rows a thread");
+  const int word = threadIdx.x % WPR<T>, group = threadIdx.x / WPR<T>;
+  uint32_t w[32];
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g) m = W::template max_abs<false>(m, col_max[g * WPR<T> + word]);
-    }
-    float inv[W::N];
+  for (int j = 0; j < 32; ++j) w[j] = tile[(group * 32 + j) * WPR<T> + 4 * unit_at(word >> 2) + (word & 3)];
+  uint32_t m = 0u;
+  if (!p.square) {
 #pragma unroll
-    for (int k = 0; k < W::N; ++k) {
-      const uint32_t f = scale_field<FMT>(W::float_bits(p.square ? all : W::half(m, k)));
-      const int c = c0 + word * W::N + k;
-      inv[k] = pow2_field(254u - f);
-      if (group == 0 && !p.square && c < p.cols) p.st[(size_t)tr * p.ldst + c] = pow2_field(f);
-    }
-#pragma unroll 1
-    for (int piece = 0; piece < ROWS / 32; ++piece) {
-      const int r = r0 + group * ROWS + piece * 32;
-      uint32_t w[32];
+    for (int j = 0; j < 32; ++j) m = W::template max_abs<BAD>(m, w[j]);
+    col_max[group * WPR<T> + word] = m;
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < 32; ++j) w[j] = src[(piece * 32 + j) * WPR<T>];
-#pragma unroll
-      for (int k = 0; k < W::N; ++k) {
-        const int c = c0 + word * W::N + k;
-        if (c >= p.cols) continue;
-        uint32_t o[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          o[j] = code4<FMT, BAD>(W::value(w[4 * j], k) * inv[k], W::value(w[4 * j + 1], k) * inv[k], W::value(w[4 * j + 2], k) * inv[k],
-                                 W::value(w[4 * j + 3], k) * inv[k]);
-        uint8_t* dst = p.qt + (size_t)c * p.ldqt + r;
-        if (r + 32 <= p.rows) {
-          store32(dst, o, p.wide_t);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (r + j < p.rows) dst[j] = (uint8_t)(o[j >> 2] >> (8 * (j & 3)));
-        }
-      }
-    }
-    if (p.square && threadIdx.x == 0) p.st[(size_t)tr * p.ldst + tc] = pow2_field(scale_field<FMT>(W::float_bits(all)));
+    for (int g = 0; g < GROUPS; ++g) m = W::template max_abs<false>(m, col_max[g * WPR<T> + word]);
   }
+  const int r = tr * QT + group * 32;
+#pragma unroll
+  for (int k = 0; k < W::N; ++k) {
+    const uint32_t f = scale_field<FMT>(W::float_bits(p.square ? all : W::half(m, k)));
+    const int c = tc * QT + word * W::N + k;
+    const float inv = pow2_field(254u - f);
+    if (c >= p.cols) break;
+    if (group == 0 && !p.square) p.st[(size_t)tr * p.ldst + c] = pow2_field(f);
+    uint32_t o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      o[j] = code4<FMT, BAD>(W::value(w[4 * j], k) * inv, W::value(w[4 * j + 1], k) * inv, W::value(w[4 * j + 2], k) * inv, W::value(w[4 * j + 3], k) * inv);
+    uint8_t* dst = p.qt + (size_t)c * p.ldqt + r;
+    if (r + 32 <= p.rows) {
+      store32(dst, o, p.wide_t);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (r + j < p.rows) dst[j] = (uint8_t)(o[j >> 2] >> (8 * (j & 3)));
+    }
+  }
+  if (p.square && threadIdx.x == 0) p.st[(size_t)tr * p.ldst + tc] = pow2_field(scale_field<FMT>(W::float_bits(all)));
 }
 
 // VEC: x is 16-byte aligned with a pitch of whole 16-byte vectors.  Outputs: pitches are multiples of 16.
+// Several blocks an SM: one's columns run under another's loads.
 template <typename T, int FMT, bool VEC, bool STRAIGHT, bool TRANSPOSED>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS<T>, sizeof(T) == 2 ? 4 : 2)
 fp8_quantize_kernel(const QuantParams p) {
   typedef Word<T> W;
   extern __shared__ uint4 tile_raw[];              // TRANSPOSED: the tile [128][128] of T
-  __shared__ uint32_t red[THREADS / 32];
-  __shared__ uint32_t col_max[TRANSPOSED ? THREADS : 1];
+  __shared__ uint32_t red[THREADS<T> / 32];
+  __shared__ uint32_t col_max[TRANSPOSED ? THREADS<T> : 1];
   fax_grid_dependency_wait();
   const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
-  const int sub = threadIdx.x & 15, grp = threadIdx.x >> 4;          // 16 lanes a row, 16 rows at a time
-  const int c = tc * QT + 8 * sub;
-  uint32_t v[8][RW<T>];
+  const int sub = threadIdx.x & 7, row = threadIdx.x >> 3;           // 8 lanes a row
+  const int c = tc * QT + 16 * sub, r0 = tr * QT + row;
+  uint32_t v[PASSES<T>][RW<T>];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = tr * QT + grp + 16 * i;
+  for (int i = 0; i < PASSES<T>; ++i) {
+    const int r = r0 + ROW_STEP<T> * i;
     const T* src = (const T*)p.x + (size_t)r * p.ldx + c;
-    if (VEC && r < p.rows && c + 8 <= p.cols) {
+    if (VEC && r < p.rows && c + 16 <= p.cols) {
 #pragma unroll
       for (int j = 0; j < RW<T>; j += 4) {
         const uint4 u = __ldg(reinterpret_cast<const uint4*>(src) + j / 4);
@@ -243,22 +255,30 @@ fp8_quantize_kernel(const QuantParams p) {
       }
     }
   }
-  uint32_t m = 0u;
+  uint32_t am[PASSES<T>], most = 0u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < PASSES<T>; ++i) {
+    uint32_t m = 0u;
 #pragma unroll
     for (int j = 0; j < RW<T>; ++j) m = W::template max_abs<false>(m, v[i][j]);
+    am[i] = W::join(m);
+    most = max(most, am[i]);
     if (TRANSPOSED) {
 #pragma unroll
       for (int j = 0; j < RW<T>; j += 4)
-        tile_raw[((grp + 16 * i) * WPR<T> + sub * RW<T> + j) / 4] = make_uint4(v[i][j], v[i][j + 1], v[i][j + 2], v[i][j + 3]);
+        tile_raw[(row + ROW_STEP<T> * i) * (WPR<T> / 4) + unit_at((sub * RW<T> + j) / 4)] = make_uint4(v[i][j], v[i][j + 1], v[i][j + 2], v[i][j + 3]);
     }
   }
-  // also the barrier between writing the tile and reading it
-  const bool bad = __syncthreads_or(W::join(m) >= W::INF_BITS) != 0;
-  const uint32_t* tile = reinterpret_cast<const uint32_t*>(tile_raw);
-  if (!bad) quantize_tile<T, FMT, STRAIGHT, TRANSPOSED, false>(p, v, tile, red, col_max, tr, tc);
-  else quantize_tile<T, FMT, STRAIGHT, TRANSPOSED, true>(p, v, tile, red, col_max, tr, tc);
+  // with a transposed output also the barrier between writing the tile and reading it
+  const bool bad = (TRANSPOSED || p.square ? __syncthreads_or(most >= W::INF_BITS) : __any_sync(0xffffffffu, most >= W::INF_BITS)) != 0;
+  uint32_t all = 0u;
+  if (STRAIGHT || p.square)
+    all = bad ? quantize_rows<T, FMT, STRAIGHT, true>(p, v, am, red, tr, tc) : quantize_rows<T, FMT, STRAIGHT, false>(p, v, am, red, tr, tc);
+  if (TRANSPOSED) {
+    const uint32_t* tile = reinterpret_cast<const uint32_t*>(tile_raw);
+    if (bad) quantize_columns<T, FMT, true>(p, tile, col_max, all, tr, tc);
+    else quantize_columns<T, FMT, false>(p, tile, col_max, all, tr, tc);
+  }
 }
 
 template <typename T, int FMT, bool VEC>
@@ -267,13 +287,13 @@ fax_status launch(fax_ctx* ctx, const QuantParams& p, unsigned int blocks) {
   if (p.q && p.qt) {
     static bool done[FAX_MAX_DEVICES] = {};
     FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_quantize_kernel<T, FMT, VEC, true, true>, tile_bytes, done));
-    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, true, true>, dim3(blocks), dim3(THREADS), tile_bytes, p);
+    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, true, true>, dim3(blocks), dim3(THREADS<T>), tile_bytes, p);
   } else if (p.q) {
-    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, true, false>, dim3(blocks), dim3(THREADS), 0, p);
+    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, true, false>, dim3(blocks), dim3(THREADS<T>), 0, p);
   } else {
     static bool done[FAX_MAX_DEVICES] = {};
     FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_quantize_kernel<T, FMT, VEC, false, true>, tile_bytes, done));
-    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, false, true>, dim3(blocks), dim3(THREADS), tile_bytes, p);
+    fax_launch(ctx, fp8_quantize_kernel<T, FMT, VEC, false, true>, dim3(blocks), dim3(THREADS<T>), tile_bytes, p);
   }
   return fax_after_launch(ctx);
 }
@@ -292,7 +312,7 @@ extern "C" fax_status fax_op_fp8_quantize(fax_ctx* ctx, int32_t prec, const fax_
     return FAX_ERR_INVALID_ARG;
   if (d->qt && (!d->st || d->ldqt < d->rows || d->ldqt % 16 || !fax_aligned(d->qt, 16) || !fax_aligned(d->st, 4) || d->ldst < (square ? cb : d->cols)))
     return FAX_ERR_INVALID_ARG;
-  if (rb * cb > 0x7fffffffLL) return FAX_ERR_UNSUPPORTED_SHAPE;
+  if (rb * cb > 0x40000000LL) return FAX_ERR_UNSUPPORTED_SHAPE;
   QuantParams p;
   p.rows = d->rows; p.cols = d->cols; p.x = d->x; p.ldx = d->ldx;
   p.q = (uint8_t*)d->q; p.ldq = d->ldq; p.s = d->s; p.lds = d->lds;
