@@ -15,6 +15,8 @@
 //     registers and written; a run that crosses a chunk's edge leaves partial sums (at most a first and
 //     a last one per chunk), and the chunk it begins in is listed.
 //  3. embed_join: adds the partial sums of each listed run in chunk order.
+// A row that is accumulated gets its sum by one reduction at L2 (nothing waits for the old value; one addition per
+// element and call, so the order is still fixed).
 //
 // An overwritten table has to be zeroed where no token touches it, most of the bytes of a small batch.
 // Where the rows that can be touched are few, further blocks of the sort's launches zero the whole table
@@ -51,16 +53,16 @@ SortPlan plan_for(int n, int vocab) {
   while (bits < 32 && ((uint32_t)vocab >> bits) != 0u) ++bits;      // keys 0 .. vocab (vocab: outside the table)
   p.passes = (bits + 7) / 8;
   p.bits = (bits + p.passes - 1) / p.passes;
-  // Chunks of 32 sorted tokens keep the launch wide; longer ones for large batches keep the partial sums few.
-  p.chunk = 32;
-  while (p.chunk < 1024 && (n + p.chunk - 1) / p.chunk > 2048) p.chunk *= 2;
+  // Chunks of 16 sorted tokens keep the launch wide; longer ones for large batches keep the partial sums few.
+  p.chunk = 16;
+  while (p.chunk < 1024 && (n + p.chunk - 1) / p.chunk > 1024) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   return p;
 }
 
 struct EmbedScratch {
   uint32_t* counts;                    // [passes][tiles][DIGITS], then the lengths of the two lists
-  uint32_t* lists;                     // [2][chunks]: chunks in which a short / long run begins that goes on
+  uint2* lists;                        // [2][chunks]: (chunk, id) of the short / long runs that begin in a chunk and go on
   uint8_t* touched;                    // [vocab]
   uint2* a; uint2* b;                  // (id, token) before and after a pass
   float* partial;                      // [chunks][2][d]: first run's part, last run's part
@@ -70,7 +72,7 @@ struct EmbedScratch {
 void carve(FaxArena& ar, const SortPlan& p, int vocab, int d, EmbedScratch* s) {
   s->count_words = (size_t)p.passes * p.tiles * DIGITS + 4;
   s->counts = (uint32_t*)ar.take(s->count_words * 4);
-  s->lists = (uint32_t*)ar.take((size_t)p.chunks * 2 * 4);
+  s->lists = (uint2*)ar.take((size_t)p.chunks * 2 * sizeof(uint2));
   s->touched = (uint8_t*)ar.take(fax_round_up((size_t)vocab, 16));
   s->a = (uint2*)ar.take((size_t)p.n * sizeof(uint2));
   s->b = (uint2*)ar.take((size_t)p.n * sizeof(uint2));
@@ -175,6 +177,9 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
   const int per_warp = p.tile / SORT_WARPS;                          // a multiple of 32
   const int w_lo = lo + warp * per_warp, w_hi = min(hi, w_lo + per_warp);
 
+  auto load = [&](int i) { return FIRST ? make_uint2(key_of(ids[i], vocab), (uint32_t)i) : in[i]; };
+  const uint2 early = w_lo + lane < w_hi ? load(w_lo + lane) : make_uint2(0u, 0u);      // in flight while the counts are read
+
   // counts of the tiles before this one, and of all tiles, by digit
   {
     const uint4* c = reinterpret_cast<const uint4*>(counts + (size_t)pass * p.tiles * DIGITS);
@@ -191,8 +196,7 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
   }
   __syncthreads();
   // this tile's digits, by warp
-  auto load = [&](int i) { return FIRST ? make_uint2(key_of(ids[i], vocab), (uint32_t)i) : in[i]; };
-  for (int i = w_lo + lane; i < w_hi; i += 32) atomicAdd(&off[warp][(load(i).x >> shift) & mask], 1u);
+  for (int i = w_lo + lane; i < w_hi; i += 32) atomicAdd(&off[warp][((i < w_lo + 32 ? early : load(i)).x >> shift) & mask], 1u);
   // exclusive sum of all tiles' totals over the digits
   uint32_t x = 0u, mine = 0u, incl = 0u;
   if (threadIdx.x < DIGITS) {
@@ -226,7 +230,7 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
   for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
     const int i = i0 + lane;
     const bool live = i < w_hi;
-    const uint2 kv = live ? load(i) : make_uint2(0u, 0u);
+    const uint2 kv = i0 == w_lo ? early : (live ? load(i) : make_uint2(0u, 0u));
     const uint32_t dgt = live ? ((kv.x >> shift) & mask) : DIGITS;   // lanes past the end match only each other
     const uint32_t same = __match_any_sync(0xffffffffu, dgt);
     const uint32_t rank = __popc(same & ((1u << lane) - 1u));
@@ -243,13 +247,20 @@ embed_sort_scatter_kernel(SortPlan p, int pass, int vocab, const int32_t* __rest
 }
 
 // ---- gradient ----
-// LG lanes (a power of two up to GRAD_THREADS) work on one chunk and one slice of LG * V columns.
+// Four sums of a table row: stored, or added to it by one vector reduction (16-byte aligned).
+__device__ __forceinline__ void put4(float* o, float a, float b, float c, float d, int accumulate) {
+  if (accumulate) asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(o), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+  else *reinterpret_cast<float4*>(o) = make_float4(a, b, c, d);
+}
+
+// `lanes` lanes (32, 64 or 128) work on one chunk and one slice of lanes * V columns.  A warp holds 32 sorted tokens at a
+// time, one a lane; where runs begin is one ballot, and rows are loaded U at a time whatever runs they belong to.
 template <typename T, int V>
 __global__ void __launch_bounds__(GRAD_THREADS)
 embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices, unsigned int grad_blocks, const uint2* __restrict__ sorted,
                   const T* __restrict__ dout, float scale, int accumulate, float* __restrict__ dtable,
                   float* __restrict__ partial, const uint8_t* __restrict__ touched, uint32_t* __restrict__ list_len,
-                  uint32_t* __restrict__ lists) {
+                  uint2* __restrict__ lists) {
   typedef typename Vec<T, V>::type vec;
   fax_grid_dependency_wait();
   if (blockIdx.x >= grad_blocks) {
@@ -268,15 +279,16 @@ embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices,
   const long long item = (long long)blockIdx.x * groups + threadIdx.x / lanes;
   const int chunk = (int)(item / slices), slice = (int)(item - (long long)chunk * slices);
   const int c = slice * lanes + (threadIdx.x & (lanes - 1));
-  if (chunk >= p.chunks || c >= nvec) return;
+  if (chunk >= p.chunks) return;
   const int lo = chunk * p.chunk, hi = min(p.n, lo + p.chunk);
   const uint32_t prev = lo > 0 ? sorted[lo - 1].x : 0xffffffffu, after = hi < p.n ? sorted[hi].x : 0xffffffffu;
-  const vec* src = reinterpret_cast<const vec*>(dout);
+  const bool active = c < nvec;
+  const vec* src = reinterpret_cast<const vec*>(dout) + (active ? c : 0);
   float acc[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) acc[j] = 0.f;
   auto flush = [&](uint32_t key, bool first_run, bool last_run) {
-    if (key >= (uint32_t)vocab) return;
+    if (key >= (uint32_t)vocab || !active) return;
     const bool from_before = first_run && prev == key, goes_on = last_run && after == key;
     if (from_before || goes_on) {
       // a run that crosses an edge: partial sums, slot 0 where it came from before, else slot 1
@@ -286,52 +298,54 @@ embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices,
       if (!from_before && c == 0) {
         const size_t far = (size_t)(chunk + 1 + JOIN_SHORT) * p.chunk;
         const int which = far < (size_t)p.n && sorted[far].x == key ? 1 : 0;
-        lists[(size_t)which * p.chunks + atomicAdd(list_len + which, 1u)] = (uint32_t)chunk;
+        lists[(size_t)which * p.chunks + atomicAdd(list_len + which, 1u)] = make_uint2((uint32_t)chunk, key);
       }
     } else {
       float* o = dtable + (size_t)key * d + (size_t)c * V;
+      if (V > 1) {
 #pragma unroll
-      for (int j = 0; j < V; j += (V > 1 ? 4 : 1)) {
-        if (V > 1) {
-          float4 y = make_float4(scale * acc[j], scale * acc[j + 1], scale * acc[j + 2], scale * acc[j + 3]);
-          if (accumulate) {
-            const float4 z = *reinterpret_cast<const float4*>(o + j);
-            y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
-          }
-          *reinterpret_cast<float4*>(o + j) = y;
-        } else {
-          o[j] = accumulate ? o[j] + scale * acc[j] : scale * acc[j];
-        }
+        for (int j = 0; j < V; j += 4) put4(o + j, scale * acc[j], scale * acc[j + 1], scale * acc[j + 2], scale * acc[j + 3], accumulate);
+      } else {
+        if (accumulate) atomicAdd(o, scale * acc[0]); else o[0] = scale * acc[0];
       }
     }
   };
-  constexpr int U = 4;
+  constexpr int U = 4;                                               // rows in flight per lane
+  const int lane = threadIdx.x & 31;
   uint32_t cur = sorted[lo].x;
   bool first_run = true;
-  for (int i0 = lo; i0 < hi; i0 += U) {
-    uint2 kv[U];
-    vec x[U];
+  for (int base = lo; base < hi; base += 32) {
+    const uint2 kv = base + lane < hi ? sorted[base + lane] : make_uint2((uint32_t)vocab, 0u);
+    uint32_t before = __shfl_up_sync(0xffffffffu, kv.x, 1);
+    if (lane == 0) before = cur;
+    const uint32_t heads = __ballot_sync(0xffffffffu, kv.x != before);
+    const int live = __popc(__ballot_sync(0xffffffffu, kv.x < (uint32_t)vocab));      // ids outside the table come last
+    for (int q = 0; q < live; q += U) {
+      vec x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) kv[u] = i0 + u < hi ? sorted[i0 + u] : make_uint2((uint32_t)vocab, 0u);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (kv[u].x < (uint32_t)vocab) x[u] = src[(size_t)kv[u].y * nvec + c];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + u >= hi) break;
-      if (kv[u].x != cur) {
-        flush(cur, first_run, false);
-        first_run = false;
-        cur = kv[u].x;
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
+      for (int u = 0; u < U; ++u) {
+        const uint32_t token = __shfl_sync(0xffffffffu, kv.y, (q + u) & 31);
+        if (q + u < live) x[u] = src[(size_t)token * nvec];
       }
-      if (cur < (uint32_t)vocab) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (q + u >= live) break;
+        if ((heads >> (q + u)) & 1u) {
+          flush(cur, first_run, false);
+          first_run = false;
+          cur = __shfl_sync(0xffffffffu, kv.x, q + u);
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] = 0.f;
+        }
         float f[V];
         widen<T, V>(x[u], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] += f[j];
       }
+    }
+    if (live < 32 && base + live < hi) {                             // what follows is outside the table: the last run ends here
+      flush(cur, first_run, false);
+      return;
     }
   }
   flush(cur, first_run, true);
@@ -342,7 +356,7 @@ embed_grad_kernel(SortPlan p, int vocab, int d, int nvec, int lanes, int slices,
 template <bool WIDE>
 __global__ void __launch_bounds__(32 * JOIN_WARPS)
 embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const float* __restrict__ partial, const uint32_t* __restrict__ list_len,
-                  const uint32_t* __restrict__ lists, float scale, int accumulate, float* __restrict__ dtable) {
+                  const uint2* __restrict__ lists, float scale, int accumulate, float* __restrict__ dtable) {
   __shared__ float4 part[JOIN_WARPS][32];
   fax_grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -361,20 +375,27 @@ embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const flo
   };
   auto add = [](float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; };
   auto finish = [&](uint32_t key, int col, const float4& t) {
-    const float f[4] = {scale * t.x, scale * t.y, scale * t.z, scale * t.w};
     float* o = dtable + (size_t)key * d + col;
+    if (WIDE) {
+      if (col < d) put4(o, scale * t.x, scale * t.y, scale * t.z, scale * t.w, accumulate);
+    } else {
+      const float f[4] = {scale * t.x, scale * t.y, scale * t.z, scale * t.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (col + j < d) o[j] = accumulate ? o[j] + f[j] : f[j];
+      for (int j = 0; j < 4; ++j)
+        if (col + j < d) { if (accumulate) atomicAdd(o + j, f[j]); else o[j] = f[j]; }
+    }
   };
   for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
     const bool is_long = item >= n_short;
     const long long k = is_long ? item - n_short : item, per = is_long ? slices : groups;
-    const int chunk = (int)lists[(is_long ? (size_t)p.chunks : 0) + (size_t)(k / per)];
+    const uint2 run = lists[(is_long ? (size_t)p.chunks : 0) + (size_t)(k / per)];
+    const int chunk = (int)run.x;
+    const uint32_t key = run.y;
     const int slice = is_long ? (int)(k % per) : (int)(k % per) * JOIN_WARPS + warp;
-    const int col = slice * 128 + 4 * lane;
-    const uint32_t key = sorted[(size_t)(chunk + 1) * p.chunk].x;
-    // the chunks after this one that begin with the key
+    const int col = slice < slices ? slice * 128 + 4 * lane : d;
+    const float* rest = partial + (size_t)(chunk + 1) * 2 * d;       // slot 0 of the next chunk
+    // the run's first part and the one after it, and the chunks after this one that begin with the id, in one go
+    const float4 first = load(partial + ((size_t)chunk * 2 + 1) * d, col), second = load(rest, col);
     int count = 0;
     for (int c = chunk + 1;; c += 32) {
       const bool same = c + lane < p.chunks && sorted[(size_t)(c + lane) * p.chunk].x == key;
@@ -382,15 +403,12 @@ embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const flo
       count += __popc(m);
       if (m != 0xffffffffu) break;
     }
-    const float* first = partial + ((size_t)chunk * 2 + 1) * d;
-    const float* rest = partial + (size_t)(chunk + 1) * 2 * d;       // slot 0 of the next chunk
     if (!is_long) {
-      if (slice < slices) {
-        float4 t = load(first, col);
+      float4 t = first;
+      add(t, second);
 #pragma unroll 8
-        for (int c = 0; c < count; ++c) add(t, load(rest + (size_t)c * 2 * d, col));
-        finish(key, col, t);
-      }
+      for (int c = 1; c < count; ++c) add(t, load(rest + (size_t)c * 2 * d, col));
+      finish(key, col, t);
     } else {
       const int share = (count + JOIN_WARPS - 1) / JOIN_WARPS, c1 = min(count, (warp + 1) * share);
       float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -399,7 +417,7 @@ embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const flo
       part[warp][lane] = t;
       __syncthreads();
       if (warp == 0) {
-        float4 u = load(first, col);
+        float4 u = first;
 #pragma unroll
         for (int w = 0; w < JOIN_WARPS; ++w) add(u, part[w][lane]);
         finish(key, col, u);
@@ -413,7 +431,7 @@ template <typename T, int V>
 fax_status launch_grad(fax_ctx* ctx, const SortPlan& p, int vocab, int d, const uint2* sorted, const void* dout, float scale,
                        int accumulate, bool fill_here, float* dtable, const EmbedScratch& s) {
   const int nvec = d / V;
-  int lanes = 1;
+  int lanes = 32;
   while (lanes < nvec && lanes < GRAD_THREADS) lanes *= 2;
   const int slices = (nvec + lanes - 1) / lanes, groups = GRAD_THREADS / lanes;
   const long long items = (long long)p.chunks * slices, gb = (items + groups - 1) / groups;
@@ -518,10 +536,10 @@ fax_status fax_embedding_grad(fax_ctx* ctx, int prec, int n, int vocab, int d, c
     const long long items = (long long)p.chunks * ((d + 1023) / 1024), cap = (long long)ctx->sm_count * 8;
     const dim3 grid((unsigned int)(items < cap ? items : cap));
     const uint32_t* len = s.counts + s.count_words - 4;
-    if (d % 4 == 0)
-      fax_launch(ctx, embed_join_kernel<true>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint32_t*)s.lists, scale, acc, dtable);
+    if (d % 4 == 0 && fax_aligned(dtable, 16))
+      fax_launch(ctx, embed_join_kernel<true>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint2*)s.lists, scale, acc, dtable);
     else
-      fax_launch(ctx, embed_join_kernel<false>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint32_t*)s.lists, scale, acc, dtable);
+      fax_launch(ctx, embed_join_kernel<false>, grid, dim3(32 * JOIN_WARPS), 0, p, d, sorted, (const float*)s.partial, len, (const uint2*)s.lists, scale, acc, dtable);
     FAX_TRY(fax_after_launch(ctx));
   }
   return FAX_OK;
