@@ -30,6 +30,7 @@ class FaxError(RuntimeError):
 
 
 FAX_KERNEL_CLASSES = 12
+FAX_ADAMW8_BLOCK = 128
 
 
 class ProfileEntry(C.Structure):
@@ -104,6 +105,7 @@ _SIGNATURES = {
     "fax_set_dependent_launch": (C.c_int32, [_P, C.c_int32]),
     "fax_set_graph_replay": (C.c_int32, [_P, C.c_int32]),
     "fax_set_attention_backward_two_chains": (C.c_int32, [_P, C.c_int32]),
+    "fax_set_sorted_embedding_gradient": (C.c_int32, [_P, C.c_int32]),
     "fax_set_gemm_l2_budget": (C.c_int32, [_P, C.c_int64]),
     "fax_set_fused_update": (C.c_int32, [_P, C.c_int32, C.c_int32]),
     "fax_profile_begin": (C.c_int32, [_P]),
@@ -225,6 +227,11 @@ def fax_set_gemm_l2_budget(ctx, nbytes: int):
 def fax_set_attention_backward_two_chains(ctx, mode: int):
     _check(load_library().fax_set_attention_backward_two_chains(ctx, int(mode)),
            "fax_set_attention_backward_two_chains")
+
+
+def fax_set_sorted_embedding_gradient(ctx, enable: bool):
+    _check(load_library().fax_set_sorted_embedding_gradient(ctx, int(bool(enable))),
+           "fax_set_sorted_embedding_gradient")
 
 
 def fax_profile_begin(ctx):

@@ -41,6 +41,7 @@ extern "C" fax_status fax_create(fax_ctx** out, int32_t device_ordinal, void* cu
   c->use_2cta = true;
   c->use_pdl = true;
   c->attn_bwd_mode = 2;
+  c->sorted_embed_grad = false;
   c->gemm_l2_budget = 48e6;
   c->use_graphs = true;
   c->fused_update = false;
@@ -160,6 +161,14 @@ extern "C" fax_status fax_set_attention_backward_two_chains(fax_ctx* ctx, int32_
   if (!ctx) return FAX_ERR_INVALID_ARG;
   if (enable < 0 || enable > 2) return FAX_ERR_INVALID_ARG;
   ctx->attn_bwd_mode = enable;
+  cudaStreamSynchronize(ctx->stream);
+  fax_graph_clear(ctx);
+  return FAX_OK;
+}
+
+extern "C" fax_status fax_set_sorted_embedding_gradient(fax_ctx* ctx, int32_t enable) {
+  if (!ctx) return FAX_ERR_INVALID_ARG;
+  ctx->sorted_embed_grad = enable != 0;
   cudaStreamSynchronize(ctx->stream);
   fax_graph_clear(ctx);
   return FAX_OK;

@@ -62,6 +62,7 @@ struct fax_ctx {
   bool use_pdl;              // kernels are launched with programmatic stream serialization allowed
   double gemm_l2_budget;     // bytes of L2 a GEMM may count on for the operand panels it keeps between waves (0: fixed raster)
   int attn_bwd_mode;         // attention backward: 0 one-tile kernel, 1 sixteen row warps, 2 also two score tiles in flight at head_dim 64
+  bool sorted_embed_grad;    // the LM step sums the token table's gradient over sorted tokens (fixed order) instead of float atomics
 };
 
 // Brackets the launches of one operator with CUDA events while profiling is on.
@@ -293,7 +294,8 @@ fax_status fax_attention_bwd_simt(fax_ctx* ctx, int prec, int B, int T, int H, i
 fax_status fax_embed_fwd(fax_ctx* ctx, int prec, int B, int T, int d, int vocab, const int32_t* ids,
                          const void* wte, const void* wpe, void* x0);
 fax_status fax_embed_bwd(fax_ctx* ctx, int prec, int B, int T, int max_seq, int d, int vocab,
-                         const int32_t* ids, const void* dx0, float* dwte, float* dwpe, bool accumulate_wpe);
+                         const int32_t* ids, const void* dx0, float* dwte, float* dwpe, bool accumulate_wpe,
+                         void* sort_scratch = nullptr, size_t sort_scratch_bytes = 0);   // sort scratch: dwte by fax_embedding_grad
 // Scaled lookup, and the table's gradient by sorted tokens (see embedding.cu); n = 0 is allowed.
 fax_status fax_embedding_lookup(fax_ctx* ctx, int prec, int n, int vocab, int d, const int32_t* ids, const void* table, float scale, void* out);
 size_t fax_embedding_grad_scratch_bytes(int n, int vocab, int d);

@@ -269,16 +269,23 @@ fax_status fax_embed_fwd(fax_ctx* ctx, int prec, int B, int T, int d, int vocab,
 }
 
 fax_status fax_embed_bwd(fax_ctx* ctx, int prec, int B, int T, int max_seq, int d, int vocab,
-                         const int32_t* ids, const void* dx0, float* dwte, float* dwpe, bool accumulate_wpe) {
+                         const int32_t* ids, const void* dx0, float* dwte, float* dwpe, bool accumulate_wpe,
+                         void* sort_scratch, size_t sort_scratch_bytes) {
   int n = B * T;
-  FaxProfScope prof(ctx, KC_EMBED, 0.0, (double)n * d * (2.0 * fax_elem_size(prec) + 8.0));
+  const bool sorted = sort_scratch != nullptr;
+  if (sorted) FAX_TRY(fax_embedding_grad(ctx, prec, n, vocab, d, ids, dx0, 1.f, true, dwte, sort_scratch, sort_scratch_bytes));
+  FaxProfScope prof(ctx, KC_EMBED, 0.0, (double)n * d * (sorted ? fax_elem_size(prec) : 2.0 * fax_elem_size(prec) + 8.0));
   if (prec == FAX_PREC_BF16) {
-    fax_launch(ctx, embed_bwd_wte_kernel<bf16>, dim3(n), dim3(128), 0, n, d, vocab, ids, (const bf16*)dx0, dwte);
-    FAX_TRY(fax_after_launch(ctx));
+    if (!sorted) {
+      fax_launch(ctx, embed_bwd_wte_kernel<bf16>, dim3(n), dim3(128), 0, n, d, vocab, ids, (const bf16*)dx0, dwte);
+      FAX_TRY(fax_after_launch(ctx));
+    }
     fax_launch(ctx, embed_bwd_wpe_kernel<bf16>, dim3(max_seq), dim3(128), 0, B, T, max_seq, d, (const bf16*)dx0, dwpe, accumulate_wpe ? 1 : 0);
   } else {
-    fax_launch(ctx, embed_bwd_wte_kernel<float>, dim3(n), dim3(128), 0, n, d, vocab, ids, (const float*)dx0, dwte);
-    FAX_TRY(fax_after_launch(ctx));
+    if (!sorted) {
+      fax_launch(ctx, embed_bwd_wte_kernel<float>, dim3(n), dim3(128), 0, n, d, vocab, ids, (const float*)dx0, dwte);
+      FAX_TRY(fax_after_launch(ctx));
+    }
     fax_launch(ctx, embed_bwd_wpe_kernel<float>, dim3(max_seq), dim3(128), 0, B, T, max_seq, d, (const float*)dx0, dwpe, accumulate_wpe ? 1 : 0);
   }
   return fax_after_launch(ctx);

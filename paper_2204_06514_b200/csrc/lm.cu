@@ -31,7 +31,8 @@ struct LmScratch {
   int32_t* ids; int32_t* targets;   // staging for the host entry point
   BlockScratch blk;
   void* dxa; void* dxb;             // gradient ping-pong between layers
-  void* logits; int head_rows;
+  void* logits; int head_rows;      // after the head also the scratch of the sorted embedding gradient
+  size_t logits_bytes;
   float* row_loss;
 };
 
@@ -65,7 +66,10 @@ void carve_scratch(const fax_lm_cfg* c, FaxArena& ar, LmScratch* s) {
   s->dxa = ar.take(N * d * es);
   s->dxb = ar.take(N * d * es);
   s->head_rows = head_rows_for(c, N, (size_t)c->vocab, es);
-  s->logits = ar.take((size_t)s->head_rows * c->vocab * es);
+  s->logits_bytes = (size_t)s->head_rows * c->vocab * es;
+  const size_t sort_bytes = fax_embedding_grad_scratch_bytes((int)N, c->vocab, (int)d);
+  if (s->logits_bytes < sort_bytes) s->logits_bytes = sort_bytes;
+  s->logits = ar.take(s->logits_bytes);
   s->row_loss = (float*)ar.take(N * 4);
 }
 
@@ -158,7 +162,8 @@ fax_status lm_fwd_bwd(fax_ctx* ctx, const fax_lm_cfg* c, const fax_lm_state* st,
     void* t = dcur; dcur = dnext; dnext = t;
   }
   // embedding gradients: scatter into the tied dwte, batch-sum into dwpe
-  return fax_embed_bwd(ctx, prec, bc->batch, bc->seq, c->max_seq, d, V, ids, dcur, st->wte.g, st->wpe.g, acc);
+  return fax_embed_bwd(ctx, prec, bc->batch, bc->seq, c->max_seq, d, V, ids, dcur, st->wte.g, st->wpe.g, acc,
+                       ctx->sorted_embed_grad ? w.logits : nullptr, w.logits_bytes);
 }
 
 // AdamW of the tensors that are not inside a block (the blocks' tensors are updated under backward).
