@@ -22,6 +22,10 @@
 // CG = 2: a pair of SMs works on one 256 x BN tile (each CTA 128 rows of A and half of B's rows); CG = 1: one
 // SM on 128 x BN.  BN and the pipeline's depth are run-time parameters: the launcher picks them by size.
 //
+// SPLIT: few tiles and a long K (one token's product with a large weight).  A cluster of CTAs shares one tile, each over a
+// slice of K; all but the first send their float sums to the first one's shared memory, which adds them in
+// order (16 x 4096 x 4096: 12.4 us unsplit, 10.4 us on clusters of eight).
+//
 // Edges: TMA fills what lies outside a matrix with zeros (scales outside are 1), and the stores are
 // limited to C.  Every wait is bounded.
 #include "gemm_common.cuh"
@@ -47,6 +51,7 @@ constexpr int NUM_THREADS = 512;
 // 128 registers a thread at launch; 256 x 64 + 256 x 192 = 512 x 128
 constexpr int REGS_OTHER = 64, REGS_SUMS = 192;
 static_assert(256 * REGS_OTHER + 256 * REGS_SUMS <= NUM_THREADS * 128, "register split");
+constexpr int SPLIT_CHUNKS = 2;    // SPLIT: tiles of 128 columns at most
 constexpr int TEAM = 64;           // threads of a scale team
 constexpr int MAX_STAGES = 12;
 constexpr int SC_SLOTS = 4;        // groups of scales in flight
@@ -66,6 +71,7 @@ struct Fp8Params {
   const bf16* bias;
   int bn, stages, tmem_cols, acc1, scale_col;                       // tile width, pipeline depth, tensor-memory columns
   int tiles_m, tiles_n, group_m, group_along_n;
+  int splits, kb_per, rows_q;                                       // SPLIT: CTAs per tile, K blocks of each, groups of 32 rows in a tile
   int32_t* status;
 };
 
@@ -234,7 +240,12 @@ __device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMa
   }
 }
 
-template <int CG, bool SUMS>
+// Words to the same place of the first CTA of the cluster.
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+template <int CG, bool SUMS, bool SPLIT>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_c,
                 const __grid_constant__ Fp8Params p) {
@@ -258,9 +269,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_ctarank();
   const bool leader = (rank == 0);
-  const int unit = blockIdx.x / CG, num_units = gridDim.x / CG;
+  static_assert(!SPLIT || (CG == 1 && SUMS), "slices of K are joined as float sums");
+  const int slice = SPLIT ? (int)cluster_ctarank() : 0;
   const int num_tiles = p.tiles_m * p.tiles_n;
-  const int kb_total = (p.K + BK - 1) / BK;
+  const int unit = SPLIT ? blockIdx.x / p.splits : blockIdx.x / CG, num_units = SPLIT ? num_tiles : gridDim.x / CG;
+  const int kb_all = (p.K + BK - 1) / BK;
+  const int kb_off = SPLIT ? slice * p.kb_per : 0, kb_total = SPLIT ? min(p.kb_per, kb_all - kb_off) : kb_all;      // this CTA's K blocks
   const int seg_len = SUMS ? SEGMENT : kb_total, segments = (kb_total + seg_len - 1) / seg_len;
 
   if (threadIdx.x == 0) {
@@ -284,7 +298,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   }
   tc_fence_before();
   __syncthreads();
-  if (CG == 2) cluster_sync_all();   // both CTAs' barriers exist before either signals the other
+  if (CG == 2 || SPLIT) cluster_sync_all();   // the other CTAs run, their barriers exist
   tc_fence_after();
   const uint32_t tmem_base = *tmem_base_slot;
   fax_grid_dependency_wait();        // global memory only from here
@@ -305,8 +319,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
           const uint32_t a_dst = tiles_base + (uint32_t)stage * stage_bytes;
           const uint32_t fbar = CG == 1 ? full_bar(stage) : leader_addr(full_bar(stage));
           if (leader) mbar_expect_tx(full_bar(stage), CG * stage_bytes);             // both CTAs' bytes
-          tma_load<CG>(a_dst, &tmap_a, fbar, kb * BK, m0);
-          tma_load<CG>(a_dst + BM * BK, &tmap_b, fbar, kb * BK, n0);
+          tma_load<CG>(a_dst, &tmap_a, fbar, (kb_off + kb) * BK, m0);
+          tma_load<CG>(a_dst + BM * BK, &tmap_b, fbar, (kb_off + kb) * BK, n0);
           if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -394,7 +408,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         uint32_t wa[BM / TEAM], wb[MAX_BN / TEAM];
         long long at[GROUP];
 #pragma unroll
-        for (int b = 0; b < GROUP; ++b) at[b] = min(g * GROUP + b, kb_total - 1);
+        for (int b = 0; b < GROUP; ++b) at[b] = kb_off + min(g * GROUP + b, kb_total - 1);
         float fa[BM / TEAM][GROUP], fb[MAX_BN / TEAM][GROUP];
 #pragma unroll
         for (int i = 0; i < BM / TEAM; ++i)
@@ -431,6 +445,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
       }
     }
   }
+  if (SPLIT) { __syncwarp(); cluster_sync_all(); }                   // the row warps' exchange below
   } else {
     // ---------------- epilogue: this CTA's 128 rows of the tile ----------------
     if (SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SUMS));
@@ -499,7 +514,34 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
           }
         }
       }
-      if (SUMS && ok) {
+      if (SPLIT) {
+        // a unit has one tile: every warp passes this exchange once.  Slot of (slice, row group, half, chunk): 32 columns x 32 rows
+        const uint32_t recv = tiles_base + bar_off + BAR_BYTES;
+        auto slot = [&](int sl, int i) { return (uint32_t)((((sl - 1) * p.rows_q + q) * 2 + half) * chunks + i) * 4096u + (uint32_t)lane * 4u; };
+        if (slice != 0 && q < p.rows_q) {
+#pragma unroll
+          for (int i = 0; i < SPLIT_CHUNKS; ++i)
+            if (i < chunks) {
+              const uint32_t dst = leader_addr(recv + slot(slice, i));
+#pragma unroll
+              for (int e = 0; e < 32; ++e) st_cluster(dst + 128u * e, sum[SUMS ? i : 0][e]);
+            }
+        }
+        __syncwarp();
+        cluster_sync_all();                        // release of the sums, acquire by the first CTA
+        if (slice == 0 && q < p.rows_q) {
+          const uint8_t* src = gen_base + bar_off + BAR_BYTES;
+#pragma unroll
+          for (int i = 0; i < SPLIT_CHUNKS; ++i)
+            if (i < chunks)
+              for (int sl = 1; sl < p.splits; ++sl) {
+                const float* f = reinterpret_cast<const float*>(src + slot(sl, i));
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[SUMS ? i : 0][e] = __float_as_uint(__uint_as_float(sum[SUMS ? i : 0][e]) + f[32 * e]);
+              }
+        }
+      }
+      if (SUMS && ok && slice == 0) {
 #pragma unroll
         for (int i = 0; i < SUM_CHUNKS; ++i)
           if (i < chunks) store_chunk(p, &tmap_c, sum[SUMS ? i : 0], row0, n0 + 32 * (half + 2 * i), stg, stg_addr, lane);
@@ -540,41 +582,55 @@ bool make_map_c(fax_ctx* ctx, CUtensorMap* map, const void* base, uint64_t inner
                                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// fax_launch, with clusters of CG CTAs.
-template <int CG, bool SUMS>
-fax_status launch(fax_ctx* ctx, int units, int smem, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Fp8Params& p) {
+// fax_launch, with clusters of `cluster` CTAs.
+template <int CG, bool SUMS, bool SPLIT>
+fax_status launch(fax_ctx* ctx, int grid, int cluster, int smem, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const Fp8Params& p) {
   static bool done[FAX_MAX_DEVICES] = {};
-  FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<CG, SUMS>, SMEM_MAX, done));
+  FAX_TRY(fax_opt_in_shared_memory(ctx, fp8_gemm_kernel<CG, SUMS, SPLIT>, SMEM_MAX, done));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(CG * units); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ctx->use_pdl ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<CG, SUMS>, ma, mb, mc, p);  // errors surface in fax_after_launch
+  (void)cudaLaunchKernelEx(&cfg, fp8_gemm_kernel<CG, SUMS, SPLIT>, ma, mb, mc, p);      // errors surface in fax_after_launch
   return fax_after_launch(ctx);
 }
 
-struct TileChoice { int cg, bn; };
+// Shared memory beside the stages; `split_bytes`: the sums that the first CTA of a cluster receives.
+constexpr int FIXED_SMEM = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + NUM_EPI_WARPS * STG_BYTES;
+int split_bytes(int splits, int M, int bn) { return (splits - 1) * (M < 128 ? (M + 31) / 32 : 4) * (bn / 32) * 4096; }
+
 // Time of a tile shape in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's end),
 // the paces as measured with all SMs busy.  A pair of SMs loads each operand byte for twice the work and runs best
 // where there are tiles for all pairs; a narrower tile has about the pace of the 128-column one (the issue of
-// its MMAs bounds it), so it pays only where it brings more SMs to work.
+// its MMAs bounds it), so it pays only where it brings more SMs to work.  Where the tiles leave SMs idle, slices of K
+// bring them in, for the price of the exchange.
+struct TileChoice { int cg, bn, splits; };
 TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
   struct Shape { int cg, bn; double pace, end; };
   static const Shape shapes[] = {{2, 256, 0.40, 1.5}, {2, 192, 0.33, 1.3}, {1, 256, 0.42, 1.2}, {1, 128, 0.31, 0.8}, {1, 64, 0.29, 0.6}};
-  const double kb = (K + BK - 1) / BK;
-  TileChoice best = {2, 256};
+  constexpr double EXCHANGE = 1.5;
+  const int kb = (K + BK - 1) / BK;
+  TileChoice best = {2, 256, 1};
   double least = 1e30;
   for (const Shape& s : shapes) {
     const double tiles = (double)((M + s.cg * BM - 1) / (s.cg * BM)) * ((N + s.bn - 1) / s.bn);
     const double waves = (double)(long long)((tiles + ctx->sm_count / s.cg - 1) / (ctx->sm_count / s.cg));
     const double pace = s.pace + (sums && s.bn == 256 ? 0.09 : 0.0);        // the accumulators share columns: a pause per segment
     const double t = waves * (kb * pace + s.end) + (s.cg == 2 ? 0.5 : 0.0);
-    if (t < least) { least = t; best = {s.cg, s.bn}; }
+    if (t < least) { least = t; best = {s.cg, s.bn, 1}; }
+    if (s.cg != 1 || s.bn > 32 * 2 * SPLIT_CHUNKS) continue;
+    for (int splits = 2; splits <= 8; splits *= 2) {
+      const int per = (kb + splits - 1) / splits;
+      if (per < 2 || (kb + per - 1) / per != splits || tiles * splits > ctx->sm_count) continue;
+      if (SMEM_MAX - FIXED_SMEM - split_bytes(splits, M, s.bn) < 4 * (BM + s.bn) * BK) continue;
+      const double ts = per * s.pace + s.end + EXCHANGE;
+      if (ts < least) { least = ts; best = {1, s.bn, splits}; }
+    }
   }
   return best;
 }
@@ -595,8 +651,8 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
     return FAX_ERR_INVALID_ARG;
   if (d->lda >= (1LL << 40) || d->ldb >= (1LL << 40)) return FAX_ERR_UNSUPPORTED_SHAPE;        // the pitch a tensor map can hold
   if (d->M > 0x7fffff00 || d->N > 0x7fffff00 || d->K > 0x7fffff00) return FAX_ERR_UNSUPPORTED_SHAPE;
-  const bool sums = d->c_f32 && d->K > SEGMENT * BK;         // otherwise one segment holds all of K
-  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K, sums);
+  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K, d->c_f32 && d->K > SEGMENT * BK);
+  const bool sums = t.splits > 1 || (d->c_f32 && d->K > SEGMENT * BK);      // otherwise one segment holds all of K
   CUtensorMap ma, mb;
   if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, (uint32_t)(t.bn / t.cg))) return FAX_ERR_INVALID_ARG;
   Fp8Params p;
@@ -610,10 +666,13 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   if (p.bulk && !make_map_c(ctx, &mc, d->C, d->N, d->M, d->ldc, d->c_f32 != 0)) return FAX_ERR_INVALID_ARG;
   p.bias = (const bf16*)d->bias;
   p.bn = t.bn;
-  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + NUM_EPI_WARPS * STG_BYTES;
+  const int stage_bytes = BM * BK + t.bn / t.cg * BK, fixed = FIXED_SMEM + (t.splits > 1 ? split_bytes(t.splits, d->M, t.bn) : 0);
   p.stages = (SMEM_MAX - fixed) / stage_bytes;
   if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
   const int smem = p.stages * stage_bytes + fixed;
+  p.splits = t.splits;
+  p.kb_per = ((d->K + BK - 1) / BK + t.splits - 1) / t.splits;
+  p.rows_q = d->M < 128 ? (d->M + 31) / 32 : 4;
   // two accumulators and the scales; at 256 columns the accumulators share the columns that the scales take
   p.tmem_cols = 64;
   while (p.tmem_cols < 2 * t.bn + TMEM_SCALE_COLS && p.tmem_cols < 512) p.tmem_cols *= 2;
@@ -626,6 +685,7 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
   FaxProfScope prof(ctx, KC_FP8_GEMM, 2.0 * d->M * (double)d->N * d->K, 0.0);
   const int tiles = p.tiles_m * p.tiles_n, max_units = ctx->sm_count / t.cg;
   const int units = tiles < max_units ? tiles : max_units;
-  if (t.cg == 2) return sums ? launch<2, true>(ctx, units, smem, ma, mb, mc, p) : launch<2, false>(ctx, units, smem, ma, mb, mc, p);
-  return sums ? launch<1, true>(ctx, units, smem, ma, mb, mc, p) : launch<1, false>(ctx, units, smem, ma, mb, mc, p);
+  if (t.splits > 1) return launch<1, true, true>(ctx, tiles * t.splits, t.splits, smem, ma, mb, mc, p);
+  if (t.cg == 2) return sums ? launch<2, true, false>(ctx, 2 * units, 2, smem, ma, mb, mc, p) : launch<2, false, false>(ctx, 2 * units, 2, smem, ma, mb, mc, p);
+  return sums ? launch<1, true, false>(ctx, units, 1, smem, ma, mb, mc, p) : launch<1, false, false>(ctx, units, 1, smem, ma, mb, mc, p);
 }

@@ -169,6 +169,28 @@ def test_product_pitches(sess, m, n, k, b_tile, f32):
         product(sess, m, n, k, 0, 0, b_tile, f32, 0, 1, rng, pad=3, out_pad=out_pad, shift=shift)
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 512, 2048), (16, 1024, 4096), (33, 200, 3000), (64, 300, 1111), (97, 129, 2500), (128, 64, 8192), (200, 130, 4100), (300, 260, 1920)])
+@pytest.mark.parametrize("b_tile", [1, 128])
+@pytest.mark.parametrize("f32,acc,bias,pad", [(0, 0, 1, 0), (1, 1, 0, 0), (1, 0, 0, 3)])
+def test_product_of_few_tiles_and_long_k(sess, m, n, k, b_tile, f32, acc, bias, pad):
+    """Slices of K on a cluster of CTAs, joined by the first: one to four groups of 32 rows, ragged last slices."""
+    rng = np.random.default_rng(m + n * 2 + k)
+    product(sess, m, n, k, 0, 1, b_tile, f32, acc, bias, rng, out_pad=pad)
+
+
+def test_product_is_the_same_bits_every_time(sess):
+    rng = np.random.default_rng(12)
+    for m, n, k in ((16, 1024, 4096), (300, 500, 2000)):
+        a, sa, b, sb = operands(m, n, k, 0, 0, 128, rng)
+        (ta, tsa), (tb, tsb) = to_dev(sess, a, sa, 0, 0, 0), to_dev(sess, b, sb, 0, 0, 0)
+        outs = []
+        for _ in range(4):
+            out = torch.full((m, n), float("nan"), device=sess.device)
+            ops.fax_op_fp8_gemm(sess.ctx, ops.Fp8GemmDesc(m, n, k, ptr(ta), ta.shape[1], 0, ptr(tsa), m, ptr(tb), tb.shape[1], 0, ptr(tsb), tsb.shape[1], 128, ptr(out), n, 1, 0, None))
+            outs.append(out)
+        assert all(torch.equal(o, outs[0]) for o in outs)
+
+
 def test_product_of_many_tiles(sess):
     """More tiles than pairs of SMs, ragged on every side; against a product in 64 bits on the GPU."""
     m, n, k = 5100, 4200, 900
