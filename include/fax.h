@@ -189,8 +189,8 @@ fax_status fax_adamw_step(fax_ctx* ctx, const fax_adamw_tensor* tensors, int32_t
  *   m = b1*m + (1-b1)*g          v = b2*v + ((1-b2)*g)*g
  *   w = (w - (lr*wd)*w) - (lr*(m*c1)) / (sqrt(v*c2) + eps)
  * Every float32 operation of m and v is rounded on its own in this order, so the
- * stored moments are the same bits everywhere; quotient and root are the hardware's,
- * the root of at least 2^-126.
+ * stored moments are the same bits everywhere; quotient and root are within one
+ * unit of the last place, the root taken of at least 2^-126.
  * (c1 = 1/(1-b1^t), c2 = 1/(1-b2^t), taken in float64 and rounded), and stored
  * again: the scale is the smallest power of two, at least 2^-126, that brings the
  * largest finite moment of the block to the format's largest value at most (1 for

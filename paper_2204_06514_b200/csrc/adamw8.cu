@@ -13,8 +13,11 @@
 // m / (sqrt(0) + eps) would be a step out of all proportion.  Why e5m2 for v: it is a square, so it
 // needs twice the exponent range of m.  Why powers of two: m / s is then exact, the rounding is the
 // only loss, and the moments after a step are one well-defined bit pattern (their float operations are each
-// rounded on its own, in the order written; no contraction).  The update of w uses the hardware's
-// reciprocal and square root (each within 2 units of the last place): its relative error is far below w's rounding.
+// rounded on its own, in the order written; no contraction).  The update of w takes root and quotient from the
+// hardware's approximations and one correction each by the exact remainder, which a fused multiply-add gives
+// (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990): rounded right but
+// for rare halfway cases, so that w's bf16 copy is the definition's too.  Two elements share an instruction (f32x2)
+// where no product is added to: the assembler contracts packed products and sums, which the moments must not be.
 //
 // The rounding in integers: y 2^-120 (2^-112 for e5m2) puts the format's smallest normal value on
 // float32's, so that the float's bits, cut off after the format's mantissa, are the format's code,
@@ -25,7 +28,8 @@
 // HBM-bound if the instructions are few: 18 bytes per element (w 8, g 4, m 2, v 2, bf16 copy 2) against 30 with
 // float32 moments.  A warp takes one block of 128 elements at a time, four elements a lane, so that a block's
 // maximum is one warp reduction (redux) and every access is a full 32-byte sector or more.  Moments that are
-// not finite are looked for once a block (their bits are the largest), not element by element.
+// not finite are looked for once a block (their bits are the largest), not element by element.  201M elements: 615 us,
+// 5.9 TB/s, 84 instructions an element; 900 us with every check and IEEE operation an element of its own.
 #include "common.cuh"
 
 #include <cuda_fp8.h>
@@ -33,7 +37,7 @@
 namespace {
 
 constexpr int QB = FAX_ADAMW8_BLOCK;   // elements per scale
-constexpr int THREADS = 256;
+constexpr int THREADS = 128;
 constexpr int UNROLL = 2;              // blocks of 128 a warp has in flight
 constexpr int CHUNK = THREADS / 32 * UNROLL * QB;
 constexpr int MAX_T = 40;              // tensors per launch (kernel-parameter space)
@@ -80,21 +84,60 @@ __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&c)[4]) {
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
 __device__ __forceinline__ uint32_t max4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return max(__vimax3_u32(a, b, c), d); }
 
-// Square root and reciprocal of the hardware.  They take numbers below 2^-126 for zero: x is kept above (a NaN stays).
-__device__ __forceinline__ float sqrt_fast(float x) {
-  float y;
-  asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0f00800000;\n\tsqrt.approx.ftz.f32 %0, t;\n\t}" : "=f"(y) : "f"(x));
-  return y;
+// Two float32 in one register pair; one instruction for both.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
-__device__ __forceinline__ float rcp_fast(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+__device__ __forceinline__ void split(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// sqrt(x) for x >= 2^-126: x is raised to that (a NaN stays): the approximation takes smaller numbers for zero.
+// s = x y, y ~ 1 / sqrt(x);  s + (x - s s) y / 2.
+__device__ __forceinline__ f2 sqrt2(f2 x) {
+  float a, b, ya, yb;
+  split(x, a, b);
+  asm("max.NaN.f32 %0, %0, 0f00800000;" : "+f"(a));
+  asm("max.NaN.f32 %0, %0, 0f00800000;" : "+f"(b));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(a));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(b));
+  const f2 c = pair(a, b), y = pair(ya, yb), minus = pair(-1.f, -1.f), half = pair(0.5f, 0.5f);
+  const f2 s = mul2(c, y);
+  return fma2(fma2(mul2(s, minus), s, c), mul2(y, half), s);
+}
+// a / b: r = 1 / b with one Newton step, q = a r;  q + (a - b q) r.
+__device__ __forceinline__ f2 div2(f2 a, f2 b) {
+  float u, v, ru, rv;
+  split(b, u, v);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ru) : "f"(u));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rv) : "f"(v));
+  const f2 r0 = pair(ru, rv), bn = mul2(b, pair(-1.f, -1.f));
+  const f2 r = fma2(r0, fma2(bn, r0, pair(1.f, 1.f)), r0);
+  const f2 q = mul2(a, r);
+  return fma2(fma2(bn, q, a), r, q);
+}
+// Four moments: values of the format times their scale.
 __device__ __forceinline__ void decode4(uint32_t q, __nv_fp8_interpretation_t fmt, float scale, float (&x)[4]) {
   const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q & 0xffffu), fmt)));
   const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16), fmt)));
-  x[0] = __fmul_rn(a.x, scale); x[1] = __fmul_rn(a.y, scale); x[2] = __fmul_rn(b.x, scale); x[3] = __fmul_rn(b.y, scale);
+  const f2 s = pair(scale, scale);
+  split(mul2(pair(a.x, a.y), s), x[0], x[1]);
+  split(mul2(pair(b.x, b.y), s), x[2], x[3]);
 }
 
 // One warp's UNROLL blocks of a chunk.  FULL: the chunk lies wholly inside its tensor.
@@ -102,7 +145,8 @@ template <bool G_BF16, bool FULL>
 __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8Scalars& sc, unsigned long long blk0, int lane) {
   constexpr int WARPS = THREADS / 32, NEXT = WARPS * QB;           // blocks, elements from one of the warp's blocks to its next
   const float omb1 = __fsub_rn(1.f, sc.b1), omb2 = __fsub_rn(1.f, sc.b2);
-  const float lrwd = sc.lr * t.wd, lrc1 = sc.lr * sc.inv_bc1;
+  const float lrwd = __fmul_rn(sc.lr, t.wd);
+  auto both = [](float x) { return pair(x, x); };
   const unsigned long long e0 = blk0 * QB + 4 * lane;
   float* const wp = t.w + e0;
   uint8_t* const mp = t.m + e0;
@@ -157,18 +201,24 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
     for (int j = 0; j < 4; ++j) {
       m[j] = __fadd_rn(__fmul_rn(sc.b1, m[j]), __fmul_rn(omb1, g[u][j]));
       v[j] = __fadd_rn(__fmul_rn(sc.b2, v[j]), __fmul_rn(__fmul_rn(omb2, g[u][j]), g[u][j]));
-      const float den = sqrt_fast(v[j] * sc.inv_bc2) + sc.eps;
-      w[u][j] = fmaf(-lrwd, w[u][j], w[u][j]);
-      w[u][j] = fmaf(-(m[j] * lrc1), rcp_fast(den), w[u][j]);
+    }
+    f2 upd[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const f2 den = add2(sqrt2(mul2(pair(v[2 * k], v[2 * k + 1]), both(sc.inv_bc2))), both(sc.eps));
+      upd[k] = div2(mul2(both(sc.lr), mul2(pair(m[2 * k], m[2 * k + 1]), both(sc.inv_bc1))), den);
     }
     uint32_t am = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(m[0]) & 0x7fffffffu, __float_as_uint(m[1]) & 0x7fffffffu,
                                                       __float_as_uint(m[2]) & 0x7fffffffu, __float_as_uint(m[3]) & 0x7fffffffu));
     uint32_t av = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
     uint32_t bad_m = 0u, bad_v = 0u;                 // bytes that become NaN
-    if (max(am, av) >= 0x7f800000u) {                // the whole warp: leave them out of the maxima
+    if (max(am, av) >= 0x6f800000u) {                // from 2^96 on, the whole warp: the update by the functions that take any
+      float d[4];                                    // number, and what is not finite left out of the maxima
       am = av = 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[j], sc.inv_bc2)), sc.eps);
+        d[j] = __fdiv_rn(__fmul_rn(sc.lr, __fmul_rn(m[j], sc.inv_bc1)), den);
         if (finite(m[j])) am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
         else { bad_m |= (m[j] < 0.f ? 0xffu : 0x7fu) << (8 * j); m[j] = 0.f; }
         if (finite(v[j])) av = max(av, __float_as_uint(v[j]));
@@ -176,6 +226,14 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
       }
       am = __reduce_max_sync(0xffffffffu, am);
       av = __reduce_max_sync(0xffffffffu, av);
+      upd[0] = pair(d[0], d[1]); upd[1] = pair(d[2], d[3]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float d0, d1;
+      split(upd[k], d0, d1);
+      w[u][2 * k] = __fsub_rn(__fsub_rn(w[u][2 * k], __fmul_rn(lrwd, w[u][2 * k])), d0);
+      w[u][2 * k + 1] = __fsub_rn(__fsub_rn(w[u][2 * k + 1], __fmul_rn(lrwd, w[u][2 * k + 1])), d1);
     }
     const int fm = scale_field<8>(am), fv = scale_field<15>(av);
     // moment times 2^(127 - field), then 2^-120 or 2^-112: one factor unless it is below 2^-126 itself
@@ -231,7 +289,7 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
 }
 
 template <bool G_BF16>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 8)
 adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
   fax_grid_dependency_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -291,7 +349,8 @@ extern "C" fax_status fax_adamw8_step(fax_ctx* ctx, const fax_adamw8_tensor* ten
     if (k == 0) continue;                                    // only empty tensors were left
     batch.n_tensors = k;
     batch.total_chunks = (unsigned int)chunks;
-    const unsigned long long cap = (unsigned long long)ctx->sm_count * 16;
+    // a dozen and more rounds of blocks even the SMs out (201M elements: 642 us with two rounds, 615 us with 16, 640 us a chunk a block)
+    const unsigned long long cap = (unsigned long long)ctx->sm_count * 128;
     const unsigned int grid = (unsigned int)(chunks < cap ? chunks : cap);
     if (hp->grad_is_bf16) fax_launch(ctx, adamw8_kernel<true>, dim3(grid), dim3(THREADS), 0, batch, sc);
     else fax_launch(ctx, adamw8_kernel<false>, dim3(grid), dim3(THREADS), 0, batch, sc);

@@ -605,14 +605,14 @@ constexpr int FIXED_SMEM = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + NUM_EPI_WARP
 int split_bytes(int splits, int M, int bn) { return (splits - 1) * (M < 128 ? (M + 31) / 32 : 4) * (bn / 32) * 4096; }
 
 // Time of a tile shape in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's end),
-// the paces as measured with all SMs busy.  A pair of SMs loads each operand byte for twice the work and runs best
+// the paces as measured with all SMs busy, with one sum over K and with sums of 512 k.  A pair of SMs loads each operand byte for twice the work and runs best
 // where there are tiles for all pairs; a narrower tile has about the pace of the 128-column one (the issue of
 // its MMAs bounds it), so it pays only where it brings more SMs to work.  Where the tiles leave SMs idle, slices of K
 // bring them in, for the price of the exchange.
 struct TileChoice { int cg, bn, splits; };
 TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
-  struct Shape { int cg, bn; double pace, end; };
-  static const Shape shapes[] = {{2, 256, 0.40, 1.5}, {2, 192, 0.33, 1.3}, {1, 256, 0.42, 1.2}, {1, 128, 0.31, 0.8}, {1, 64, 0.29, 0.6}};
+  struct Shape { int cg, bn; double pace, pace_sums, end; };
+  static const Shape shapes[] = {{2, 256, 0.41, 0.54, 1.5}, {2, 192, 0.38, 0.45, 1.3}, {1, 256, 0.45, 0.56, 1.2}, {1, 128, 0.31, 0.40, 0.8}, {1, 64, 0.29, 0.36, 0.6}};
   constexpr double EXCHANGE = 1.5;
   const int kb = (K + BK - 1) / BK;
   TileChoice best = {2, 256, 1};
@@ -620,7 +620,7 @@ TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
   for (const Shape& s : shapes) {
     const double tiles = (double)((M + s.cg * BM - 1) / (s.cg * BM)) * ((N + s.bn - 1) / s.bn);
     const double waves = (double)(long long)((tiles + ctx->sm_count / s.cg - 1) / (ctx->sm_count / s.cg));
-    const double pace = s.pace + (sums && s.bn == 256 ? 0.09 : 0.0);        // the accumulators share columns: a pause per segment
+    const double pace = sums ? s.pace_sums : s.pace;
     const double t = waves * (kb * pace + s.end) + (s.cg == 2 ? 0.5 : 0.0);
     if (t < least) { least = t; best = {s.cg, s.bn, 1}; }
     if (s.cg != 1 || s.bn > 32 * 2 * SPLIT_CHUNKS) continue;
@@ -628,7 +628,7 @@ TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
       const int per = (kb + splits - 1) / splits;
       if (per < 2 || (kb + per - 1) / per != splits || tiles * splits > ctx->sm_count) continue;
       if (SMEM_MAX - FIXED_SMEM - split_bytes(splits, M, s.bn) < 4 * (BM + s.bn) * BK) continue;
-      const double ts = per * s.pace + s.end + EXCHANGE;
+      const double ts = per * s.pace_sums + s.end + EXCHANGE;
       if (ts < least) { least = ts; best = {1, s.bn, splits}; }
     }
   }
