@@ -29,7 +29,7 @@
 // float32 moments.  A warp takes one block of 128 elements at a time, four elements a lane, so that a block's
 // maximum is one warp reduction (redux) and every access is a full 32-byte sector or more.  Moments that are
 // not finite are looked for once a block (their bits are the largest), not element by element.  201M elements: 615 us,
-// 5.9 TB/s, 84 instructions an element; 900 us with every check and IEEE operation an element of its own.
+// 5.9 TB/s (in a run of a second 670 us), some 80 instructions an element; 900 us with every check and IEEE operation an element of its own.
 #include "common.cuh"
 
 #include <cuda_fp8.h>
@@ -74,15 +74,21 @@ __device__ __forceinline__ uint32_t sr_e4m3(float y, uint32_t h) {
   const uint32_t t = __float_as_uint(y) + ((h >> 12) & 0xffff0u) + 8u;
   return (t & 0x80000000u) | ((t << 4) & 0x7f000000u);
 }
-__device__ __forceinline__ uint32_t sr_e5m2(float y, bool above_zero, uint32_t h) {
-  const uint32_t t = __float_as_uint(y) + ((h & 0xffffu) << 5) + 16u;
-  return max(t, above_zero ? 1u << 21 : 0u) << 3;
+__device__ __forceinline__ uint32_t sr_e5m2(float y, uint32_t h) {
+  return (__float_as_uint(y) + ((h & 0xffffu) << 5) + 16u) << 3;
 }
 __device__ __forceinline__ uint32_t top_bytes(const uint32_t (&c)[4]) {
   return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
 __device__ __forceinline__ uint32_t max4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return max(__vimax3_u32(a, b, c), d); }
+// Bits of the largest magnitude; a NaN stays.
+__device__ __forceinline__ uint32_t max4_abs(float a, float b, float c, float d) {
+  float m;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(d), "f"(d));
+  return __float_as_uint(m) & 0x7fffffffu;
+}
 
 // Two float32 in one register pair; one instruction for both.
 typedef unsigned long long f2;
@@ -208,8 +214,7 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
       const f2 den = add2(sqrt2(mul2(pair(v[2 * k], v[2 * k + 1]), both(sc.inv_bc2))), both(sc.eps));
       upd[k] = div2(mul2(both(sc.lr), mul2(pair(m[2 * k], m[2 * k + 1]), both(sc.inv_bc1))), den);
     }
-    uint32_t am = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(m[0]) & 0x7fffffffu, __float_as_uint(m[1]) & 0x7fffffffu,
-                                                      __float_as_uint(m[2]) & 0x7fffffffu, __float_as_uint(m[3]) & 0x7fffffffu));
+    uint32_t am = __reduce_max_sync(0xffffffffu, max4_abs(m[0], m[1], m[2], m[3]));
     uint32_t av = __reduce_max_sync(0xffffffffu, max4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
     uint32_t bad_m = 0u, bad_v = 0u;                 // bytes that become NaN
     if (max(am, av) >= 0x6f800000u) {                // from 2^96 on, the whole warp: the update by the functions that take any
@@ -261,7 +266,13 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
       h = (h ^ (h >> 15)) * 0x846ca68bu;
       h ^= h >> 16;
       cm[j] = sr_e4m3(ym[j], h);
-      cv[j] = sr_e5m2(yv[j], v[j] > 0.f, h);
+      cv[j] = sr_e5m2(yv[j], h);
+    }
+    // a v above zero keeps at least its format's smallest value; looked at only where some code came out as 0
+    if (__any_sync(0xffffffffu, min(min(cv[0], cv[1]), min(cv[2], cv[3])) < (1u << 24))) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (v[j] > 0.f) cv[j] = max(cv[j], 1u << 24);
     }
     const uint32_t qm = top_bytes(cm) | bad_m, qv = top_bytes(cv) | bad_v;
     const int in = inside(u);
