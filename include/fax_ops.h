@@ -120,9 +120,9 @@ fax_status fax_op_embedding_forward(fax_ctx* ctx, int32_t prec, int32_t n_tokens
  * dout[i, :]  (accumulate != 0: added to what dtable holds, e.g. the output
  * head's gradient of a tied table).  dout [n_tokens, d] T; dtable [vocab, d]
  * float: overwritten in full, or with accumulate != 0 changed only in rows
- * that a token touches.  Tokens with an id outside [0, vocab) add nothing.  The
- * tokens are sorted by id first and each row is summed in float32 in a fixed
- * order: the same inputs give the same bits (an accumulated row gets its sum in
+ * that a token touches.  Tokens with an id outside [0, vocab) add nothing.  Each
+ * row is summed over its tokens in float32 in a fixed order (long batches are
+ * sorted by id first, short ones are not): the same inputs give the same bits (an accumulated row gets its sum in
  * one addition per element).  Concurrent calls, and graphs that may be replayed at
  * the same time, need scratch of their own.  n_tokens <= 2^30; scratch 256-byte aligned. */
 fax_status fax_op_embedding_backward_scratch_bytes(int32_t n_tokens, int32_t vocab, int32_t d, size_t* bytes);

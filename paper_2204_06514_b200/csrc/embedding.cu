@@ -3,8 +3,16 @@
 //   forward   out[i] = scale * table[ids[i]]                     (a zero row where ids[i] is outside the table)
 //   backward  dtable[v] (+)= scale * sum_{i : ids[i] = v} dout[i]
 //
-// The gradient's sums run over tokens sorted by id, in the order in which the tokens stand: every row of
+// The gradient's sums run over tokens grouped by id, in the order in which the tokens stand: every row of
 // the table is written once, nothing is added by float atomics, and the same call gives the same bits.
+//
+// Small batches (DIRECT_TOKENS) need no sort: a block per token looks through all ids; the first token of its id
+// sums the rows of those that are alike.  One launch instead of five, bound by its latency; back to back, accumulated:
+// 64 tokens x 256 7.6 us against 15-20 by the sort, 256 x 768 6.4 against 16.  512 tokens of one id x 1,024 (the
+// longest list, bf16): 9.4 against 13.2; at 1,024 tokens of one id the sort is ahead (13.2 against 15.9), and so it is
+// from about 2,000 blocks (1,000 different ids x 1,024: 16.8 against 18.4), whence the two limits.
+//
+// Larger ones:
 //
 //  1. A least-significant-digit radix sort of the ids (8 bits a pass at most, as many passes as the
 //     vocabulary needs: two for 50,304 ids).  embed_sort_count zeroes the counters and counts the first
@@ -33,6 +41,11 @@ constexpr int TILE_UNIT = 512;         // tokens per tile: a multiple of this
 constexpr int MAX_TILES = 256;         // a scatter block reads every tile's counts of its pass
 constexpr int MAX_TOKENS = 1 << 30;    // token and tile positions stay within 32 bits
 constexpr int GRAD_THREADS = 128;
+constexpr int DIRECT_THREADS = 512;
+constexpr int DIRECT_TOKENS = DIRECT_THREADS;   // one id a thread
+constexpr int DIRECT_BLOCKS = 1024;    // tokens times slices of columns: each block looks through all ids
+constexpr int DIRECT_LANES = 64;       // of a group: the other groups share a long list
+constexpr int DIRECT_ROWS = 32;        // table rows that a zeroing block looks up at a time
 constexpr int JOIN_WARPS = 8;
 constexpr int JOIN_SHORT = 8;          // a run over at most this many further chunks is joined by one warp per 128 columns
 // Rows of a batch that may be written twice for the zeros to run under the sort: at HBM rate about what the sort takes.
@@ -253,6 +266,100 @@ __device__ __forceinline__ void put4(float* o, float a, float b, float c, float 
   else *reinterpret_cast<float4*>(o) = make_float4(a, b, c, d);
 }
 
+// Small batches: blocks (token, slice of lanes * V columns), then blocks that zero the rows no token touches.
+template <typename T, int V>
+__global__ void __launch_bounds__(DIRECT_THREADS)
+embed_direct_kernel(int n, int vocab, int d, int nvec, int lanes, int slices, unsigned int work_blocks, const int32_t* __restrict__ ids,
+                    const T* __restrict__ dout, float scale, int accumulate, float* __restrict__ dtable) {
+  typedef typename Vec<T, V>::type vec;
+  constexpr int WARPS = DIRECT_THREADS / 32;
+  __shared__ uint32_t list[DIRECT_TOKENS];
+  __shared__ int counts[WARPS];
+  __shared__ int hit[DIRECT_ROWS];
+  __shared__ float parts[DIRECT_THREADS * V];
+  fax_grid_dependency_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int i = threadIdx.x;                                         // this thread's token
+  const uint32_t mine = i < n ? key_of(ids[i], vocab) : (uint32_t)vocab;
+  if (blockIdx.x >= work_blocks) {
+    for (long long v0 = (long long)(blockIdx.x - work_blocks) * DIRECT_ROWS; v0 < vocab; v0 += (long long)(gridDim.x - work_blocks) * DIRECT_ROWS) {
+      if (threadIdx.x < DIRECT_ROWS) hit[threadIdx.x] = 0;
+      __syncthreads();
+      const long long r0 = (long long)mine - v0;
+      if (mine < (uint32_t)vocab && r0 >= 0 && r0 < DIRECT_ROWS) hit[r0] = 1;
+      __syncthreads();
+      for (int r = warp; r < DIRECT_ROWS && v0 + r < vocab; r += WARPS) {
+        if (hit[r]) continue;
+        float* row = dtable + (size_t)(v0 + r) * d;
+        if (V > 1) for (int c = lane; c < d / 4; c += 32) reinterpret_cast<float4*>(row)[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        else for (int c = lane; c < d; c += 32) row[c] = 0.f;
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  const int token = blockIdx.x / slices, slice = blockIdx.x - token * slices;
+  const uint32_t key = key_of(ids[token], vocab);
+  if (key >= (uint32_t)vocab) return;                                // the whole block
+  const bool match = mine == key;
+  if (__syncthreads_or(match && i < token)) return;                  // an earlier token has this id
+  // the tokens that are alike, in their order
+  const uint32_t alike = __ballot_sync(0xffffffffu, match);
+  if (lane == 0) counts[warp] = __popc(alike);
+  __syncthreads();
+  int at = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    at += w < warp ? counts[w] : 0;
+    total += counts[w];
+  }
+  if (match) list[at + __popc(alike & ((1u << lane) - 1u))] = (uint32_t)i;
+  __syncthreads();
+  // one group of lanes sums a short list; a longer one is cut into equal parts, whose sums are added in order
+  const int groups = DIRECT_THREADS / lanes, group = threadIdx.x / lanes, c = slice * lanes + (threadIdx.x & (lanes - 1));
+  const int used = total > 8 ? groups : 1, share = (total + used - 1) / used;
+  const int r0 = group * share, r1 = group < used ? min(total, r0 + share) : r0;
+  float acc[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) acc[j] = 0.f;
+  if (c < nvec) {
+    const vec* src = reinterpret_cast<const vec*>(dout) + c;
+    constexpr int U = 8;
+    for (int q = r0; q < r1; q += U) {
+      vec x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (q + u < r1) x[u] = src[(size_t)list[q + u] * nvec];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (q + u < r1) {
+          float f[V];
+          widen<T, V>(x[u], f);
+#pragma unroll
+          for (int j = 0; j < V; ++j) acc[j] += f[j];
+        }
+    }
+  }
+  if (used > 1) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) parts[j * DIRECT_THREADS + threadIdx.x] = acc[j];
+    __syncthreads();
+    if (group == 0)
+      for (int g = 1; g < used; ++g)
+#pragma unroll
+        for (int j = 0; j < V; ++j) acc[j] += parts[j * DIRECT_THREADS + g * lanes + threadIdx.x];
+  }
+  if (group == 0 && c < nvec) {
+    float* o = dtable + (size_t)key * d + (size_t)c * V;
+    if (V > 1) {
+#pragma unroll
+      for (int j = 0; j < V; j += 4) put4(o + j, scale * acc[j], scale * acc[j + 1], scale * acc[j + 2], scale * acc[j + 3], accumulate);
+    } else {
+      if (accumulate) atomicAdd(o, scale * acc[0]); else o[0] = scale * acc[0];
+    }
+  }
+}
+
 // `lanes` lanes (32, 64 or 128) work on one chunk and one slice of lanes * V columns.  A warp holds 32 sorted tokens at a
 // time, one a lane; where runs begin is one ballot, and rows are loaded U at a time whatever runs they belong to.
 template <typename T, int V>
@@ -427,13 +534,33 @@ embed_join_kernel(SortPlan p, int d, const uint2* __restrict__ sorted, const flo
   }
 }
 
+// Lanes of a group and slices of columns: one vector a lane, 32 to `most` lanes.
+void lanes_for(int nvec, int most, int* lanes, int* slices) {
+  *lanes = 32;
+  while (*lanes < nvec && *lanes < most) *lanes *= 2;
+  *slices = (nvec + *lanes - 1) / *lanes;
+}
+
+template <typename T, int V>
+fax_status launch_direct(fax_ctx* ctx, int n, int vocab, int d, int lanes, const int32_t* ids, const void* dout, float scale, int accumulate, float* dtable) {
+  const int nvec = d / V, slices = (nvec + lanes - 1) / lanes;
+  long long zb = 0;
+  if (!accumulate) {
+    zb = ((long long)vocab + DIRECT_ROWS - 1) / DIRECT_ROWS;
+    if (zb > (long long)ctx->sm_count * 4) zb = (long long)ctx->sm_count * 4;
+  }
+  fax_launch(ctx, embed_direct_kernel<T, V>, dim3((unsigned int)(n * slices + zb)), dim3(DIRECT_THREADS), 0, n, vocab, d, nvec, lanes, slices,
+             (unsigned int)(n * slices), ids, (const T*)dout, scale, accumulate, dtable);
+  return fax_after_launch(ctx);
+}
+
 template <typename T, int V>
 fax_status launch_grad(fax_ctx* ctx, const SortPlan& p, int vocab, int d, const uint2* sorted, const void* dout, float scale,
                        int accumulate, bool fill_here, float* dtable, const EmbedScratch& s) {
   const int nvec = d / V;
-  int lanes = 32;
-  while (lanes < nvec && lanes < GRAD_THREADS) lanes *= 2;
-  const int slices = (nvec + lanes - 1) / lanes, groups = GRAD_THREADS / lanes;
+  int lanes, slices;
+  lanes_for(nvec, GRAD_THREADS, &lanes, &slices);
+  const int groups = GRAD_THREADS / lanes;
   const long long items = (long long)p.chunks * slices, gb = (items + groups - 1) / groups;
   long long zb = 0;
   if (fill_here) {
@@ -487,11 +614,27 @@ fax_status fax_embedding_grad(fax_ctx* ctx, int prec, int n, int vocab, int d, c
     return FAX_OK;
   }
   FaxProfScope prof(ctx, KC_EMBED, 0.0, (double)n * d * fax_elem_size(prec) + (accumulate ? 0.0 : 4.0 * vocab * (double)d));
+  const bool wide = fax_aligned(dout, 16) && fax_aligned(dtable, 16);
+  {
+    // The route and the cut of a list into parts follow d and the type, never the alignment: the sums' order, and so
+    // their bits, are those of aligned buffers.
+    const int v = prec == FAX_PREC_BF16 ? (d % 8 == 0 ? 8 : 1) : (d % 4 == 0 ? 4 : 1);
+    int lanes, slices;
+    lanes_for(d / v, DIRECT_LANES, &lanes, &slices);
+    if (n <= DIRECT_TOKENS && (long long)n * slices <= DIRECT_BLOCKS) {
+      const int acc = accumulate ? 1 : 0;
+      const bool vec = wide && v > 1;
+      if (prec == FAX_PREC_BF16)
+        return vec ? launch_direct<bf16, 8>(ctx, n, vocab, d, lanes, ids, dout, scale, acc, dtable)
+                   : launch_direct<bf16, 1>(ctx, n, vocab, d, lanes, ids, dout, scale, acc, dtable);
+      return vec ? launch_direct<float, 4>(ctx, n, vocab, d, lanes, ids, dout, scale, acc, dtable)
+                 : launch_direct<float, 1>(ctx, n, vocab, d, lanes, ids, dout, scale, acc, dtable);
+    }
+  }
   const SortPlan p = plan_for(n, vocab);
   FaxArena ar(scratch, scratch_bytes);
   EmbedScratch s;
   carve(ar, p, vocab, d, &s);
-  const bool wide = fax_aligned(dout, 16) && fax_aligned(dtable, 16);
   const double rows = n < vocab ? n : vocab;
   const bool prefill = !accumulate && fax_aligned(dtable, 16) && ((size_t)vocab * d) % 4 == 0 && rows * d * 4.0 <= PREFILL_BYTES;
   const bool mark = !accumulate && !prefill;

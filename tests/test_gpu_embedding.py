@@ -64,7 +64,8 @@ def test_lookup(sess, prec, n, vocab, d, kind):
 
 
 SHAPES = [(1, 1, 1), (1, 9, 64), (5, 2, 7), (31, 31, 8), (32, 400, 16), (33, 7, 1000), (511, 100, 24), (513, 255, 520), (513, 256, 40),
-          (1000, 65535, 64), (1025, 65536, 8), (4099, 300, 96), (3000, 70000, 33)]
+          (1000, 65535, 64), (1025, 65536, 8), (4099, 300, 96), (3000, 70000, 33),
+          (512, 1, 1024), (512, 40000, 520), (513, 9, 256), (512, 70, 519), (37, 3000, 1032), (300, 1, 513), (512, 33, 2), (1024, 5, 256), (1024, 40000, 1032), (700, 90, 513), (1037, 1, 40), (2048, 255, 24), (5000, 7, 1), (1700, 256, 2056), (1100, 3000, 1025)]
 
 
 @pytest.mark.parametrize("prec", [0, 1])
@@ -110,7 +111,11 @@ def test_gradient_of_long_batches(sess, n, vocab, d):
 def test_gradient_is_the_same_bits_and_order(sess):
     """Twice the same call: the same bits, also with the scratch as another call left it, and for unaligned buffers."""
     rng = np.random.default_rng(3)
-    n, vocab, d = 6000, 50, 72
+    for n, vocab, d in ((6000, 50, 72), (900, 20, 72), (500, 20, 72), (512, 3, 1024), (100, 2, 4100), (300, 40, 33)):
+        same_bits(sess, rng, n, vocab, d)
+
+
+def same_bits(sess, rng, n, vocab, d):
     i = torch.as_tensor(ids_for("zipf", n, vocab, rng)).to(sess.device)
     g = torch.as_tensor((rng.standard_normal((n, d)) * 10.0 ** rng.uniform(-4, 4, (n, 1))).astype(np.float32)).to(sess.device)
     a, b = torch.empty((vocab, d), device=sess.device), torch.empty((vocab, d), device=sess.device)
@@ -127,7 +132,11 @@ def test_gradient_is_the_same_bits_and_order(sess):
 def test_gradient_replayed_from_a_graph(sess):
     """Captured with its launches and replayed on other ids: nothing is kept from the first run."""
     rng = np.random.default_rng(5)
-    n, vocab, d = 700, 90, 48
+    for n in (700, 1500, 300):
+        replayed(sess, rng, n, 90, 48)
+
+
+def replayed(sess, rng, n, vocab, d):
     st = torch.cuda.Stream(sess.device)
     with torch.cuda.stream(st):
         s2 = Session(0)
