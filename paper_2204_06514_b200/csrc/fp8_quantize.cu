@@ -149,7 +149,7 @@ __device__ __forceinline__ uint32_t quantize_rows(const QuantParams& p, const ui
         for (int e = 0; e < 4; ++e) y[e] = W::value(v[i][(4 * j + e) / W::N], e % W::N) * inv;
         o[j] = code4<FMT, BAD>(y[0], y[1], y[2], y[3]);
       }
-      if (c + 16 <= p.cols) {
+      if (c <= p.cols - 16) {                          // c + 16 may pass 32 bits
         *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
       } else {
 #pragma unroll
@@ -207,7 +207,7 @@ __device__ __forceinline__ void quantize_columns(const QuantParams& p, uint4* ti
     if (c >= p.cols) continue;
     const uint4 u = tile_raw[col * 8 + (unit ^ ((col / W::N) & 7))];
     uint8_t* dst = p.qt + (size_t)c * p.ldqt + r;
-    if (r + 16 <= p.rows) {
+    if (r <= p.rows - 16) {
       *reinterpret_cast<uint4*>(dst) = u;
     } else {
       const uint32_t x[4] = {u.x, u.y, u.z, u.w};
@@ -237,7 +237,7 @@ fp8_quantize_kernel(const QuantParams p) {
   for (int i = 0; i < PASSES<T>; ++i) {
     const int r = r0 + ROW_STEP<T> * i;
     const T* src = (const T*)p.x + (size_t)r * p.ldx + c;
-    if (VEC && r < p.rows && c + 16 <= p.cols) {
+    if (VEC && r < p.rows && c <= p.cols - 16) {
 #pragma unroll
       for (int j = 0; j < RW<T>; j += 4) {
         const uint4 u = __ldg(reinterpret_cast<const uint4*>(src) + j / 4);

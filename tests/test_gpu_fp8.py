@@ -253,3 +253,30 @@ def test_quantize_and_product_in_a_graph(sess):
             del graph
         finally:
             s2.close()
+
+
+@pytest.mark.parametrize("tall", [0, 1])
+def test_quantize_of_the_longest_rows(sess, tall):
+    """2^31 - 1 columns (rows for the transposed output): the last vector is cut, and positions pass 32 bits."""
+    big, tail = 2 ** 31 - 1, 400
+    dev = sess.device
+    if torch.cuda.mem_get_info(dev)[0] < 40 * 2 ** 30:
+        pytest.skip("too little device memory is free")
+    x = torch.zeros(big + 25, dtype=torch.bfloat16, device=dev)
+    end = torch.as_tensor(values(1, tail, np.random.default_rng(1))[0]).to(torch.bfloat16)
+    x[big - tail:big] = end.to(dev)
+    x[big:] = float("inf")                                           # not part of the matrix
+    q = torch.full((big + 1,), 0x55, dtype=torch.uint8, device=dev)
+    s = torch.full((2 ** 24 + 1,), 7.0, device=dev)
+    wide = (ptr(q), big + 1, ptr(s), 1)
+    none = (None, 0, None, 0)
+    if tall:
+        d = ops.Fp8QuantizeDesc(big, 1, ptr(x), 1, 0, 1, *none, *wide)
+    else:
+        d = ops.Fp8QuantizeDesc(1, big, ptr(x), big + 9, 0, 1, *wide, *none)
+    ops.fax_op_fp8_quantize(sess.ctx, 0, d)
+    lead = 128 - (big - tail) % 128                                  # the tail's first element stands inside a block
+    want, ws = ref.quantize(np.concatenate([np.zeros(128 - lead), end.double().numpy()])[None], 0, 1)
+    got = host(q[big - tail - (128 - lead):big].view(ref.TORCH8[0]))
+    assert np.array_equal(got, want[0]) and np.array_equal(host(s[2 ** 24 - ws.shape[0]:2 ** 24]), ws[:, 0])
+    assert int(q[big]) == 0x55 and float(s[2 ** 24]) == 7 and not bool(q[:big - tail].any()) and bool((s[:2 ** 24 - ws.shape[0]] == 1).all())
