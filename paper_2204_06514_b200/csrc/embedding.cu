@@ -40,6 +40,7 @@ constexpr int DIGITS = 256;
 constexpr int TILE_UNIT = 512;         // tokens per tile: a multiple of this
 constexpr int MAX_TILES = 256;         // a scatter block reads every tile's counts of its pass
 constexpr int MAX_TOKENS = 1 << 30;    // token and tile positions stay within 32 bits
+constexpr int MAX_WIDTH = 1 << 30;     // so do columns
 constexpr int GRAD_THREADS = 128;
 constexpr int DIRECT_THREADS = 512;
 constexpr int DIRECT_TOKENS = DIRECT_THREADS;   // one id a thread
@@ -585,7 +586,7 @@ fax_status launch_lookup(fax_ctx* ctx, int n, int vocab, int d, const int32_t* i
 fax_status embed_args(int32_t prec, int32_t n, int32_t vocab, int32_t d) {
   if (prec != FAX_PREC_BF16 && prec != FAX_PREC_FP32_VALIDATE) return FAX_ERR_INVALID_ARG;
   if (n < 0 || vocab <= 0 || d <= 0) return FAX_ERR_INVALID_ARG;
-  if (n > MAX_TOKENS) return FAX_ERR_UNSUPPORTED_SHAPE;
+  if (n > MAX_TOKENS || d > MAX_WIDTH) return FAX_ERR_UNSUPPORTED_SHAPE;
   return FAX_OK;
 }
 

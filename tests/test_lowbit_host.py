@@ -131,3 +131,12 @@ def test_reference_moments():
         t = np.repeat(s, 128)[:1000]
         assert np.all(np.abs(low) <= np.abs(high)) and np.all(np.abs(low * t - y) <= ref.step_at(y / t, fmt) * t * (1 + 1e-6))
         assert np.array_equal(torch.as_tensor(low).to(ref.TORCH8[fmt]).double().numpy(), low)
+
+
+def test_embedding_refuses_rows_past_its_positions(lib, ctx):
+    nb = C.c_size_t()
+    for d in ((1 << 30) + 1, 0x7fffffff):
+        assert lib.fax_op_embedding_forward(ctx, 0, 1, 2, d, P, P, 1.0, P) == SHAPE
+        assert lib.fax_op_embedding_backward_scratch_bytes(1, 2, d, C.byref(nb)) == SHAPE
+        assert lib.fax_op_embedding_backward(ctx, 0, 1, 2, d, P, P, 1.0, 0, P, P, 1 << 40) == SHAPE
+    assert lib.fax_op_embedding_backward_scratch_bytes(1, 2, 1 << 30, C.byref(nb)) == 0
