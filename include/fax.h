@@ -205,7 +205,8 @@ fax_status fax_adamw_step(fax_ctx* ctx, const fax_adamw_tensor* tensors, int32_t
  *   h(x): x ^= x>>16; x *= 0x7FEB352D; x ^= x>>15; x *= 0x846CA68B; x ^= x>>16:
  * a step is the same bits wherever the tensor stands in a call.  Give tensors
  * different seeds.  w and g are 16-byte, w_compute 8-byte, m, v and the scales
- * 4-byte aligned; a tensor with n = 0 is skipped. */
+ * 4-byte aligned; a tensor with n = 0 is skipped.  Tensors of a call share no
+ * buffer but g; the same w twice is refused. */
 #define FAX_ADAMW8_BLOCK 128
 typedef struct {
   float* w;

@@ -34,6 +34,9 @@
 
 #include <cuda_fp8.h>
 
+#include <algorithm>
+#include <cstdlib>
+
 namespace {
 
 constexpr int QB = FAX_ADAMW8_BLOCK;   // elements per scale
@@ -317,6 +320,20 @@ adamw8_kernel(const __grid_constant__ Adam8Batch batch, Adam8Scalars sc) {
   }
 }
 
+// Do two tensors update the same weights?  Their blocks would race.
+fax_status check_distinct(const fax_adamw8_tensor* tensors, int n) {
+  const float* few[MAX_T];
+  const float** w = n <= MAX_T ? few : (const float**)malloc((size_t)n * sizeof(*w));
+  if (!w) return FAX_ERR_WORKSPACE_TOO_SMALL;          // host memory
+  int k = 0;
+  for (int i = 0; i < n; ++i)
+    if (tensors[i].n) w[k++] = tensors[i].w;
+  std::sort(w, w + k);
+  const bool twice = std::adjacent_find(w, w + k) != w + k;
+  if (w != few) free(w);
+  return twice ? FAX_ERR_INVALID_ARG : FAX_OK;
+}
+
 }  // namespace
 
 extern "C" fax_status fax_adamw8_step(fax_ctx* ctx, const fax_adamw8_tensor* tensors, int32_t n, const fax_adamw_hparams* hp) {
@@ -333,6 +350,7 @@ extern "C" fax_status fax_adamw8_step(fax_ctx* ctx, const fax_adamw8_tensor* ten
     if ((t.n + CHUNK - 1) / CHUNK > 0xffffffffull) return FAX_ERR_UNSUPPORTED_SHAPE;
     total += (double)t.n;
   }
+  FAX_TRY(check_distinct(tensors, n));
   Adam8Scalars sc;
   sc.lr = hp->lr; sc.b1 = hp->beta1; sc.b2 = hp->beta2; sc.eps = hp->eps;
   sc.inv_bc1 = (float)(1.0 / (1.0 - pow((double)hp->beta1, (double)hp->step)));

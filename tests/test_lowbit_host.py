@@ -140,3 +140,16 @@ def test_embedding_refuses_rows_past_its_positions(lib, ctx):
         assert lib.fax_op_embedding_backward_scratch_bytes(1, 2, d, C.byref(nb)) == SHAPE
         assert lib.fax_op_embedding_backward(ctx, 0, 1, 2, d, P, P, 1.0, 0, P, P, 1 << 40) == SHAPE
     assert lib.fax_op_embedding_backward_scratch_bytes(1, 2, 1 << 30, C.byref(nb)) == 0
+
+
+@pytest.mark.parametrize("n", [2, 40, 41, 300])
+def test_adamw8_refuses_the_same_weights_twice(lib, ctx, n):
+    from paper_2204_06514_b200 import binding as fx
+    t = [fx.Adamw8Tensor(P * (i + 1), P, P, P, P, P, None, 64, 0.0, 1) for i in range(n)]
+    t[-1].w = t[n // 2 - 1].w
+    arr = (fx.Adamw8Tensor * n)(*t)
+    hp = C.byref(fx.AdamwHparams(1e-3, 0.9, 0.95, 1e-8, 1, 0))
+    assert lib.fax_adamw8_step(ctx, arr, n, hp) == INV
+    for x in arr:                                                    # empty tensors share whatever they like
+        x.n = 0
+    assert lib.fax_adamw8_step(ctx, arr, n, hp) == 0
