@@ -252,7 +252,8 @@ fax_status fax_set_graph_replay(fax_ctx* ctx, int32_t enable);
 
 /* GEMMs whose M and N are multiples of 256 run on pairs of SMs (two-CTA
  * clusters, one 256 x 256 tile per pair); enable = 0 keeps every GEMM on the
- * one-CTA 128 x N kernel.  Same arithmetic either way.  Default: enabled. */
+ * one-CTA 128 x N kernel.  Same arithmetic either way (in an 8-bit product the
+ * choice of tiles may also cut K in other places).  Default: enabled. */
 fax_status fax_set_gemm_two_cta(fax_ctx* ctx, int32_t enable);
 
 /* Kernels are launched with programmatic dependent launch allowed: a kernel's

@@ -615,9 +615,10 @@ TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
   static const Shape shapes[] = {{2, 256, 0.41, 0.54, 1.5}, {2, 192, 0.38, 0.45, 1.3}, {1, 256, 0.45, 0.56, 1.2}, {1, 128, 0.31, 0.40, 0.8}, {1, 64, 0.29, 0.36, 0.6}};
   constexpr double EXCHANGE = 1.5;
   const int kb = (K + BK - 1) / BK;
-  TileChoice best = {2, 256, 1};
+  TileChoice best = {1, 256, 1};
   double least = 1e30;
   for (const Shape& s : shapes) {
+    if (s.cg == 2 && !ctx->use_2cta) continue;
     const double tiles = (double)((M + s.cg * BM - 1) / (s.cg * BM)) * ((N + s.bn - 1) / s.bn);
     const double waves = (double)(long long)((tiles + ctx->sm_count / s.cg - 1) / (ctx->sm_count / s.cg));
     const double pace = sums ? s.pace_sums : s.pace;

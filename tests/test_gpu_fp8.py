@@ -280,3 +280,14 @@ def test_quantize_of_the_longest_rows(sess, tall):
     got = host(q[big - tail - (128 - lead):big].view(ref.TORCH8[0]))
     assert np.array_equal(got, want[0]) and np.array_equal(host(s[2 ** 24 - ws.shape[0]:2 ** 24]), ws[:, 0])
     assert int(q[big]) == 0x55 and float(s[2 ** 24]) == 7 and not bool(q[:big - tail].any()) and bool((s[:2 ** 24 - ws.shape[0]] == 1).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(300, 260, 600), (256, 512, 128), (5100, 1300, 200)])
+@pytest.mark.parametrize("f32,acc,bias", [(0, 0, 1), (1, 1, 0)])
+def test_product_on_single_sms(sess, m, n, k, f32, acc, bias):
+    """With pairs of SMs switched off."""
+    fx.fax_set_gemm_two_cta(sess.ctx, False)
+    try:
+        product(sess, m, n, k, 0, 0, 128, f32, acc, bias, np.random.default_rng(m))
+    finally:
+        fx.fax_set_gemm_two_cta(sess.ctx, True)
