@@ -222,20 +222,32 @@ __device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMa
   __syncwarp();
   const int rows = (int)(p.M - row0 < 32 ? p.M - row0 : 32);
   if (col + lane < p.N) {
+    // Eight rows at a time: their words leave shared memory together.  A product that is added is added at L2 too, one
+    // addition an element (1891 x 7069 x 1283: 37 us; 65 us where each lane read C, added and wrote; with N = 7072,
+    // through the tensor map, 36 us).
+    auto each = [&](auto put) {
+      const float* src = stg + lane;
+      for (int i0 = 0; i0 < rows; i0 += 8, src += 8 * 33) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = src[i * 33];
+        if (rows - i0 >= 8) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) put(v[i] + bias);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i0 + i < rows) put(v[i] + bias);
+        }
+      }
+    };
     if (p.c_f32) {
       float* o = (float*)p.C + row0 * p.ldc + col + lane;
-      for (int i0 = 0; i0 < rows; i0 += 8) {
-        float old[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) old[i] = p.accumulate && i0 + i < rows ? o[(i0 + i) * p.ldc] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i0 + i < rows) o[(i0 + i) * p.ldc] = old[i] + (stg[(i0 + i) * 33 + lane] + bias);
-      }
+      if (p.accumulate) each([&](float x) { atomicAdd(o, x); o += p.ldc; });
+      else each([&](float x) { *o = x; o += p.ldc; });
     } else {
       bf16* o = (bf16*)p.C + row0 * p.ldc + col + lane;
-#pragma unroll 8
-      for (int i = 0; i < rows; ++i) o[i * p.ldc] = __float2bfloat16_rn(stg[i * 33 + lane] + bias);
+      each([&](float x) { *o = __float2bfloat16_rn(x); o += p.ldc; });
     }
   }
 }
