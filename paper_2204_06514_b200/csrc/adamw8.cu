@@ -116,13 +116,16 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-// sqrt(x) for x >= 2^-126: x is raised to that (a NaN stays): the approximation takes smaller numbers for zero.
-// s = x y, y ~ 1 / sqrt(x);  s + (x - s s) y / 2.
+// What a root is taken of: at least 2^-126 (a NaN stays), because the approximation takes smaller numbers for zero.
+__device__ __forceinline__ float root_arg(float x) {
+  asm("max.NaN.f32 %0, %0, 0f00800000;" : "+f"(x));
+  return x;
+}
+// sqrt(x) of the raised x: s = x y, y ~ 1 / sqrt(x);  s + (x - s s) y / 2.
 __device__ __forceinline__ f2 sqrt2(f2 x) {
   float a, b, ya, yb;
   split(x, a, b);
-  asm("max.NaN.f32 %0, %0, 0f00800000;" : "+f"(a));
-  asm("max.NaN.f32 %0, %0, 0f00800000;" : "+f"(b));
+  a = root_arg(a); b = root_arg(b);
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(a));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(b));
   const f2 c = pair(a, b), y = pair(ya, yb), minus = pair(-1.f, -1.f), half = pair(0.5f, 0.5f);
@@ -225,7 +228,7 @@ __device__ __forceinline__ void update_blocks(const Adam8Tensor& t, const Adam8S
       am = av = 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[j], sc.inv_bc2)), sc.eps);
+        const float den = __fadd_rn(__fsqrt_rn(root_arg(__fmul_rn(v[j], sc.inv_bc2))), sc.eps);
         d[j] = __fdiv_rn(__fmul_rn(sc.lr, __fmul_rn(m[j], sc.inv_bc1)), den);
         if (finite(m[j])) am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
         else { bad_m |= (m[j] < 0.f ? 0xffu : 0x7fu) << (8 * j); m[j] = 0.f; }
