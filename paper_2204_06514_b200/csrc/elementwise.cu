@@ -1,5 +1,5 @@
 // Element-wise GELU (tanh form), used when backward recomputes g = GELU(h) instead of reading a saved
-// copy: the same functions as the FC1 epilogues (hardware tanh on the bf16 path), so the recomputed
+// copy: the same functions as the FC1 epilogues (hardware exponential on the bf16 path), so the recomputed
 // values are the ones forward produced.
 #include "gemm_common.cuh"
 
