@@ -124,7 +124,8 @@ fax_status fax_op_embedding_forward(fax_ctx* ctx, int32_t prec, int32_t n_tokens
  * row is summed over its tokens in float32 in a fixed order (long batches are
  * sorted by id first, short ones are not): the same inputs give the same bits (an accumulated row gets its sum in
  * one addition per element).  Concurrent calls, and graphs that may be replayed at
- * the same time, need scratch of their own.  n_tokens and d <= 2^30; scratch 256-byte aligned. */
+ * the same time, need scratch of their own.  n_tokens and d <= 2^30; scratch 256-byte aligned.
+ * Scratch of the longest batch serves every shorter one: the bytes never shrink with n_tokens, vocab or d. */
 fax_status fax_op_embedding_backward_scratch_bytes(int32_t n_tokens, int32_t vocab, int32_t d, size_t* bytes);
 fax_status fax_op_embedding_backward(fax_ctx* ctx, int32_t prec, int32_t n_tokens, int32_t vocab, int32_t d,
                                      const int32_t* ids, const void* dout, float scale, int32_t accumulate,

@@ -56,6 +56,8 @@ struct SortPlan {
   int n, tile, tiles, passes, bits;    // bits per pass
   int chunk, chunks;                   // sorted tokens per gradient chunk
 };
+// Chunks of 16 sorted tokens keep the launch wide; longer ones for large batches keep the partial sums few.
+constexpr int CHUNK_LEAST = 16, CHUNK_MOST = 1024, CHUNKS = 1024;    // longer chunks are taken from CHUNKS of them on
 
 SortPlan plan_for(int n, int vocab) {
   SortPlan p;
@@ -67,10 +69,20 @@ SortPlan plan_for(int n, int vocab) {
   while (bits < 32 && ((uint32_t)vocab >> bits) != 0u) ++bits;      // keys 0 .. vocab (vocab: outside the table)
   p.passes = (bits + 7) / 8;
   p.bits = (bits + p.passes - 1) / p.passes;
-  // Chunks of 16 sorted tokens keep the launch wide; longer ones for large batches keep the partial sums few.
-  p.chunk = 16;
-  while (p.chunk < 1024 && (n + p.chunk - 1) / p.chunk > 1024) p.chunk *= 2;
+  p.chunk = CHUNK_LEAST;
+  while (p.chunk < CHUNK_MOST && (n + p.chunk - 1) / p.chunk > CHUNKS) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
+  return p;
+}
+
+// Tiles and chunks that no batch of up to n tokens exceeds: a longer tile or chunk makes fewer of them, and scratch sized
+// for a batch has to serve every shorter one.
+SortPlan most_for(int n, int vocab) {
+  SortPlan p = plan_for(n, vocab);
+  const int units = (n + TILE_UNIT - 1) / TILE_UNIT, least = (n + CHUNK_LEAST - 1) / CHUNK_LEAST;
+  p.tiles = units < MAX_TILES ? units : MAX_TILES;
+  const int at_least = least < CHUNKS ? least : CHUNKS;
+  if (p.chunks < at_least) p.chunks = at_least;
   return p;
 }
 
@@ -603,7 +615,7 @@ fax_status fax_embedding_lookup(fax_ctx* ctx, int prec, int n, int vocab, int d,
 size_t fax_embedding_grad_scratch_bytes(int n, int vocab, int d) {
   FaxArena ar(nullptr, 0);
   EmbedScratch s;
-  carve(ar, plan_for(n > 0 ? n : 1, vocab), vocab, d, &s);
+  carve(ar, most_for(n > 0 ? n : 1, vocab), vocab, d, &s);
   return ar.used();
 }
 
