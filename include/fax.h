@@ -283,7 +283,8 @@ fax_status fax_set_attention_backward_two_chains(fax_ctx* ctx, int32_t enable);
 /* The token table's gradient in the LM calls (fax_lm_step*, fax_lm_accumulate, fax_lm_forward_backward).
  * enable = 0 (default): float atomics, whose order of addition changes from run to run.  enable != 0: the
  * tokens are sorted by id and each row is summed in a fixed order, as fax_op_embedding_backward does (in
- * the scratch arena, which fax_lm_sizes makes large enough either way). */
+ * the scratch arena, which fax_lm_sizes makes large enough either way; where the logits' buffer is too small
+ * for the sort, what it needs lies behind row_loss, and is asked for only while the switch is on). */
 fax_status fax_set_sorted_embedding_gradient(fax_ctx* ctx, int32_t enable);
 
 /* One trainable tensor of a training state: float32 master, compute-precision

@@ -31,9 +31,11 @@ struct LmScratch {
   int32_t* ids; int32_t* targets;   // staging for the host entry point
   BlockScratch blk;
   void* dxa; void* dxb;             // gradient ping-pong between layers
-  void* logits; int head_rows;      // after the head also the scratch of the sorted embedding gradient
-  size_t logits_bytes;
+  void* logits; int head_rows;
   float* row_loss;
+  size_t without_sort;              // bytes of all of the above
+  void* sort; size_t sort_bytes;    // scratch of the sorted embedding gradient: the logits' buffer where that is large enough
+  size_t need(const fax_ctx* ctx, const FaxArena& ar) const { return ctx->sorted_embed_grad ? ar.used() : without_sort; }
 };
 
 fax_status lm_validate(const fax_lm_cfg* c) {
@@ -66,11 +68,12 @@ void carve_scratch(const fax_lm_cfg* c, FaxArena& ar, LmScratch* s) {
   s->dxa = ar.take(N * d * es);
   s->dxb = ar.take(N * d * es);
   s->head_rows = head_rows_for(c, N, (size_t)c->vocab, es);
-  s->logits_bytes = (size_t)s->head_rows * c->vocab * es;
-  const size_t sort_bytes = fax_embedding_grad_scratch_bytes((int)N, c->vocab, (int)d);
-  if (s->logits_bytes < sort_bytes) s->logits_bytes = sort_bytes;
-  s->logits = ar.take(s->logits_bytes);
+  const size_t logits_bytes = (size_t)s->head_rows * c->vocab * es;
+  s->logits = ar.take(logits_bytes);
   s->row_loss = (float*)ar.take(N * 4);
+  s->without_sort = ar.used();
+  s->sort_bytes = fax_embedding_grad_scratch_bytes((int)N, c->vocab, (int)d);
+  s->sort = s->sort_bytes <= logits_bytes ? s->logits : ar.take(s->sort_bytes);
 }
 
 fax_status check_param(const fax_param& p, uint64_t n, int prec) {
@@ -163,7 +166,7 @@ fax_status lm_fwd_bwd(fax_ctx* ctx, const fax_lm_cfg* c, const fax_lm_state* st,
   }
   // embedding gradients: scatter into the tied dwte, batch-sum into dwpe
   return fax_embed_bwd(ctx, prec, bc->batch, bc->seq, c->max_seq, d, V, ids, dcur, st->wte.g, st->wpe.g, acc,
-                       ctx->sorted_embed_grad ? w.logits : nullptr, w.logits_bytes);
+                       ctx->sorted_embed_grad ? w.sort : nullptr, w.sort_bytes);
 }
 
 // AdamW of the tensors that are not inside a block (the blocks' tensors are updated under backward).
@@ -194,7 +197,7 @@ fax_status lm_run(fax_ctx* ctx, const fax_lm_cfg* cfg, const fax_lm_state* st, c
   LmSaved sv; LmScratch w;
   carve_saved(cfg, ar, &sv);
   carve_scratch(cfg, aw, &w);
-  if (ar.used() > st->saved_bytes || aw.used() > st->scratch_bytes) return FAX_ERR_WORKSPACE_TOO_SMALL;
+  if (ar.used() > st->saved_bytes || w.need(ctx, aw) > st->scratch_bytes) return FAX_ERR_WORKSPACE_TOO_SMALL;
   if (ids_host) {
     const size_t nb = (size_t)cfg->block.batch * cfg->block.seq * sizeof(int32_t);
     FAX_CUDA_TRY(ctx, cudaMemcpyAsync(w.ids, ids_host, nb, cudaMemcpyHostToDevice, ctx->stream));
@@ -258,7 +261,7 @@ extern "C" fax_status fax_lm_accumulate(fax_ctx* ctx, const fax_lm_cfg* cfg, con
   LmSaved sv; LmScratch w;
   carve_saved(cfg, ar, &sv);
   carve_scratch(cfg, aw, &w);
-  if (ar.used() > st->saved_bytes || aw.used() > st->scratch_bytes) return FAX_ERR_WORKSPACE_TOO_SMALL;
+  if (ar.used() > st->saved_bytes || w.need(ctx, aw) > st->scratch_bytes) return FAX_ERR_WORKSPACE_TOO_SMALL;
   return lm_fwd_bwd(ctx, cfg, st, ids, targets, loss_device, sv, w, nullptr, accumulate != 0, grad_scale);
 }
 
