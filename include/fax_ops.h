@@ -182,6 +182,12 @@ typedef struct {
 } fax_fp8_gemm_desc;
 fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* desc);
 
+/* The tile that fax_op_fp8_gemm takes for a product of these sizes under the context's settings (host pointers): how
+ * many SMs share one (1, or 2: a pair, unless fax_set_gemm_two_cta is off), its columns (64 to 256; 128 rows an SM), and
+ * the slices of K that a cluster of SMs joins (1: none).  For inspection and tests; nothing is launched. */
+fax_status fax_op_fp8_gemm_tile(const fax_ctx* ctx, int32_t M, int32_t N, int32_t K, int32_t c_f32,
+                                int32_t* sms, int32_t* columns, int32_t* slices);
+
 #ifdef __cplusplus
 }
 #endif

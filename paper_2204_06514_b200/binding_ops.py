@@ -56,6 +56,7 @@ _SIGNATURES = {
                                               C.c_int32, _P, _P, C.c_size_t]),
     "fax_op_fp8_quantize": (C.c_int32, [_P, C.c_int32, C.POINTER(Fp8QuantizeDesc)]),
     "fax_op_fp8_gemm": (C.c_int32, [_P, C.POINTER(Fp8GemmDesc)]),
+    "fax_op_fp8_gemm_tile": (C.c_int32, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32] + [C.POINTER(C.c_int32)] * 3),
 }
 
 _lib = None
@@ -153,3 +154,10 @@ def fax_op_fp8_quantize(ctx, prec, desc: Fp8QuantizeDesc):
 
 def fax_op_fp8_gemm(ctx, desc: Fp8GemmDesc):
     _check(_L().fax_op_fp8_gemm(ctx, C.byref(desc)), "fax_op_fp8_gemm")
+
+
+def fax_op_fp8_gemm_tile(ctx, M, N, K, c_f32) -> tuple[int, int, int]:
+    """(SMs that share a tile, its columns, slices of K) of such a product under the context's settings."""
+    out = [C.c_int32() for _ in range(3)]
+    _check(_L().fax_op_fp8_gemm_tile(ctx, M, N, K, int(bool(c_f32)), *(C.byref(o) for o in out)), "fax_op_fp8_gemm_tile")
+    return tuple(o.value for o in out)

@@ -647,8 +647,23 @@ TileChoice choose_tile(const fax_ctx* ctx, int M, int N, int K, bool sums) {
   }
   return best;
 }
+// A float output longer than one segment is summed in registers; otherwise one accumulator holds all of K.
+TileChoice tile_for(const fax_ctx* ctx, int M, int N, int K, bool c_f32) { return choose_tile(ctx, M, N, K, c_f32 && K > SEGMENT * BK); }
+
+fax_status check_sizes(int M, int N, int K) {
+  if (M <= 0 || N <= 0 || K <= 0) return FAX_ERR_INVALID_ARG;
+  return M > 0x7ffffe00 || N > 0x7ffffe00 || K > 0x7ffffe00 ? FAX_ERR_UNSUPPORTED_SHAPE : FAX_OK;
+}
 
 }  // namespace
+
+extern "C" fax_status fax_op_fp8_gemm_tile(const fax_ctx* ctx, int32_t M, int32_t N, int32_t K, int32_t c_f32, int32_t* sms, int32_t* columns, int32_t* slices) {
+  if (!ctx || !sms || !columns || !slices) return FAX_ERR_INVALID_ARG;
+  FAX_TRY(check_sizes(M, N, K));
+  const TileChoice t = tile_for(ctx, M, N, K, c_f32 != 0);
+  *sms = t.cg; *columns = t.bn; *slices = t.splits;
+  return FAX_OK;
+}
 
 extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) {
   if (!ctx || !d || !d->A || !d->B || !d->C || !d->a_scale || !d->b_scale) return FAX_ERR_INVALID_ARG;
@@ -663,9 +678,9 @@ extern "C" fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* d) 
       !fax_aligned(d->bias, 2))
     return FAX_ERR_INVALID_ARG;
   if (d->lda >= (1LL << 40) || d->ldb >= (1LL << 40)) return FAX_ERR_UNSUPPORTED_SHAPE;        // the pitch a tensor map can hold
-  if (d->M > 0x7ffffe00 || d->N > 0x7ffffe00 || d->K > 0x7ffffe00) return FAX_ERR_UNSUPPORTED_SHAPE;
-  const TileChoice t = choose_tile(ctx, d->M, d->N, d->K, d->c_f32 && d->K > SEGMENT * BK);
-  const bool sums = t.splits > 1 || (d->c_f32 && d->K > SEGMENT * BK);      // otherwise one segment holds all of K
+  FAX_TRY(check_sizes(d->M, d->N, d->K));
+  const TileChoice t = tile_for(ctx, d->M, d->N, d->K, d->c_f32 != 0);
+  const bool sums = t.splits > 1 || (d->c_f32 && d->K > SEGMENT * BK);
   CUtensorMap ma, mb;
   if (!make_map_u8(ctx, &ma, d->A, d->K, d->M, d->lda, BM) || !make_map_u8(ctx, &mb, d->B, d->K, d->N, d->ldb, (uint32_t)(t.bn / t.cg))) return FAX_ERR_INVALID_ARG;
   Fp8Params p;
