@@ -288,7 +288,9 @@ fax_status fax_set_attention_backward_two_chains(fax_ctx* ctx, int32_t enable);
 fax_status fax_set_sorted_embedding_gradient(fax_ctx* ctx, int32_t enable);
 
 /* One trainable tensor of a training state: float32 master, compute-precision
- * copy (bf16; in FP32_VALIDATE may equal w or be NULL), Adam moments, float32
+ * copy (bf16; in FP32_VALIDATE may equal w or be NULL), Adam moments (calls that
+ * update nothing, fax_lm_forward_backward and fax_lm_accumulate, do not need them:
+ * NULL where another optimizer state, as fax_adamw8_step's, holds them), float32
  * gradient, element count and its weight decay. */
 typedef struct {
   float* w; void* w_compute; float* m; float* v; float* g;

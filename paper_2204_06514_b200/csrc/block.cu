@@ -312,12 +312,12 @@ int fax_layer_adamw_tensors(const fax_layer_state* L, int prec, fax_adamw_tensor
   return 12;
 }
 
-fax_status fax_layer_check(const fax_layer_state* L, const fax_block_cfg* c) {
+fax_status fax_layer_check(const fax_layer_state* L, const fax_block_cfg* c, bool updates) {
   const fax_param* a = (const fax_param*)L;
   const uint64_t d = c->d_model, f = c->d_ff;
   const uint64_t want[12] = {d, d, d * 3 * d, 3 * d, d * d, d, d, d, d * f, f, f * d, d};
   for (int i = 0; i < 12; ++i) {
-    if (!a[i].w || !a[i].m || !a[i].v || !a[i].g) return FAX_ERR_INVALID_ARG;
+    if (!a[i].w || !a[i].g || (updates && (!a[i].m || !a[i].v))) return FAX_ERR_INVALID_ARG;
     if (c->prec == FAX_PREC_BF16 && !a[i].w_compute) return FAX_ERR_INVALID_ARG;
     if (a[i].n != want[i]) return FAX_ERR_INVALID_ARG;
   }
@@ -370,7 +370,7 @@ extern "C" fax_status fax_block_step(fax_ctx* ctx, const fax_block_cfg* cfg, con
                                      const fax_adamw_hparams* hp) {
   if (!ctx || !st || !x || !dy || !y || !dx || !hp || !st->saved || !st->scratch || x == y) return FAX_ERR_INVALID_ARG;
   FAX_TRY(fax_block_validate(cfg));
-  FAX_TRY(fax_layer_check(&st->layer, cfg));
+  FAX_TRY(fax_layer_check(&st->layer, cfg, true));
   FAX_TRY(fax_adamw_check_hparams(hp));
   FaxStepKey key;
   key.add('B');
@@ -397,7 +397,7 @@ extern "C" fax_status fax_block_step_host(fax_ctx* ctx, const fax_block_cfg* cfg
     return FAX_ERR_INVALID_ARG;
   FAX_TRY(fax_adamw_check_hparams(hp));
   FAX_TRY(fax_block_validate(cfg));
-  FAX_TRY(fax_layer_check(&st->layer, cfg));
+  FAX_TRY(fax_layer_check(&st->layer, cfg, true));
   const size_t bytes = (size_t)cfg->batch * cfg->seq * cfg->d_model * fax_elem_size(cfg->prec);
   const size_t nd = fax_round_up(bytes, 256);
   if (st->scratch_bytes < 4 * nd) return FAX_ERR_WORKSPACE_TOO_SMALL;

@@ -23,4 +23,4 @@ fax_status fax_block_backward_impl(fax_ctx* ctx, const fax_block_cfg* c, const f
                                    const FaxAdamHook* hook = nullptr);
 void fax_layer_views(const fax_layer_state* L, int prec, fax_block_params* p, fax_block_grads* g);
 int fax_layer_adamw_tensors(const fax_layer_state* L, int prec, fax_adamw_tensor* out);
-fax_status fax_layer_check(const fax_layer_state* L, const fax_block_cfg* c);
+fax_status fax_layer_check(const fax_layer_state* L, const fax_block_cfg* c, bool updates);      // updates: AdamW's moments are needed too

@@ -76,8 +76,8 @@ void carve_scratch(const fax_lm_cfg* c, FaxArena& ar, LmScratch* s) {
   s->sort = s->sort_bytes <= logits_bytes ? s->logits : ar.take(s->sort_bytes);
 }
 
-fax_status check_param(const fax_param& p, uint64_t n, int prec) {
-  if (!p.w || !p.m || !p.v || !p.g || p.n != n) return FAX_ERR_INVALID_ARG;
+fax_status check_param(const fax_param& p, uint64_t n, int prec, bool updates) {
+  if (!p.w || !p.g || p.n != n || (updates && (!p.m || !p.v))) return FAX_ERR_INVALID_ARG;
   if (prec == FAX_PREC_BF16 && !p.w_compute) return FAX_ERR_INVALID_ARG;
   return FAX_OK;
 }
@@ -85,15 +85,15 @@ const void* compute_ptr(const fax_param& p, int prec) {
   return (prec == FAX_PREC_BF16 || p.w_compute) ? (const void*)p.w_compute : (const void*)p.w;
 }
 
-fax_status lm_check_state(const fax_lm_cfg* c, const fax_lm_state* st) {
+fax_status lm_check_state(const fax_lm_cfg* c, const fax_lm_state* st, bool updates) {
   if (!st || !st->layers || !st->saved || !st->scratch) return FAX_ERR_INVALID_ARG;
   const uint64_t d = c->block.d_model;
   const int prec = c->block.prec;
-  FAX_TRY(check_param(st->wte, (uint64_t)c->vocab * d, prec));
-  FAX_TRY(check_param(st->wpe, (uint64_t)c->max_seq * d, prec));
-  FAX_TRY(check_param(st->lnf_g, d, prec));
-  FAX_TRY(check_param(st->lnf_b, d, prec));
-  for (int l = 0; l < c->n_layers; ++l) FAX_TRY(fax_layer_check(&st->layers[l], &c->block));
+  FAX_TRY(check_param(st->wte, (uint64_t)c->vocab * d, prec, updates));
+  FAX_TRY(check_param(st->wpe, (uint64_t)c->max_seq * d, prec, updates));
+  FAX_TRY(check_param(st->lnf_g, d, prec, updates));
+  FAX_TRY(check_param(st->lnf_b, d, prec, updates));
+  for (int l = 0; l < c->n_layers; ++l) FAX_TRY(fax_layer_check(&st->layers[l], &c->block, updates));
   if (!fax_aligned(st->saved, 256) || !fax_aligned(st->scratch, 256)) return FAX_ERR_INVALID_ARG;
   return FAX_OK;
 }
@@ -191,7 +191,7 @@ fax_status lm_run(fax_ctx* ctx, const fax_lm_cfg* cfg, const fax_lm_state* st, c
                   const int32_t* targets, const fax_adamw_hparams* hp, float* loss_device,
                   const int32_t* ids_host, const int32_t* targets_host) {
   FAX_TRY(lm_validate(cfg));
-  FAX_TRY(lm_check_state(cfg, st));
+  FAX_TRY(lm_check_state(cfg, st, hp != nullptr));
   if (!loss_device) return FAX_ERR_INVALID_ARG;
   FaxArena ar(st->saved, st->saved_bytes), aw(st->scratch, st->scratch_bytes);
   LmSaved sv; LmScratch w;
@@ -256,7 +256,7 @@ extern "C" fax_status fax_lm_accumulate(fax_ctx* ctx, const fax_lm_cfg* cfg, con
                                         int32_t accumulate, float grad_scale) {
   if (!ctx || !ids || !targets || !loss_device) return FAX_ERR_INVALID_ARG;
   FAX_TRY(lm_validate(cfg));
-  FAX_TRY(lm_check_state(cfg, st));
+  FAX_TRY(lm_check_state(cfg, st, false));
   FaxArena ar(st->saved, st->saved_bytes), aw(st->scratch, st->scratch_bytes);
   LmSaved sv; LmScratch w;
   carve_saved(cfg, ar, &sv);
@@ -270,7 +270,7 @@ extern "C" fax_status fax_lm_apply_adamw(fax_ctx* ctx, const fax_lm_cfg* cfg, co
   if (!ctx || !hp) return FAX_ERR_INVALID_ARG;
   FAX_TRY(fax_adamw_check_hparams(hp));
   FAX_TRY(lm_validate(cfg));
-  FAX_TRY(lm_check_state(cfg, st));
+  FAX_TRY(lm_check_state(cfg, st, true));
   fax_adamw_hparams h = *hp;
   h.grad_is_bf16 = 0;
   const int prec = cfg->block.prec;

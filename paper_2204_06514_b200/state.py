@@ -28,14 +28,15 @@ def hparams(lr, beta1, beta2, eps, step, grad_is_bf16=0, **_) -> fx.AdamwHparams
 
 
 class ParamSet:
-    """One trainable tensor on the device: fp32 master, compute copy, m, v, g."""
+    """One trainable tensor on the device: fp32 master, compute copy, m, v, g.  moments=False leaves m and v out, for an
+    optimizer state of its own (Moments8); the calls that update weights with float32 moments then refuse it."""
 
-    def __init__(self, w: np.ndarray | torch.Tensor, prec: int, device, weight_decay: float):
+    def __init__(self, w: np.ndarray | torch.Tensor, prec: int, device, weight_decay: float, moments: bool = True):
         w = torch.as_tensor(w, dtype=torch.float32)
         self.w = w.to(device).contiguous()
         self.wc = self.w.to(torch.bfloat16) if prec == fx.FAX_PREC_BF16 else None
-        self.m = torch.zeros_like(self.w)
-        self.v = torch.zeros_like(self.w)
+        self.m = torch.zeros_like(self.w) if moments else None
+        self.v = torch.zeros_like(self.w) if moments else None
         self.g = torch.zeros_like(self.w)
         self.weight_decay = weight_decay
 
@@ -52,8 +53,9 @@ class ParamSet:
 
 
 class Moments8:
-    """Adam moments in 8 bits for a list of ParamSets: an optimizer state of 2.06 bytes per parameter beside
-    the float32 moments' 8, stepped in one call (fax_adamw8_step).  Reads the sets' w, g and compute copy."""
+    """Adam moments in 8 bits for a list of ParamSets: an optimizer state of 2.06 bytes per parameter in place of
+    the float32 moments' 8 (sets, LmRunner and BlockRunner take moments=False), stepped in one call (fax_adamw8_step).
+    Reads the sets' w, g and compute copy."""
 
     def __init__(self, params: list[ParamSet], seed: int = 1):
         self.params = list(params)
@@ -97,11 +99,11 @@ class BlockRunner:
     """One decoder block with its training state resident on the device."""
 
     def __init__(self, sess: Session, cfg: Config, params: dict, prec: int = fx.FAX_PREC_BF16,
-                 weight_decay: float = 0.1, host_io: bool = False, recompute: bool = False):
+                 weight_decay: float = 0.1, host_io: bool = False, recompute: bool = False, moments: bool = True):
         self.sess, self.cfg, self.prec = sess, cfg, prec
         self.bcfg = block_cfg(cfg, prec, int(recompute))
         self.dtype = torch.bfloat16 if prec == fx.FAX_PREC_BF16 else torch.float32
-        self.p = {k: ParamSet(params[k], prec, sess.device, weight_decay) for k in PARAM_NAMES}
+        self.p = {k: ParamSet(params[k], prec, sess.device, weight_decay, moments) for k in PARAM_NAMES}
         self.saved_bytes, self.scratch_bytes = fx.fax_block_sizes(self.bcfg)
         if host_io:
             self.scratch_bytes = fx.fax_block_host_scratch_bytes(self.bcfg)
@@ -144,11 +146,11 @@ class LmRunner:
     """N-layer LM with its training state resident on the device."""
 
     def __init__(self, sess: Session, cfg: Config, lm: dict, prec: int = fx.FAX_PREC_BF16,
-                 weight_decay: float = 0.1, recompute: bool = False, head_rows: int = 0):
+                 weight_decay: float = 0.1, recompute: bool = False, head_rows: int = 0, moments: bool = True):
         self.sess, self.cfg, self.prec = sess, cfg, prec
         self.lcfg = fx.LmCfg(cfg.n_layers, cfg.vocab, lm["wpe"].shape[0], block_cfg(cfg, prec, int(recompute)),
                              head_rows)
-        mk = lambda a: ParamSet(a, prec, sess.device, weight_decay)
+        mk = lambda a: ParamSet(a, prec, sess.device, weight_decay, moments)
         self.wte, self.wpe = mk(lm["wte"]), mk(lm["wpe"])
         self.lnf_g, self.lnf_b = mk(lm["lnf_g"]), mk(lm["lnf_b"])
         self.layers = [{k: mk(p[k]) for k in PARAM_NAMES} for p in lm["blocks"]]
