@@ -284,7 +284,8 @@ fax_status fax_set_attention_backward_two_chains(fax_ctx* ctx, int32_t enable);
  * enable = 0 (default): float atomics, whose order of addition changes from run to run.  enable != 0: the
  * tokens are sorted by id and each row is summed in a fixed order, as fax_op_embedding_backward does (in
  * the scratch arena, which fax_lm_sizes makes large enough either way; where the logits' buffer is too small
- * for the sort, what it needs lies behind row_loss, and is asked for only while the switch is on). */
+ * for the sort, what it needs lies behind row_loss, and is asked for only while the switch is on).  The fixed
+ * order costs time: 122 us of a 17 ms step against 99 - 109 us (124M model, 16 x 1024 tokens). */
 fax_status fax_set_sorted_embedding_gradient(fax_ctx* ctx, int32_t enable);
 
 /* One trainable tensor of a training state: float32 master, compute-precision

@@ -123,7 +123,7 @@ fax_status fax_op_embedding_forward(fax_ctx* ctx, int32_t prec, int32_t n_tokens
  * that a token touches.  Tokens with an id outside [0, vocab) add nothing.  Each
  * row is summed over its tokens in float32 in a fixed order (long batches are
  * sorted by id first, short ones are not): the same inputs give the same bits (an accumulated row gets its sum in
- * one addition per element).  Concurrent calls, and graphs that may be replayed at
+ * one addition per element, in memory, where subnormal numbers count as 0).  Concurrent calls, and graphs that may be replayed at
  * the same time, need scratch of their own.  n_tokens and d <= 2^30; scratch 256-byte aligned.
  * Scratch of the longest batch serves every shorter one: the bytes never shrink with n_tokens, vocab or d. */
 fax_status fax_op_embedding_backward_scratch_bytes(int32_t n_tokens, int32_t vocab, int32_t d, size_t* bytes);
@@ -169,7 +169,9 @@ fax_status fax_op_fp8_quantize(fax_ctx* ctx, int32_t prec, const fax_fp8_quantiz
  * to bf16, or kept as float (c_f32 != 0), or added to a float C (accumulate != 0).
  * The forward product takes activations and transposed weights (tile 128),
  * the input gradient output gradients and weights as stored, the weight gradient
- * both factors transposed with tile 1.  Any M, N, K.  The scales are powers of
+ * both factors transposed with tile 1.  Any M, N, K from 1 on.  What is added to
+ * C is added in memory, where subnormal numbers count as 0 (on either side and in
+ * the sum).  The scales are powers of
  * two from 2^-126 to 2^127, as fax_op_fp8_quantize gives them (of any other
  * float the exponent alone counts; infinities and NaN make NaN).  ldc >= N in elements; C aligned to its
  * elements (16-byte aligned rows are stored faster).  C may not overlap A or B. */

@@ -24,7 +24,8 @@
 //
 // SPLIT: few tiles and a long K (one token's product with a large weight).  A cluster of CTAs shares one tile, each over a
 // slice of K; all but the first send their float sums to the first one's shared memory, which adds them in
-// order (16 x 4096 x 4096: 12.4 us unsplit, 10.4 us on clusters of eight).
+// order (16 x 4096 x 4096: 12.5 us unsplit, 10.4 us on clusters of four with eight K blocks a CTA; 128 x 1024 x 8192:
+// 21.9 and 16.1 us).
 //
 // Edges: TMA fills what lies outside a matrix with zeros (scales outside are 1), and the stores are
 // limited to C.  Every wait is bounded.
@@ -173,8 +174,8 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
 
 // A warp's 32 x 32 sums (a row a lane) of rows row0 .. and columns col .., to C, through the warp's staging buffer.
 // Where a tensor map can describe C, one bulk store (or, for a product that is added, one bulk reduction at L2: nothing
-// waits for C) takes the buffer, swizzled as the map says, and cuts it off at C's edges; the sums of a float
-// output 4096 x 4096 x 4096 took 86.5 us with rows stored from registers, 85 us so.  Other pitches: the lanes write along a row.
+// waits for C) takes the buffer, swizzled as the map says, and cuts it off at C's edges (float 4096 x 4096 x 4096: 78 us,
+// 81 us by rows; bf16 4096 x 4096 x 128: 11 and 18 us).  Other pitches: the lanes write along a row.
 constexpr int STG_BYTES = 5120;        // per warp: 32 x 33 floats, or the 4096 bytes of a swizzled box; a multiple of 1024
 __device__ __forceinline__ void store_chunk(const Fp8Params& p, const CUtensorMap* mc, const uint32_t (&r)[32], long long row0, int col, float* stg,
                                             uint32_t stg_addr, int lane) {
@@ -616,8 +617,10 @@ fax_status launch(fax_ctx* ctx, int grid, int cluster, int smem, const CUtensorM
 constexpr int FIXED_SMEM = SC_SLOTS * SC_BYTES + 1024 + BAR_BYTES + NUM_EPI_WARPS * STG_BYTES;
 int split_bytes(int splits, int M, int bn) { return (splits - 1) * (M < 128 ? (M + 31) / 32 : 4) * (bn / 32) * 4096; }
 
-// Time of a tile shape in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's end),
-// the paces as measured with all SMs busy, with one sum over K and with sums of 512 k.  A pair of SMs loads each operand byte for twice the work and runs best
+// What tile shapes are compared by, in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's
+// end), the paces as measured with all SMs busy, with one sum over K and with sums of 512 k.  It orders the shapes and is no
+// forecast of a call, which also pays for the launch, the first loads and the last stores (4096 x 1000 x 5000 added to float:
+// 23.6 here, for pairs and single SMs alike, of which the first in the table is taken; 30 us measured).  A pair of SMs loads each operand byte for twice the work and runs best
 // where there are tiles for all pairs; a narrower tile has about the pace of the 128-column one (the issue of
 // its MMAs bounds it), so it pays only where it brings more SMs to work.  Where the tiles leave SMs idle, slices of K
 // bring them in, for the price of the exchange.
