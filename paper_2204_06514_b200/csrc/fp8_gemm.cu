@@ -620,7 +620,7 @@ int split_bytes(int splits, int M, int bn) { return (splits - 1) * (M < 128 ? (M
 // What tile shapes are compared by, in microseconds: waves of tiles times (K blocks times the pace of one, plus the tile's
 // end), the paces as measured with all SMs busy, with one sum over K and with sums of 512 k.  It orders the shapes and is no
 // forecast of a call, which also pays for the launch, the first loads and the last stores (4096 x 1000 x 5000 added to float:
-// 23.6 here, for pairs and single SMs alike, of which the first in the table is taken; 30 us measured).  A pair of SMs loads each operand byte for twice the work and runs best
+// 23.6 here, for pairs and single SMs alike, of which the first in the table is taken; 30 us measured in a graph).  A pair of SMs loads each operand byte for twice the work and runs best
 // where there are tiles for all pairs; a narrower tile has about the pace of the 128-column one (the issue of
 // its MMAs bounds it), so it pays only where it brings more SMs to work.  Where the tiles leave SMs idle, slices of K
 // bring them in, for the price of the exchange.
