@@ -71,7 +71,8 @@ class Moments8:
                             _ptr(p.wc), p.w.numel(), p.weight_decay, (seed + i) & 0xFFFFFFFF) for i, p in enumerate(self.params)])
 
     def step(self, ctx, hp):
-        fx.fax_adamw8_step(ctx, self.tensors, hp)
+        # the sets' gradients are float32 whatever hp says, as in the whole-step calls
+        fx.fax_adamw8_step(ctx, self.tensors, fx.AdamwHparams(hp.lr, hp.beta1, hp.beta2, hp.eps, hp.step, 0))
 
 
 class Session:

@@ -97,3 +97,14 @@ def test_block_without_float32_moments(sess):
         with pytest.raises(fx.FaxError) as e:
             call()
         assert e.value.status == fx.FAX_ERR_INVALID_ARG
+
+
+def test_gradients_of_the_sets_are_float32(sess):
+    """A step asked for with bf16 gradients reads the sets' own all the same, as fax_lm_step does."""
+    rng = np.random.default_rng(2)
+    p = ParamSet(rng.standard_normal(1000).astype(np.float32), fx.FAX_PREC_BF16, sess.device, 0.1)
+    p.g.copy_(torch.as_tensor(rng.standard_normal(1000).astype(np.float32)))
+    opt, state = Moments8([p], seed=4), zero_state([p])
+    opt.step(sess.ctx, hparams(step=1, grad_is_bf16=1, **HP))
+    want = ref.adamw8(*state[0], host(p.g), 0.1, 4, step=1, **HP)
+    assert np.array_equal(host(opt.m[0].view(torch.float8_e4m3fn)), want[1]) and np.abs(host(p.w) - want[0]).max() <= 1e-6
