@@ -89,9 +89,9 @@ def check(sess, m, n, k, fa, fb, b_tile, f32, acc, bias, seed, pad=0, out_pad=0,
     return a, b, out
 
 
-# Rows: a last pair of tiles whose second SM has all, some (900, 1900) or none (520, 1300) of its 128 rows; columns that end anywhere
-# in a tile; K that ends anywhere in a block, a word of four scales, or a segment of 512.  4100 x 4099 and 4100 x 4104 have
-# several tiles for each pair, so that both accumulators are used again.
+# Rows: a last pair of tiles whose second SM has all (4096), some (900, 3000, 3500) or none (the others) of its 128 rows; columns
+# that end anywhere in a tile; K that ends anywhere in a block, a word of four scales, or a segment of 512.  4100 x 4099 and
+# 4100 x 4104 have several tiles for each pair, so that both accumulators are used again.
 PAIRS = [
     (520, 5000, 3900, 0, (2, 256, 1)), (900, 3500, 3900, 0, (2, 256, 1)), (4096, 770, 3900, 0, (2, 256, 1)), (4100, 4104, 2100, 0, (2, 256, 1)),
     (1300, 5000, 3900, 1, (2, 256, 1)), (1900, 3500, 3900, 1, (2, 256, 1)), (1100, 6010, 3900, 1, (2, 256, 1)), (4100, 4099, 4000, 1, (2, 256, 1)),
