@@ -82,12 +82,12 @@ uint64_t fax_launch_count(const fax_ctx* ctx);
  * operator launch on this context is bracketed by a pair of CUDA events on the
  * context's stream.  fax_profile_end synchronises the stream and fills `out`
  * (HOST array of n_out entries, indexed by kernel class: FAX_KERNEL_CLASSES for all;
- * an array of the FAX_KERNEL_CLASSES_MIN classes of earlier versions is filled as far as it goes)
+ * an array of the 12 or FAX_KERNEL_CLASSES_MIN classes of earlier versions is filled as far as it goes)
  * with, per class: operator launches, summed device milliseconds, summed
  * algorithmic FLOPs (2 per multiply-add) and summed algorithmic bytes (what the
  * operator must read and write once).  Profiling costs two event records per
  * launch, so timed runs keep it off. */
-#define FAX_KERNEL_CLASSES 12
+#define FAX_KERNEL_CLASSES 16
 #define FAX_KERNEL_CLASSES_MIN 10
 typedef struct { int64_t launches; double ms, flops, bytes; } fax_profile_entry;
 fax_status fax_profile_begin(fax_ctx* ctx);

@@ -190,6 +190,170 @@ fax_status fax_op_fp8_gemm(fax_ctx* ctx, const fax_fp8_gemm_desc* desc);
 fax_status fax_op_fp8_gemm_tile(const fax_ctx* ctx, int32_t M, int32_t N, int32_t K, int32_t c_f32,
                                 int32_t* sms, int32_t* columns, int32_t* slices);
 
+/* ---- positions by rotation ----
+ * The first rot_dim elements of each head are rot_dim / 2 pairs, (i, i + rot_dim / 2) with FAX_ROTARY_HALVES or
+ * (2i, 2i + 1) with FAX_ROTARY_PAIRS; pair i of a token at position p is turned by the angle p * frequency[i]:
+ *   y_a = amplitude * (cos * x_a - sin * x_b),   y_b = amplitude * (cos * x_b + sin * x_a)
+ * (backward != 0: sin negated, which is the gradient: dx from dy).  The elements behind rot_dim are copied, or stay
+ * where y is x.  x [rows, heads * head_dim] T, pitch ldx: `heads` heads one after another, e.g. q and k (2 * n_heads) of a fused
+ * qkv buffer; y likewise with pitch ldy, x itself (ldy = ldx) or memory that holds none of x's elements.  A token's position
+ * is positions[row] (int32, device), or without positions first + row % seq (seq = 0: first + row).  frequencies: device,
+ * rot_dim / 2 words from fax_rotary_frequencies.  The angle is exact modulo a turn at any position (whole numbers
+ * modulo 2^64); y is rounded once to T.  rows = 0 does nothing; rot_dim is even,
+ * head_dim <= FAX_ROTARY_MAX_DIM and, where y is not x, even too. */
+enum { FAX_ROTARY_HALVES = 0, FAX_ROTARY_PAIRS = 1 };
+#define FAX_ROTARY_MAX_DIM 1024
+typedef struct {
+  int32_t rows, heads, head_dim, rot_dim, layout;
+  const void* x; int64_t ldx;
+  void* y; int64_t ldy;
+  const int32_t* positions; int32_t first, seq;
+  const uint64_t* frequencies;
+  float amplitude;
+  int32_t backward;
+} fax_rotary_desc;
+fax_status fax_op_rotary(fax_ctx* ctx, int32_t prec, const fax_rotary_desc* desc);
+
+/* frequency[i] = base^(-2 i / rot_dim) radians a position, as turns in units of 2^-64 (host, rot_dim / 2 words).
+ * For contexts `factor` times longer than trained: original_seq = 0 divides every frequency by factor; original_seq > 0
+ * keeps pairs that make high_turns or more turns in original_seq tokens, divides those of low_turns or fewer by factor
+ * and goes linearly in the turns between.  base >= 1, factor >= 1 (1: no scaling, the rest is not looked at), low_turns < high_turns. */
+fax_status fax_rotary_frequencies(int32_t rot_dim, double base, double factor, int32_t original_seq, double low_turns,
+                                  double high_turns, uint64_t* frequencies_host);
+
+/* ---- dropout ----
+ * y = resid + (kept ? x / (1 - p) : 0), rounded once to T (resid NULL: without it; a dropped element's x is not
+ * looked at).  An element is dropped where its 16 random bits are below round(65536 p); 1 - p is taken as
+ * 1 - round(65536 p) / 65536, so that the mean is x.  The bits are those of Philox4x32-10 (Salmon, Moraes, Dror,
+ * Shaw 2011) under the key `seed` for the counter (column / 8, row, offset), two 32-bit words of offset, low ones
+ * first: elements 2 w and 2 w + 1 of the eight columns have the low and the high half of word w.  Nothing is stored: the gradient is the
+ * same call on dy without resid.  Where offset_device is not NULL the 64-bit word there is added to offset when the kernel
+ * runs, so that a captured graph draws anew at each replay.  x, resid, y [rows, cols] T with pitches; y may be x
+ * or resid (same pitch), otherwise it holds none of their elements.  0 <= p <= 1 (1: nothing is kept); rows = 0 does nothing. */
+typedef struct {
+  int32_t rows, cols;
+  const void* x; int64_t ldx;
+  const void* resid; int64_t ldr;
+  void* y; int64_t ldy;
+  float p;
+  uint64_t seed, offset;
+  const uint64_t* offset_device;
+} fax_dropout_desc;
+fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropout_desc* desc);
+
+/* ---- gated linear recurrence ----
+ * For each channel c of d and the tokens t of a sequence, in float32:
+ *   a_t = 1 / (1 + exp(-f_t))      h_t = a_t h_{t-1} + b_t      y_t = h_t, or with g: h_t g_t / (1 + exp(-g_t))
+ * with b_t = x_t (FAX_RECURRENCE_PLAIN) or (1 - a_t) x_t (FAX_RECURRENCE_COMPLEMENT).  h starts at h0 [n_seq, d] float
+ * (NULL: zeros) and ends in h_last [n_seq, d] float (NULL: not wanted; may be h0), so that a sequence can be continued, a
+ * token at a time too.  f, x, g (NULL: none), y are [rows, d] T with pitches (columns of one fused projection, e.g.).
+ * Sequences are `seq` rows each (rows = n_seq * seq), or with offsets (device, [n_seq + 1] int32, from 0 not falling up to rows) sequence s is
+ * rows offsets[s] to offsets[s + 1] - 1, with seq the longest one's length (a choice of kernel goes by it, no result); rows outside stay as
+ * they were.  Offsets outside [0, rows] are taken as the nearest end, a falling one as an empty sequence.
+ * states: NULL, or for the backward pass fax_op_recurrence_states_floats floats, which receive h before every 16th token.
+ * y holds no element of f, x or g.  The same inputs give the same bits.  rows = 0 still writes h_last. */
+enum { FAX_RECURRENCE_PLAIN = 0, FAX_RECURRENCE_COMPLEMENT = 1 };
+#define FAX_RECURRENCE_BLOCK 16
+typedef struct {
+  int32_t rows, d, n_seq, seq;
+  const int32_t* offsets;
+  int32_t input;
+  const void* f; int64_t ldf;
+  const void* x; int64_t ldx;
+  const void* g; int64_t ldg;
+  const float* h0;
+  void* y; int64_t ldy;
+  float* h_last;
+  float* states;
+} fax_recurrence_desc;
+fax_status fax_op_recurrence_states_floats(int32_t rows, int32_t n_seq, int32_t d, size_t* floats);
+fax_status fax_op_recurrence_forward(fax_ctx* ctx, int32_t prec, const fax_recurrence_desc* desc);
+
+/* Its reverse: from dy [rows, d] T and dh_last [n_seq, d] float (NULL: zeros), with the forward call's inputs, states and
+ * sequences: df, dx, dg (wanted with g) [rows, d] T, and dh0 [n_seq, d] float (NULL: not wanted; may be dh_last).
+ *   dh_t = dy_t (g_t / (1 + exp(-g_t)) or 1) + a_{t+1} dh_{t+1}      dh0 = a_1 dh_1
+ * The gradients' memory holds no element of the inputs, except that each may be the input it belongs to (df f, dx x,
+ * dg g; same pitch). */
+typedef struct {
+  int32_t rows, d, n_seq, seq;
+  const int32_t* offsets;
+  int32_t input;
+  const void* f; int64_t ldf;
+  const void* x; int64_t ldx;
+  const void* g; int64_t ldg;
+  const float* h0;
+  const float* states;
+  const void* dy; int64_t lddy;
+  const float* dh_last;
+  void* df; int64_t lddf;
+  void* dx; int64_t lddx;
+  void* dg; int64_t lddg;
+  float* dh0;
+} fax_recurrence_backward_desc;
+fax_status fax_op_recurrence_backward(fax_ctx* ctx, int32_t prec, const fax_recurrence_backward_desc* desc);
+
+/* ---- a feed-forward layer of experts: tokens to their experts and back ----
+ * ids [n_tokens, top_k] int32: the experts a token chose; choices outside [0, n_experts) (padding) go nowhere.
+ * Each choice gets a slot, a row of a buffer in which every expert's tokens are together, in the order of
+ * (token, choice).  capacity > 0: expert e has the slots from e * capacity on, choices beyond its capacity go
+ * nowhere (the latest ones).  capacity = 0: an expert has as many slots as choices, rounded up to a multiple of
+ * `align` (e.g. 128 for fax_op_gemm).  Written: slot_of [n_tokens, top_k] (-1: nowhere), source [slots] (token * top_k +
+ * choice, -1: empty), offsets [n_experts + 1] (first slot of each expert), counts [n_experts] (choices
+ * made, kept or not), all int32.  slots is the length of source and the rows of the buffer, at least fax_op_expert_slots'.
+ * n_experts <= FAX_EXPERT_MAX; n_tokens = 0 gives an empty plan. */
+#define FAX_EXPERT_MAX 1024
+typedef struct {
+  int32_t n_tokens, top_k, n_experts, capacity, align, slots;
+  const int32_t* ids;
+  int32_t* slot_of;
+  int32_t* source;
+  int32_t* offsets;
+  int32_t* counts;
+} fax_expert_sort_desc;
+fax_status fax_op_expert_slots(int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t capacity, int32_t align,
+                               int32_t* slots_host);
+fax_status fax_op_expert_sort(fax_ctx* ctx, const fax_expert_sort_desc* desc);
+
+/* out[slot] = x[token] for every choice that has a slot, zeros in empty slots: all `slots` rows are written.
+ * x [n_tokens, d] T, out [slots, d] T, with pitches.  Its reverse is fax_op_expert_combine without weights.
+ * In all three calls a slot_of outside [0, slots) counts as -1. */
+typedef struct {
+  int32_t n_tokens, top_k, d, slots;
+  const int32_t* slot_of;
+  const int32_t* source;
+  const void* x; int64_t ldx;
+  void* out; int64_t ldo;
+} fax_expert_dispatch_desc;
+fax_status fax_op_expert_dispatch(fax_ctx* ctx, int32_t prec, const fax_expert_dispatch_desc* desc);
+
+/* y[token] = resid[token] (NULL: 0) + sum over its choices j, in their order, of weights[token, j] (NULL: 1) *
+ * z[slot_of[token, j]], in float32, rounded once to T.  weights [n_tokens, top_k] float; z [slots, d], resid and
+ * y [n_tokens, d] T, with pitches; y may be resid (same pitch). */
+typedef struct {
+  int32_t n_tokens, top_k, d, slots;
+  const int32_t* slot_of;
+  const float* weights;
+  const void* z; int64_t ldz;
+  const void* resid; int64_t ldr;
+  void* y; int64_t ldy;
+} fax_expert_combine_desc;
+fax_status fax_op_expert_combine(fax_ctx* ctx, int32_t prec, const fax_expert_combine_desc* desc);
+
+/* Its reverse (resid's gradient is dy): dz[slot] = weights[token, j] * dy[token], zeros in empty slots (all `slots`
+ * rows are written); dw[token, j] = sum over d of z[slot] dy[token], 0 for a choice without a slot (NULL: not wanted;
+ * z is not read then).  dz [slots, d] T, dw [n_tokens, top_k] float; dz may be z (same pitch). */
+typedef struct {
+  int32_t n_tokens, top_k, d, slots;
+  const int32_t* slot_of;
+  const int32_t* source;
+  const float* weights;
+  const void* z; int64_t ldz;
+  const void* dy; int64_t lddy;
+  void* dz; int64_t lddz;
+  float* dw;
+} fax_expert_combine_backward_desc;
+fax_status fax_op_expert_combine_backward(fax_ctx* ctx, int32_t prec, const fax_expert_combine_backward_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,7 @@ class FaxError(RuntimeError):
         super().__init__(f"{where}: {status_string(status)} ({status})")
 
 
-FAX_KERNEL_CLASSES = 12
+FAX_KERNEL_CLASSES = 16
 FAX_ADAMW8_BLOCK = 128
 
 

@@ -202,7 +202,7 @@ extern "C" fax_status fax_profile_end(fax_ctx* ctx, fax_profile_entry* out, int3
 extern "C" const char* fax_kernel_class_name(int32_t cls) {
   static const char* names[FAX_KERNEL_CLASSES] = {"gemm_tcgen05", "gemm_simt", "attention_fwd", "attention_bwd",
                                                   "layernorm_fwd", "layernorm_bwd", "adamw", "colsum", "embed", "xent",
-                                                  "fp8_quantize", "fp8_gemm"};
+                                                  "fp8_quantize", "fp8_gemm", "rotary", "dropout", "recurrence", "expert"};
   static_assert(KC_COUNT == FAX_KERNEL_CLASSES, "class names");
   return (cls >= 0 && cls < FAX_KERNEL_CLASSES) ? names[cls] : "unknown";
 }

@@ -16,7 +16,7 @@ typedef __nv_bfloat16 bf16;
 // Kernel classes of the per-kernel profile (order fixed by fax.h).
 enum FaxKernelClass {
   KC_GEMM_TC = 0, KC_GEMM_SIMT, KC_ATTN_FWD, KC_ATTN_BWD, KC_LN_FWD, KC_LN_BWD, KC_ADAMW, KC_COLSUM,
-  KC_EMBED, KC_XENT, KC_FP8_QUANT, KC_FP8_GEMM, KC_COUNT
+  KC_EMBED, KC_XENT, KC_FP8_QUANT, KC_FP8_GEMM, KC_ROTARY, KC_DROPOUT, KC_RECURRENCE, KC_EXPERT, KC_COUNT
 };
 struct FaxProfRec { int cls; cudaEvent_t e0, e1; double flops, bytes; };
 

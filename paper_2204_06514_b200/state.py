@@ -9,6 +9,7 @@ import numpy as np
 import torch
 
 from . import binding as fx
+from . import binding_ops as ops
 from .synth import Config
 
 PARAM_NAMES = fx.PARAM_NAMES
@@ -73,6 +74,13 @@ class Moments8:
     def step(self, ctx, hp):
         # the sets' gradients are float32 whatever hp says, as in the whole-step calls
         fx.fax_adamw8_step(ctx, self.tensors, fx.AdamwHparams(hp.lr, hp.beta1, hp.beta2, hp.eps, hp.step, 0))
+
+
+def rotary_frequencies(device, rot_dim: int, base: float = 10000.0, factor: float = 1.0, original_seq: int = 0,
+                       low_turns: float = 1.0, high_turns: float = 32.0) -> torch.Tensor:
+    """A model's frequency table of fax_op_rotary on the device: the words of fax_rotary_frequencies (as int64)."""
+    words = ops.fax_rotary_frequencies(rot_dim, base, factor, original_seq, low_turns, high_turns)
+    return torch.from_numpy(np.array(words, dtype=np.uint64).view(np.int64)).to(device)
 
 
 class Session:
