@@ -247,7 +247,7 @@ fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropout_desc* de
  * with b_t = x_t (FAX_RECURRENCE_PLAIN) or (1 - a_t) x_t (FAX_RECURRENCE_COMPLEMENT).  h starts at h0 [n_seq, d] float
  * (NULL: zeros) and ends in h_last [n_seq, d] float (NULL: not wanted; may be h0), so that a sequence can be continued, a
  * token at a time too.  f, x, g (NULL: none), y are [rows, d] T with pitches (columns of one fused projection, e.g.).
- * Sequences are `seq` rows each (rows = n_seq * seq), or with offsets (device, [n_seq + 1] int32, from 0 not falling up to rows) sequence s is
+ * Sequences are `seq` rows each (rows = n_seq * seq), or with offsets (device, [n_seq + 1] int32, not falling, within 0 to rows) sequence s is
  * rows offsets[s] to offsets[s + 1] - 1, with seq the longest one's length (a choice of kernel goes by it, no result); rows outside stay as
  * they were.  Offsets outside [0, rows] are taken as the nearest end, a falling one as an empty sequence.
  * states: NULL, or for the backward pass fax_op_recurrence_states_floats floats, which receive h before every 16th token.
