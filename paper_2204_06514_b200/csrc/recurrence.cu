@@ -2,24 +2,37 @@
 //
 // A stretch of tokens maps the state before it to the state behind it as h -> A h + B, and two stretches join as
 // (A2 A1, A2 B1 + B2), so that time can be split: a thread folds 16 tokens of its channels into (A, B), the (A, B) of
-// the stretches before it are joined in their order, and with the state that gives it goes over its 16 tokens again, which
-// are still in its registers.  Backward the same runs from the end: e_t = a_t (u_t + e_{t+1}) with u_t = dy_t gate_t is what token t
-// hands to the one before it, dh_t = u_t + e_{t+1}; h itself is worked out again from the state the forward pass kept
-// for every 16th token.  Inputs are read once and outputs written once, which bounds both passes by memory.
+// the stretches before it are joined in their order, and with the state that gives it goes over its 16 tokens again.
+// Backward the same runs from the end: e_t = a_t (u_t + e_{t+1}) with u_t = dy_t gate_t is what token t hands to the one
+// before it, dh_t = u_t + e_{t+1}; h itself is worked out again from the state the forward pass kept for every 16th token.
+// Inputs are read once and outputs written once, which is the floor of both passes (memory); next to it stand the
+// instructions, so that two channels share one wherever the hardware has it (f32x2).
 //
-// A warp has 32 * V channels (V = 2: a 128-byte line of bf16 a row) and 16 tokens at a time.  Where sequences are few, a
-// cluster of CTAs shares one: each CTA has 8 warps, one after the other in time, and the CTAs of a cluster follow one
-// another; (A, B) of a CTA goes to the others through distributed shared memory, one cluster barrier a stretch of
-// (CTAs * 128) tokens.  Where channels and sequences alone fill the GPU (or a sequence is one stretch), each warp takes a whole sequence by itself.
+// A warp has 64 channels, two a lane, and 16 tokens at a time.  Where sequences are few, a cluster of CTAs shares one:
+// each CTA has 8 warps, one after the other in time, and the CTAs of a cluster follow one another; (A, B) of a CTA goes to
+// the others through distributed shared memory, one cluster barrier a round of (CTAs * 128) tokens.  Where channels and sequences
+// alone fill the GPU, or sequences are one stretch, each warp takes a whole sequence by itself.
 // The order of joining is fixed by the sizes: the same inputs give the same bits.
+#include <type_traits>
+
+#include "gemm_common.cuh"
 #include "stream_common.cuh"
 #include "../../include/fax_ops.h"
 
 namespace {
 
-constexpr int WARPS = 8;
-constexpr int STEPS = FAX_RECURRENCE_BLOCK;      // tokens of a thread
-constexpr int MAX_CLUSTER = 8;                   // portable
+constexpr int MAX_WARPS = 16;                    // of a CTA: 128 registers a thread
+constexpr int STEPS = FAX_RECURRENCE_BLOCK;      // tokens of a stretch
+constexpr int CHANNELS = 64;                     // of a warp
+constexpr int MAX_CLUSTER = 16;
+constexpr int MAX_STAGES = 3;
+constexpr int SMEM_MAX = 226 * 1024;
+
+// How rows come in and go out.  TILES: 16 x 64 boxes by TMA through shared memory, those of the next rounds under the
+// current one's work (the backward pass, which has no room for its outputs, and a sequence's last rows, fewer than 16,
+// are stored row by row).  PAIRS: straight to registers, a lane's two channels side by side in one access.  SINGLES: a lane has channels c and
+// c + 32, an access each, for widths, pitches and addresses of any kind.
+enum Rows { TILES, PAIRS, SINGLES };
 
 struct RecurrenceParams {
   int32_t rows, d, n_seq, seq, tiles;
@@ -29,8 +42,79 @@ struct RecurrenceParams {
   int64_t ldf, ldx, ldg, lddy, ldy, lddf, lddx, lddg;
   const float *h0, *dh_last;
   float *h_last, *states, *dh0;
-  int32_t units;                                 // sequences * tiles
+  int32_t units;                                 // sequences * tiles of channels
+  int32_t warps;                                 // of a CTA
+  int32_t stages;                                // TILES: buffers of a warp, 1 to MAX_STAGES
+  int32_t* status;
 };
+struct Maps { CUtensorMap in[4], out; };          // f, x, (g), (dy); y
+
+// ---- two channels at once ----
+
+typedef unsigned long long two;
+__device__ __forceinline__ two pack2(float a, float b) { two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpack2(two v) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v)); return r; }
+__device__ __forceinline__ two mul2(two a, two b) { two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ two add2(two a, two b) { two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ two fma2(two a, two b, two c) { two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// Two elements as they are stored.
+template <typename T> struct Raw;
+template <> struct Raw<bf16> {
+  uint32_t v;
+  __device__ __forceinline__ two wide() const { return pack2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+  static __device__ __forceinline__ Raw of(two x) {
+    const float2 f = unpack2(x);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return {*reinterpret_cast<const uint32_t*>(&h)};
+  }
+  static __device__ __forceinline__ Raw of(bf16 a, bf16 b) { return {(uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(b) << 16}; }
+  __device__ __forceinline__ bf16 first() const { return __ushort_as_bfloat16((unsigned short)v); }
+  __device__ __forceinline__ bf16 second() const { return __ushort_as_bfloat16((unsigned short)(v >> 16)); }
+};
+template <> struct Raw<float> {
+  two v;
+  __device__ __forceinline__ two wide() const { return v; }
+  static __device__ __forceinline__ Raw of(two x) { return {x}; }
+  static __device__ __forceinline__ Raw of(float a, float b) { return {pack2(a, b)}; }
+  __device__ __forceinline__ float first() const { return unpack2(v).x; }
+  __device__ __forceinline__ float second() const { return unpack2(v).y; }
+};
+
+// sigmoid(f) and sigmoid(-f), both with a small relative error (where a is close to 1, 1 - a is what a channel forgets): with
+// e = exp(-f) they are 1 / (1 + e) and e / (1 + e).  bf16 inputs take the hardware's exponential and reciprocal (within 2^-21 + |f| 2^-23
+// of their values, against the 2^-8 of f's and the outputs' own rounding) and cut -f at 87, where a is 2^-126 and the other one 1;
+// min keeps a NaN.  Float inputs take the library's functions of |f|.
+template <typename T>
+__device__ __forceinline__ void gates(two f, two* a, two* rest) {
+  if constexpr (sizeof(T) == 2) {
+    const float2 t = unpack2(mul2(f, pack2(-1.4426950408889634f, -1.4426950408889634f)));
+    float t0, t1, e0, e1, r0, r1;
+    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t0) : "f"(t.x));               // 126
+    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t1) : "f"(t.y));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
+    const two e = pack2(e0, e1);
+    const float2 s = unpack2(add2(e, pack2(1.f, 1.f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(s.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(s.y));
+    *a = pack2(r0, r1);
+    *rest = mul2(e, *a);
+  } else {
+    const float2 v = unpack2(f);
+    float big[2], small[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float e = expf(-fabsf(i ? v.y : v.x));
+      big[i] = 1.f / (1.f + e);
+      small[i] = e * big[i];
+    }
+    *a = pack2(v.x < 0.f ? small[0] : big[0], v.y < 0.f ? small[1] : big[1]);
+    *rest = pack2(v.x < 0.f ? big[0] : small[0], v.y < 0.f ? big[1] : small[1]);
+  }
+}
+
+// ---- clusters ----
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
@@ -38,78 +122,81 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void store_remote(const float2* here, uint32_t rank, float2 v) {
-  uint32_t a = (uint32_t)__cvta_generic_to_shared(here), r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
-  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(r), "f"(v.x), "f"(v.y) : "memory");
-}
 
-// sigmoid(f) and sigmoid(-f), both with a small relative error (where a is close to 1, 1 - a is what a channel forgets): the
-// larger one is 1 / (1 + e) with e = exp(-|f|), the smaller one e times that.  bf16 inputs take the hardware's exponential and
-// reciprocal (4e-7 of the value at |f| = 8, against 2e-3 of f's and the outputs' own rounding), float inputs the library's.
-template <typename T>
-__device__ __forceinline__ void gates(float f, float* a, float* rest) {
-  float e, big;
-  if constexpr (sizeof(T) == 2) {
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(f) * -1.4426950408889634f));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(big) : "f"(1.f + e));
-  } else {
-    e = expf(-fabsf(f));
-    big = 1.f / (1.f + e);
+// (A, B) of a lane's two channels.
+struct alignas(16) Link { two a, b; };
+// To the same place of CTA `rank`, whose barrier at the place of `bar` counts the bytes: nothing else is waited for or flushed.
+__device__ __forceinline__ void send(const Link* here, uint32_t bar, uint32_t rank, const Link& v) {
+  uint32_t at, remote_bar;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(tc::smem_u32(here)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote_bar) : "r"(bar), "r"(rank));
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(at), "l"(v.a), "l"(v.b), "r"(remote_bar) : "memory");
+}
+// Bounded wait for what other CTAs sent.
+__device__ __forceinline__ void wait_sent(uint32_t bar, uint32_t parity, volatile int* gave_up, int32_t* status) {
+  const long long t0 = clock64();
+  for (int spins = 0;; ++spins) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return;
+    if ((spins & 255) == 255) {
+      if (*gave_up) return;
+      if (clock64() - t0 > tc::WAIT_CYCLES) {
+        *gave_up = 1;
+        if (atomicCAS(status, 0, 1) == 0) status[1] = 602;
+        return;
+      }
+    }
   }
-  const float small = e * big;
-  *a = f < 0.f ? small : big;
-  *rest = f < 0.f ? big : small;
-}
-// g sigmoid(g)
-template <typename T>
-__device__ __forceinline__ float silu(float g) { float s, r; gates<T>(g, &s, &r); return g * s; }
-
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> load_row(const T* p, bool live) {
-  Pack<T, V> v;
-  if (live) v = load_pack<T, V>(p);
-  else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v.e[i] = from_f32<T>(0.f);
-  }
-  return v;
 }
 
-// The same value, of which the compiler knows nothing: what was worked out from it before is worked out again instead of
-// being kept in registers that are not there.
-template <typename P>
-__device__ __forceinline__ void forget(P& v) {
-  if constexpr (sizeof(P) == 2) asm volatile("" : "+h"(reinterpret_cast<unsigned short&>(v)));
-  else asm volatile("" : "+r"(reinterpret_cast<unsigned&>(v)));
-}
+// What warps and CTAs tell one another, in the order of joining.  Two of each in turn: a place is written again two rounds
+// later, by a warp (or for a CTA) that has seen every warp of this CTA pass the barrier of the round between, after its reading.
+struct Exchange {
+  Link* mem;                                     // [2][warps][32] of the CTA's warps, then [2][CTAs][32]
+  int n_warps, n_ctas;
+  uint32_t bars;                                 // two barriers, of what the CTAs send
+  volatile int* gave_up;
+  int32_t* status;
+  __device__ __forceinline__ Link* warps(int parity) const { return mem + parity * n_warps * 32; }
+  __device__ __forceinline__ Link* ctas(int parity) const { return mem + (2 * n_warps + parity * n_ctas) * 32; }
+};
 
-// Which stretch of which sequence a warp works on.
-template <int V, bool CLUSTER>
+// Which stretches of which sequence a warp works on.
+template <int ROWS, bool CLUSTER>
 struct Place {
-  int warp, lane, unit, seq, channel, slot, n;   // slot: place in time among the warps that share the sequence
+  int warp, lane, seq, tile, slot, n;            // slot: place in time among the warps that share the sequence
   uint32_t rank, ctas;
-  int64_t lo;                                    // first row
-  int64_t block0;                                // first kept state
-  bool channel_live;
-  int span;                                      // tokens of a round
+  int64_t lo, block0;                            // first row, first kept state
+  int c0;                                        // first of the lane's channels
+  bool live0, live1;
+  int span, rounds;                              // tokens of a round
+  static constexpr int STEP = ROWS == SINGLES ? 32 : 1;          // from the first channel to the second
   __device__ __forceinline__ bool set(const RecurrenceParams& p) {
-    warp = threadIdx.x / 32; lane = threadIdx.x % 32;
+    warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0);
+    lane = threadIdx.x % 32;
+    int unit;
     if (CLUSTER) {
       rank = cluster_rank(); ctas = cluster_size();
       unit = blockIdx.x / ctas;
-      slot = rank * WARPS + warp;
-      span = ctas * WARPS * STEPS;
+      slot = rank * p.warps + warp;
+      span = ctas * p.warps * STEPS;
     } else {
       rank = 0; ctas = 1;
-      unit = blockIdx.x * WARPS + warp;
+      unit = blockIdx.x * p.warps + warp;
       slot = 0;
       span = STEPS;
       if (unit >= p.units) return false;
     }
     seq = unit / p.tiles;
-    channel = ((unit - seq * p.tiles) * 32 + lane) * V;
-    channel_live = channel < p.d;
+    tile = unit - seq * p.tiles;
+    c0 = tile * CHANNELS + (ROWS == SINGLES ? lane : 2 * lane);
+    live0 = c0 < p.d;
+    live1 = c0 + STEP < p.d;
     if (p.offsets) {
       const int a = min(max(p.offsets[seq], 0), p.rows), b = min(max(p.offsets[seq + 1], a), p.rows);
       lo = a; n = b - a;
@@ -117,256 +204,443 @@ struct Place {
       lo = (int64_t)seq * p.seq; n = p.seq;
     }
     block0 = lo / STEPS + seq;
+    rounds = (n + span - 1) / span;
     return true;
   }
-};
-
-// What the warps and CTAs of a cluster tell one another: (A, B) of each warp, and of each CTA.  Two of each in turn, so that one
-// barrier a round is enough: nobody writes a place again before all have passed the barrier after its reading.
-template <int V>
-struct Exchange {
-  float2 warps[2][WARPS][32 * V];
-  float2 ctas[2][MAX_CLUSTER][32 * V];
-};
-
-// Joins the stretches of a round.  (A, B): this warp's; carry: the state before the round, afterwards the state behind it;
-// returns the state before this warp's stretch in `start`.  FORWARD: earlier slots come first; else later ones.
-template <int V, bool FORWARD>
-__device__ __forceinline__ void join(Exchange<V>& ex, const Place<V, true>& at, int parity, const float* A, const float* B, float* carry, float* start) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) ex.warps[parity][at.warp][at.lane * V + v] = make_float2(A[v], B[v]);
-  __syncthreads();
-  float pa[V], pb[V], ta[V], tb[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) { pa[v] = ta[v] = 1.f; pb[v] = tb[v] = 0.f; }
-#pragma unroll
-  for (int i = 0; i < WARPS; ++i) {
-    const int w = FORWARD ? i : WARPS - 1 - i;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (w == at.warp) { pa[v] = ta[v]; pb[v] = tb[v]; }
-      const float2 s = ex.warps[parity][w][at.lane * V + v];
-      ta[v] *= s.x;
-      tb[v] = fmaf(s.x, tb[v], s.y);
+  __device__ __forceinline__ two load_state(const float* row) const {
+    return pack2(live0 ? row[c0] : 0.f, live1 ? row[c0 + STEP] : 0.f);
+  }
+  __device__ __forceinline__ void store_state(float* row, two v) const {
+    const float2 f = unpack2(v);
+    if (ROWS != SINGLES) { if (live0) *reinterpret_cast<float2*>(row + c0) = f; }
+    else { if (live0) row[c0] = f.x; if (live1) row[c0 + STEP] = f.y; }
+  }
+  template <typename T>
+  __device__ __forceinline__ Raw<T> load(const T* at, bool row) const {      // at: the lane's first channel
+    if (ROWS != SINGLES) {
+      Raw<T> r = Raw<T>::of(0ull);
+      if (live0 && row) r = *reinterpret_cast<const Raw<T>*>(at);
+      return r;
     }
+    return Raw<T>::of(live0 && row ? at[0] : from_f32<T>(0.f), live1 && row ? at[STEP] : from_f32<T>(0.f));
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* at, Raw<T> v) const {
+    if (ROWS != SINGLES) { if (live0) *reinterpret_cast<Raw<T>*>(at) = v; }
+    else { if (live0) at[0] = v.first(); if (live1) at[STEP] = v.second(); }
+  }
+};
+
+// Joins the stretches of a round: mine is this warp's; carry: the state before the round, afterwards the one behind it; start: the
+// state before this warp's stretch.  FORWARD: earlier slots come first; else later ones.
+template <bool FORWARD, typename P>
+__device__ __forceinline__ void join(const Exchange& ex, const P& at, int round, const Link& mine, two& carry, two& start) {
+  const int parity = round & 1;
+  const int me = FORWARD ? at.warp : ex.n_warps - 1 - at.warp;
+  Link* const warps = ex.warps(parity) + at.lane;
+  Link* const ctas = ex.ctas(parity) + at.lane;
+  warps[me * 32] = mine;
+  __syncthreads();
+  // the warps before this one; the last warp then knows the CTA's
+  Link all{pack2(1.f, 1.f), pack2(0.f, 0.f)};
+  const int upto = at.ctas == 1 ? ex.n_warps : me;
+  two a0 = all.a, b0 = all.b;
+#pragma unroll 4
+  for (int i = 0; i < upto; ++i) {
+    if (i == me) { a0 = all.a; b0 = all.b; }
+    const Link s = warps[i * 32];
+    all.a = mul2(all.a, s.a);
+    all.b = fma2(s.a, all.b, s.b);
   }
   if (at.ctas == 1) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) { start[v] = fmaf(pa[v], carry[v], pb[v]); carry[v] = fmaf(ta[v], carry[v], tb[v]); }
+    start = fma2(a0, carry, b0);
+    carry = fma2(all.a, carry, all.b);
     return;
   }
-  for (uint32_t r = at.warp; r < at.ctas; r += WARPS) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) store_remote(&ex.ctas[parity][at.rank][at.lane * V + v], r, make_float2(ta[v], tb[v]));
+  const uint32_t my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
+  const uint32_t bar = ex.bars + 8 * parity;
+  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
+  if (me == ex.n_warps - 1) {
+    const Link cta{mul2(all.a, mine.a), fma2(mine.a, all.b, mine.b)};
+    for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, cta);
   }
-  cluster_sync();
-  for (uint32_t i = 0; i < at.ctas; ++i) {
-    const uint32_t c = FORWARD ? i : at.ctas - 1 - i;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (c == at.rank) start[v] = fmaf(pa[v], carry[v], pb[v]);
-      const float2 s = ex.ctas[parity][c][at.lane * V + v];
-      carry[v] = fmaf(s.x, carry[v], s.y);
-    }
+  wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status);
+  two before = carry;
+#pragma unroll 4
+  for (uint32_t c = 0; c < at.ctas; ++c) {
+    if (c == my_cta) before = carry;
+    const Link s = ctas[c * 32];
+    carry = fma2(s.a, carry, s.b);
   }
+  start = fma2(all.a, before, all.b);
 }
 
-template <typename T, int V, bool GATE, bool COMPLEMENT, bool CLUSTER>
-__global__ void __launch_bounds__(WARPS * 32, 2) recurrence_forward_kernel(const RecurrenceParams p) {
-  __shared__ Exchange<V> ex;                      // of clusters only
-  if (CLUSTER && cluster_size() > 1) cluster_sync();                             // the others run: their shared memory can be written
-  fax_grid_dependency_wait();
-  Place<V, CLUSTER> at;
-  if (!at.set(p)) return;
-  const int64_t sc = (int64_t)at.seq * p.d + at.channel;
-  float carry[V];
+// ---- rows coming in ----
+
+template <typename T> constexpr int box_bytes() { return STEPS * CHANNELS * (int)sizeof(T); }
+
+// N tensors' rows of one stretch, in a warp's buffer of N boxes of STEPS x CHANNELS elements, a lane's two side by side.
+template <typename T, int N>
+struct Inputs {
+  uint8_t* at;                                   // this lane's pair of row 0
+  template <int K>
+  __device__ __forceinline__ Raw<T>* place(int i) const { return reinterpret_cast<Raw<T>*>(at + K * box_bytes<T>() + i * CHANNELS * (int)sizeof(T)); }
+  __device__ __forceinline__ two get(int k, int i) const { return reinterpret_cast<const Raw<T>*>(at + k * box_bytes<T>() + i * CHANNELS * (int)sizeof(T))->wide(); }
+  // PAIRS and SINGLES: through registers, R rows' loads on their way together.
+  template <int R, typename P>
+  __device__ __forceinline__ void fetch(const P& pl, const T* const (&src)[N], const int64_t (&ld)[N], int64_t row, int from, int count) const {
+    Raw<T> r[N][R];
 #pragma unroll
-  for (int v = 0; v < V; ++v) carry[v] = at.channel_live && p.h0 ? p.h0[sc + v] : 0.f;
-  int parity = 0;
-  for (int t0 = 0; t0 < at.n; t0 += at.span, parity ^= 1) {
-    const int ts = t0 + at.slot * STEPS;
-    const int left = at.channel_live ? at.n - ts : 0;           // tokens of this thread's stretch: those up to `left`
-    const int64_t row = at.lo + ts;
-    const T* pf = (const T*)p.f + row * p.ldf + at.channel;
-    const T* px = (const T*)p.x + row * p.ldx + at.channel;
-    const T* pg = GATE ? (const T*)p.g + row * p.ldg + at.channel : nullptr;
-    Pack<T, V> f[STEPS], x[STEPS], g[STEPS];
+    for (int k = 0; k < N; ++k) {
+      const T* q = src[k] + (row + from) * ld[k] + pl.c0;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      f[i] = load_row<T, V>(pf + i * p.ldf, i < left);
-      x[i] = load_row<T, V>(px + i * p.ldx, i < left);
-      if (GATE) g[i] = load_row<T, V>(pg + i * p.ldg, i < left);
+      for (int i = 0; i < R; ++i) {
+        r[k][i] = pl.load(q, from + i < count);
+        q += ld[k];
+      }
     }
-    T* py = (T*)p.y + row * p.ldy + at.channel;
-    float* state = p.states + (at.block0 + ts / STEPS) * p.d + at.channel;
-    const bool keep = p.states && left > 0;
-    if constexpr (CLUSTER) {
-      float a[STEPS][V], b[STEPS][V], A[V], B[V], h[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) { A[v] = 1.f; B[v] = 0.f; }
+    for (int k = 0; k < N; ++k)
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i)
+      for (int i = 0; i < R; ++i) *reinterpret_cast<Raw<T>*>(at + k * box_bytes<T>() + (from + i) * CHANNELS * (int)sizeof(T)) = r[k][i];
+  }
+  template <typename P>
+  __device__ __forceinline__ void fetch(const P& pl, const T* const (&src)[N], const int64_t (&ld)[N], int64_t row, int count) const {
+    if (count > 4) fetch<STEPS>(pl, src, ld, row, 0, count);
+    else if (count > 1) fetch<4>(pl, src, ld, row, 0, count);
+    else if (count == 1) fetch<1>(pl, src, ld, row, 0, count);
+  }
+};
+
+// A warp's buffers, in turn, and the barriers that say they are full.  Rows are asked for as many rounds ahead as there are other
+// buffers; a buffer is asked for again when every lane has read it and what was stored from it has left.
+template <typename T, int N>
+struct Tiles {
+  uint32_t bar, phase;                           // barriers, their phases
+  uint8_t* buf;
+  int stages, now;                               // buffers, the current round's one
+  __device__ __forceinline__ void init(uint8_t* buffers, uint64_t* bars, int n, int lane) {
+    buf = buffers; bar = tc::smem_u32(bars); phase = 0; stages = n; now = 0;
+    if (lane == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float rest;
-          gates<T>(to_f32(f[i].e[v]), &a[i][v], &rest);
-          b[i][v] = COMPLEMENT ? rest * to_f32(x[i].e[v]) : to_f32(x[i].e[v]);
-          if (i >= left) { a[i][v] = 1.f; b[i][v] = 0.f; }
-          A[v] *= a[i][v];
-          B[v] = fmaf(a[i][v], B[v], b[i][v]);
-        }
-      join<V, true>(ex, at, parity, A, B, carry, h);
-      if (keep) {
+      for (int i = 0; i < MAX_STAGES; ++i) tc::mbar_init(bar + 8 * i, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ uint8_t* current() const { return buf + now * N * box_bytes<T>(); }
+  // The rows of `ahead` rounds from now, when lane 0's stores have left their buffers.
+  __device__ __forceinline__ void ask(const Maps& maps, int ahead, int col, int64_t row, int lane) {
+    int s = now + ahead;
+    s = s >= stages ? s - stages : s;
+    __syncwarp();
+    if (lane == 0) {
+      tc::bulk_wait_read_all();
+      tc::mbar_expect_tx(bar + 8 * s, N * box_bytes<T>());
 #pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = h[v];
-      }
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        Pack<T, V> y;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          h[v] = fmaf(a[i][v], h[v], b[i][v]);
-          y.e[v] = from_f32<T>(GATE ? h[v] * silu<T>(to_f32(g[i].e[v])) : h[v]);
-        }
-        if (i < left) store_pack<T, V>(py + i * p.ldy, y);
-      }
+      for (int k = 0; k < N; ++k) tc::tma_load_2d(tc::smem_u32(buf + (s * N + k) * box_bytes<T>()), &maps.in[k], bar + 8 * s, col, (int)row);
+    }
+  }
+  // Bounded; a wait that runs out sets the context's status, and the work goes on with what is there so that nobody waits for this warp.
+  __device__ __forceinline__ void wait(volatile int* gave_up, int32_t* status) {
+    tc::mbar_wait_warp(bar + 8 * now, (phase >> now) & 1, gave_up, status, 601);
+    phase ^= 1u << now;
+  }
+  __device__ __forceinline__ void next() { now = now + 1 == stages ? 0 : now + 1; }
+};
+// Before what the lanes wrote to shared memory is stored by lane 0.
+__device__ __forceinline__ void written() { tc::fence_proxy_async(); __syncwarp(); }
+
+__host__ __device__ constexpr int align128(int n) { return (n + 127) / 128 * 128; }
+// Shared memory: the exchange of a cluster (its bytes), its two barriers and each warp's, then the warps' buffers (their place).
+template <bool CLUSTER> __host__ __device__ constexpr int exchange_bytes(int warps, int ctas) { return CLUSTER ? 2 * (warps + ctas) * 32 * (int)sizeof(Link) : 0; }
+template <bool CLUSTER> __host__ __device__ constexpr int buffers_at(int warps, int ctas) { return align128(exchange_bytes<CLUSTER>(warps, ctas) + 16 + warps * 8 * MAX_STAGES); }
+
+template <typename T, int ROWS, bool GATE, bool COMPLEMENT, bool CLUSTER>
+__global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(const __grid_constant__ Maps maps, const RecurrenceParams p) {
+  constexpr int N = 2 + GATE;
+  extern __shared__ __align__(128) uint8_t mem[];
+  __shared__ int gave_up;
+  const int ctas = CLUSTER ? (int)cluster_size() : 1;
+  const Exchange ex{reinterpret_cast<Link*>(mem), p.warps, ctas, tc::smem_u32(mem + exchange_bytes<CLUSTER>(p.warps, ctas)), &gave_up, p.status};
+  const int warp_buffer = p.stages * N * box_bytes<T>();
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    if (CLUSTER) {
+      tc::mbar_init(ex.bars, 1);
+      tc::mbar_init(ex.bars + 8, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+  }
+  Tiles<T, N> tiles;
+  uint8_t* const buffer = mem + buffers_at<CLUSTER>(p.warps, ctas) + (threadIdx.x / 32) * warp_buffer;
+  if (ROWS == TILES)
+    tiles.init(buffer, reinterpret_cast<uint64_t*>(mem + exchange_bytes<CLUSTER>(p.warps, ctas) + 16) + threadIdx.x / 32 * MAX_STAGES,
+               p.stages, threadIdx.x % 32);
+  __syncthreads();
+  if (CLUSTER && ctas > 1) cluster_sync();             // the others run: their shared memory can be written
+  fax_grid_dependency_wait();
+  Place<ROWS, CLUSTER> at;
+  if (!at.set(p)) return;
+  const int64_t seq_row = (int64_t)at.seq * p.d;
+  two carry = p.h0 ? at.load_state(p.h0 + seq_row) : 0ull;
+  const T* src[N]; int64_t ld[N];
+  src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
+  if constexpr (GATE) { src[2] = (const T*)p.g; ld[2] = p.ldg; }
+
+  const int first = at.slot * STEPS;
+  auto tokens = [&](int round) { return round < at.rounds ? min(max(at.n - (round * at.span + first), 0), STEPS) : 0; };
+  const int ahead = p.stages - 1;
+  auto ask = [&](int round, int by) {
+    if (tokens(round) > 0) tiles.ask(maps, by, at.tile * CHANNELS, at.lo + (int64_t)round * at.span + first, at.lane);
+  };
+  if (ROWS == TILES)
+    for (int i = 0; i < max(ahead, 1); ++i) ask(i, i);
+  for (int round = 0; round < at.rounds; ++round) {
+    const int count = tokens(round);
+    const int64_t row = at.lo + (int64_t)round * at.span + first;
+    Inputs<T, N> in;
+    if constexpr (ROWS == TILES) {
+      if (count > 0) tiles.wait(&gave_up, p.status);
+      in.at = tiles.current() + at.lane * 2 * sizeof(T);
     } else {
-      if (keep) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = carry[v];
-      }
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        if (i >= left) break;
-        Pack<T, V> y;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float a, rest;
-          gates<T>(to_f32(f[i].e[v]), &a, &rest);
-          carry[v] = fmaf(a, carry[v], COMPLEMENT ? rest * to_f32(x[i].e[v]) : to_f32(x[i].e[v]));
-          y.e[v] = from_f32<T>(GATE ? carry[v] * silu<T>(to_f32(g[i].e[v])) : carry[v]);
+      in.at = buffer + at.lane * 2 * sizeof(T);
+      in.fetch(at, src, ld, row, count);
+    }
+    T* out = (T*)p.y + row * p.ldy + at.c0;
+    float* kept = p.states && count > 0 ? p.states + (at.block0 + (row - at.lo) / STEPS) * p.d : nullptr;
+    // FULL: a whole stretch, nothing to look at token by token
+    auto work = [&](auto full) {
+      constexpr bool FULL = decltype(full)::value, BOX = FULL && ROWS == TILES;
+      // y goes out in the place of f
+      auto put = [&](int i, two h) {
+        two y = h;
+        if constexpr (GATE) {
+          const two g = in.get(2, i);
+          two s, r;
+          gates<T>(g, &s, &r);
+          y = mul2(h, mul2(g, s));
         }
-        store_pack<T, V>(py + i * p.ldy, y);
+        if constexpr (BOX) *in.template place<0>(i) = Raw<T>::of(y);
+        else at.store(out + i * p.ldy, Raw<T>::of(y));
+      };
+      if constexpr (CLUSTER) {
+        two a[STEPS], b[STEPS], h;
+        Link mine{pack2(1.f, 1.f), pack2(0.f, 0.f)};
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          a[i] = pack2(1.f, 1.f); b[i] = 0ull;
+          if (FULL || i < count) {
+            two rest;
+            gates<T>(in.get(0, i), &a[i], &rest);
+            b[i] = COMPLEMENT ? mul2(rest, in.get(1, i)) : in.get(1, i);
+            mine.a = mul2(mine.a, a[i]);
+            mine.b = fma2(a[i], mine.b, b[i]);
+          }
+        }
+        if (ROWS == TILES && ahead > 0) ask(round + ahead, ahead);
+        join<true>(ex, at, round, mine, carry, h);
+        if (kept) at.store_state(kept, h);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+          if (FULL || i < count) {
+            h = fma2(a[i], h, b[i]);
+            put(i, h);
+          }
+      } else {
+        if (kept) at.store_state(kept, carry);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+          if (FULL || i < count) {
+            two a, rest;
+            gates<T>(in.get(0, i), &a, &rest);
+            carry = fma2(a, carry, COMPLEMENT ? mul2(rest, in.get(1, i)) : in.get(1, i));
+            put(i, carry);
+          }
+          if (ROWS == TILES && i == STEPS / 2 && ahead > 0) ask(round + ahead, ahead);
+        }
       }
+      if constexpr (BOX) {
+        written();
+        if (at.lane == 0) {
+          tc::tma_store_2d(&maps.out, tc::smem_u32(tiles.current()), at.tile * CHANNELS, (int)row);
+          tc::bulk_commit_group();
+        }
+      }
+    };
+    if (count == STEPS) work(std::true_type{}); else work(std::false_type{});
+    if constexpr (ROWS == TILES) {
+      if (ahead == 0) ask(round + 1, 0);
+      tiles.next();
     }
   }
-  if (p.h_last && at.slot == 0 && at.channel_live) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) p.h_last[sc + v] = carry[v];
-  }
+  if (ROWS == TILES && at.lane == 0) tc::bulk_wait_all();
+  if (p.h_last && at.slot == 0) at.store_state(p.h_last + seq_row, carry);
 }
 
-template <typename T, int V, bool GATE, bool COMPLEMENT, bool CLUSTER>
-__global__ void __launch_bounds__(WARPS * 32, 2) recurrence_backward_kernel(const RecurrenceParams p) {
-  __shared__ Exchange<V> ex;
-  __shared__ float before[STEPS][WARPS][32 * V];  // h before each token: a thread's own places (kept in registers beside four rows of inputs they spill)
-  if (CLUSTER && cluster_size() > 1) cluster_sync();
-  fax_grid_dependency_wait();
-  Place<V, CLUSTER> at;
-  if (!at.set(p)) return;
-  const int64_t sc = (int64_t)at.seq * p.d + at.channel;
-  float carry[V];                                                // e behind the round: what its last token receives
-#pragma unroll
-  for (int v = 0; v < V; ++v) carry[v] = at.channel_live && p.dh_last ? p.dh_last[sc + v] : 0.f;
-  int parity = 0;
-  for (int t0 = at.n > 0 ? (at.n - 1) / at.span * at.span : -1; t0 >= 0; t0 -= at.span, parity ^= 1) {
-    const int ts = t0 + at.slot * STEPS;
-    const int left = at.channel_live ? at.n - ts : 0;
-    const int64_t row = at.lo + ts;
-    const T* pf = (const T*)p.f + row * p.ldf + at.channel;
-    const T* px = (const T*)p.x + row * p.ldx + at.channel;
-    const T* pg = GATE ? (const T*)p.g + row * p.ldg + at.channel : nullptr;
-    const T* pdy = (const T*)p.dy + row * p.lddy + at.channel;
-    Pack<T, V> f[STEPS], x[STEPS], g[STEPS], dy[STEPS];
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-      f[i] = load_row<T, V>(pf + i * p.ldf, i < left);
-      x[i] = load_row<T, V>(px + i * p.ldx, i < left);
-      if (GATE) g[i] = load_row<T, V>(pg + i * p.ldg, i < left);
-      dy[i] = load_row<T, V>(pdy + i * p.lddy, i < left);
+// What the backward pass keeps of a token between its walks over a stretch, in the buffer its inputs were in: w, what h_{t-1} (and x) make of dh in df, and with a gate u.  A lane's own places throughout.
+template <typename T>
+struct Kept {
+  uint8_t* at;                                   // this lane's pair of row 0
+  static constexpr bool WIDE = sizeof(T) == 4;   // a pair's place holds two floats; else it takes two boxes' places
+  static constexpr int ROW = CHANNELS * (int)sizeof(T), BOX = box_bytes<T>();
+  __device__ __forceinline__ void put(int box, int i, two v) const {
+    if constexpr (WIDE) {
+      *reinterpret_cast<two*>(at + box / 2 * BOX + i * ROW) = v;
+    } else {
+      const float2 f = unpack2(v);
+      *reinterpret_cast<float*>(at + box * BOX + i * ROW) = f.x;
+      *reinterpret_cast<float*>(at + (box + 1) * BOX + i * ROW) = f.y;
     }
-    float h[V];
-    const float* s = p.states + (at.block0 + ts / STEPS) * p.d + at.channel;
+  }
+  __device__ __forceinline__ two get(int box, int i) const {
+    if constexpr (WIDE) return *reinterpret_cast<const two*>(at + box / 2 * BOX + i * ROW);
+    else return pack2(*reinterpret_cast<const float*>(at + box * BOX + i * ROW), *reinterpret_cast<const float*>(at + (box + 1) * BOX + i * ROW));
+  }
+  __device__ __forceinline__ void put_w(int i, two v) const { put(0, i, v); }
+  __device__ __forceinline__ two get_w(int i) const { return get(0, i); }
+  __device__ __forceinline__ void put_u(int i, two v) const { put(2, i, v); }
+  __device__ __forceinline__ two get_u(int i) const { return get(2, i); }
+};
+
+template <typename T, int ROWS, bool GATE, bool COMPLEMENT, bool CLUSTER>
+__global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(const __grid_constant__ Maps maps, const RecurrenceParams p) {
+  constexpr int N = 3 + GATE, DY = 2 + GATE;
+  extern __shared__ __align__(128) uint8_t mem[];
+  __shared__ int gave_up;
+  const int ctas = CLUSTER ? (int)cluster_size() : 1;
+  const Exchange ex{reinterpret_cast<Link*>(mem), p.warps, ctas, tc::smem_u32(mem + exchange_bytes<CLUSTER>(p.warps, ctas)), &gave_up, p.status};
+  const int warp_buffer = p.stages * N * box_bytes<T>();
+  uint8_t* const buffer = mem + buffers_at<CLUSTER>(p.warps, ctas) + (threadIdx.x / 32) * warp_buffer;
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    if (CLUSTER) {
+      tc::mbar_init(ex.bars, 1);
+      tc::mbar_init(ex.bars + 8, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+  }
+  Tiles<T, N> tiles;
+  if (ROWS == TILES) tiles.init(buffer, reinterpret_cast<uint64_t*>(mem + exchange_bytes<CLUSTER>(p.warps, ctas) + 16) + threadIdx.x / 32 * MAX_STAGES, p.stages, threadIdx.x % 32);
+  __syncthreads();
+  if (CLUSTER && ctas > 1) cluster_sync();
+  fax_grid_dependency_wait();
+  Place<ROWS, CLUSTER> at;
+  if (!at.set(p)) return;
+  const int64_t seq_row = (int64_t)at.seq * p.d;
+  two carry = p.dh_last ? at.load_state(p.dh_last + seq_row) : 0ull;          // e behind the round: what its last token receives
+  const T* src[N]; int64_t ld[N];
+  src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
+  if constexpr (GATE) { src[2] = (const T*)p.g; ld[2] = p.ldg; }
+  src[DY] = (const T*)p.dy; ld[DY] = p.lddy;
+
+  // round 0 is the sequence's last one
+  const int first = at.slot * STEPS;
+  auto begin = [&](int round) { return (at.rounds - 1 - round) * at.span + first; };
+  auto tokens = [&](int round) { return round < at.rounds ? min(max(at.n - begin(round), 0), STEPS) : 0; };
+  const int ahead = p.stages - 1;
+  auto ask = [&](int round, int by) {
+    if (tokens(round) > 0) tiles.ask(maps, by, at.tile * CHANNELS, at.lo + begin(round), at.lane);
+  };
+  if (ROWS == TILES)
+    for (int i = 0; i < max(ahead, 1); ++i) ask(i, i);
+  for (int round = 0; round < at.rounds; ++round) {
+    const int count = tokens(round);
+    const int64_t row = at.lo + begin(round);
+    Inputs<T, N> in;
+    Kept<T> kept;
+    two before = count > 0 ? at.load_state(p.states + (at.block0 + begin(round) / STEPS) * p.d) : 0ull;
+    if constexpr (ROWS == TILES) {
+      if (ahead > 0) ask(round + ahead, ahead);
+      if (count > 0) tiles.wait(&gave_up, p.status);
+      in.at = tiles.current() + at.lane * 2 * sizeof(T);
+    } else {
+      in.at = buffer + at.lane * 2 * sizeof(T);
+      in.fetch(at, src, ld, row, count);
+    }
+    kept.at = in.at;
+    // rows are stored a pitch apart; the last walk goes from the end
+    auto row_of = [&](void* base, int64_t pitch, int i) { return (T*)base + (row + i) * pitch + at.c0; };
+    auto work = [&](auto full) {
+      constexpr bool FULL = decltype(full)::value;
+      two a[STEPS], rest[STEPS];
+      [[maybe_unused]] T* dg = GATE ? row_of(p.dg, p.lddg, 0) : nullptr;
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = left > 0 ? s[v] : 0.f;
-    float e[V];
-#pragma unroll
-    for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        before[i][at.warp][at.lane * V + v] = h[v];
-        float a, rest;
-        gates<T>(to_f32(f[i].e[v]), &a, &rest);
-        h[v] = fmaf(a, h[v], COMPLEMENT ? rest * to_f32(x[i].e[v]) : to_f32(x[i].e[v]));
+      for (int i = 0; i < STEPS; ++i) {
+        a[i] = pack2(1.f, 1.f); rest[i] = 0ull;
+        if (FULL || i < count) {
+          gates<T>(in.get(0, i), &a[i], &rest[i]);
+          const two x = in.get(1, i);
+          const two h = fma2(a[i], before, COMPLEMENT ? mul2(rest[i], x) : x);
+          const two w = COMPLEMENT ? fma2(x, pack2(-1.f, -1.f), before) : before;
+          if constexpr (GATE) {
+            const two g = in.get(2, i), dy = in.get(DY, i);
+            two s, r;
+            gates<T>(g, &s, &r);
+            const two gs = mul2(g, s);
+            at.store(dg, Raw<T>::of(mul2(mul2(dy, h), fma2(gs, r, s))));
+            dg += p.lddg;
+            kept.put_u(i, mul2(dy, gs));
+          }
+          kept.put_w(i, w);
+          before = h;
+        }
       }
-    if constexpr (CLUSTER) {
-      float A[V], B[V];                                           // the stretch's, from its end
+      auto u_of = [&](int i) { if constexpr (GATE) return kept.get_u(i); else return in.get(DY, i); };
+      two e = carry;
+      if constexpr (CLUSTER) {
+        Link mine{pack2(1.f, 1.f), pack2(0.f, 0.f)};               // the stretch's, from its end
 #pragma unroll
-      for (int v = 0; v < V; ++v) { A[v] = 1.f; B[v] = 0.f; }
+        for (int i = STEPS - 1; i >= 0; --i)
+          if (FULL || i < count) {
+            mine.a = mul2(mine.a, a[i]);
+            mine.b = mul2(a[i], add2(u_of(i), mine.b));
+          }
+        join<false>(ex, at, round, mine, carry, e);
+      }
+      const int last = (FULL ? STEPS : count) - 1;
+      T* df = row_of(p.df, p.lddf, last);
+      T* dx = row_of(p.dx, p.lddx, last);
 #pragma unroll
       for (int i = STEPS - 1; i >= 0; --i)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float a, rest;
-          if (v == 0) forget(f[i]);
-          gates<T>(to_f32(f[i].e[v]), &a, &rest);
-          const float u = GATE ? to_f32(dy[i].e[v]) * silu<T>(to_f32(g[i].e[v])) : to_f32(dy[i].e[v]);
-          if (i >= left) a = 1.f;                                 // u is 0 there
-          A[v] *= a;
-          B[v] = a * (u + B[v]);
+        if (FULL || i < count) {
+          const two dh = add2(u_of(i), e);
+          at.store(df, Raw<T>::of(mul2(mul2(dh, kept.get_w(i)), mul2(a[i], rest[i]))));
+          at.store(dx, Raw<T>::of(COMPLEMENT ? mul2(dh, rest[i]) : dh));
+          df -= p.lddf;
+          dx -= p.lddx;
+          e = mul2(a[i], dh);
         }
-      join<V, false>(ex, at, parity, A, B, carry, e);
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) e[v] = carry[v];
-    }
-    T* pdf = (T*)p.df + row * p.lddf + at.channel;
-    T* pdx = (T*)p.dx + row * p.lddx + at.channel;
-    T* pdg = GATE ? (T*)p.dg + row * p.lddg + at.channel : nullptr;
-#pragma unroll
-    for (int i = STEPS - 1; i >= 0; --i) {
-      Pack<T, V> df, dx, dg;
-      forget(f[i]);
-      if (GATE) forget(g[i]);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float a, rest, u = to_f32(dy[i].e[v]);
-        gates<T>(to_f32(f[i].e[v]), &a, &rest);
-        const float xv = to_f32(x[i].e[v]), hb = before[i][at.warp][at.lane * V + v];
-        if (GATE) {
-          const float gv = to_f32(g[i].e[v]);
-          float sg, sr;
-          gates<T>(gv, &sg, &sr);
-          const float ht = fmaf(a, hb, COMPLEMENT ? rest * xv : xv);
-          dg.e[v] = from_f32<T>(u * ht * fmaf(gv * sg, sr, sg));
-          u *= gv * sg;
-        }
-        const float dh = u + e[v];
-        df.e[v] = from_f32<T>(dh * (COMPLEMENT ? hb - xv : hb) * (a * rest));
-        dx.e[v] = from_f32<T>(COMPLEMENT ? dh * rest : dh);
-        if (i < left) e[v] = a * dh;
-      }
-      if (i < left) {
-        store_pack<T, V>(pdf + i * p.lddf, df);
-        store_pack<T, V>(pdx + i * p.lddx, dx);
-        if (GATE) store_pack<T, V>(pdg + i * p.lddg, dg);
-      }
-    }
-    if constexpr (!CLUSTER) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) carry[v] = e[v];
+      if (ROWS == TILES) tc::fence_proxy_async();                  // this lane wrote to the buffer, which is TMA's again
+      if constexpr (!CLUSTER) carry = e;
+    };
+    if (count == STEPS) work(std::true_type{}); else work(std::false_type{});
+    if constexpr (ROWS == TILES) {
+      if (ahead == 0) ask(round + 1, 0);
+      tiles.next();
     }
   }
-  if (p.dh0 && at.slot == 0 && at.channel_live) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) p.dh0[sc + v] = carry[v];
-  }
+  if (p.dh0 && at.slot == 0) at.store_state(p.dh0 + seq_row, carry);
 }
 
-// fax_launch, with clusters of `cluster` CTAs where there is more than one.
-fax_status launch(fax_ctx* ctx, void (*kernel)(RecurrenceParams), int64_t grid, int cluster, const RecurrenceParams& p) {
+template <bool BACKWARD, typename T, int ROWS, bool GATE, bool COMPLEMENT, bool CLUSTER>
+fax_status launch(fax_ctx* ctx, int64_t grid, int cluster, const Maps& maps, RecurrenceParams p) {
+  constexpr int N = 2 + GATE + BACKWARD;
+  auto kernel = [] {
+    if constexpr (BACKWARD) return recurrence_backward_kernel<T, ROWS, GATE, COMPLEMENT, CLUSTER>;
+    else return recurrence_forward_kernel<T, ROWS, GATE, COMPLEMENT, CLUSTER>;
+  }();
+  auto smem = [&](int stages) { return buffers_at<CLUSTER>(p.warps, cluster) + p.warps * stages * N * box_bytes<T>(); };
+  if (ROWS != TILES) p.stages = 1;
+  while (p.stages > 1 && smem(p.stages) > SMEM_MAX) --p.stages;
+  static bool done[FAX_MAX_DEVICES] = {}, wide[FAX_MAX_DEVICES] = {};
+  FAX_TRY(fax_opt_in_shared_memory(ctx, kernel, SMEM_MAX, done));
+  if (CLUSTER && cluster > 8 && !(ctx->device < FAX_MAX_DEVICES && wide[ctx->device])) {
+    FAX_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (ctx->device < FAX_MAX_DEVICES) wide[ctx->device] = true;
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(WARPS * 32); cfg.stream = ctx->stream;
+  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(p.warps * 32); cfg.dynamicSmemBytes = smem(p.stages); cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -374,43 +648,92 @@ fax_status launch(fax_ctx* ctx, void (*kernel)(RecurrenceParams), int64_t grid, 
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = ctx->use_pdl ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, p);          // errors surface in fax_after_launch
+  (void)cudaLaunchKernelEx(&cfg, kernel, maps, p);          // errors surface in fax_after_launch
   return fax_after_launch(ctx);
 }
 
-template <bool BACKWARD, typename T, int V, bool CLUSTER>
-void (*pick(bool gate, bool complement))(RecurrenceParams) {
-  if constexpr (BACKWARD) {
-    if (gate) return complement ? recurrence_backward_kernel<T, V, true, true, CLUSTER> : recurrence_backward_kernel<T, V, true, false, CLUSTER>;
-    return complement ? recurrence_backward_kernel<T, V, false, true, CLUSTER> : recurrence_backward_kernel<T, V, false, false, CLUSTER>;
-  } else {
-    if (gate) return complement ? recurrence_forward_kernel<T, V, true, true, CLUSTER> : recurrence_forward_kernel<T, V, true, false, CLUSTER>;
-    return complement ? recurrence_forward_kernel<T, V, false, true, CLUSTER> : recurrence_forward_kernel<T, V, false, false, CLUSTER>;
-  }
+template <bool BACKWARD, typename T, int ROWS, bool CLUSTER>
+fax_status launch(fax_ctx* ctx, bool complement, int64_t grid, int cluster, const Maps& maps, const RecurrenceParams& p) {
+  if (p.g) return complement ? launch<BACKWARD, T, ROWS, true, true, CLUSTER>(ctx, grid, cluster, maps, p) : launch<BACKWARD, T, ROWS, true, false, CLUSTER>(ctx, grid, cluster, maps, p);
+  return complement ? launch<BACKWARD, T, ROWS, false, true, CLUSTER>(ctx, grid, cluster, maps, p) : launch<BACKWARD, T, ROWS, false, false, CLUSTER>(ctx, grid, cluster, maps, p);
 }
 
+// Boxes of 16 rows x 64 columns, as they are in memory.
+bool make_map_rows(fax_ctx* ctx, CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int64_t ld, bool f32) {
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * (f32 ? 4 : 2)};
+  cuuint32_t box[2] = {CHANNELS, STEPS};
+  cuuint32_t estr[2] = {1, 1};
+  return ((tc::EncodeTiledFn)ctx->encode_tiled)(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)base, dims, strides, box, estr,
+                                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How warps share the work.
+struct Shape { bool alone; int warps, cluster; };
 template <bool BACKWARD>
-fax_status run(fax_ctx* ctx, int prec, RecurrenceParams p, bool complement, bool pairs) {
-  const int v = pairs ? 2 : 1;
-  p.tiles = (p.d + 32 * v - 1) / (32 * v);
+Shape shape_for(const fax_ctx* ctx, int64_t units, int seq) {
+  const int64_t sms = ctx->sm_count;
+  // A warp a sequence and tile: sequences of one stretch, or 12 warps an SM and more of them.
+  if (seq <= STEPS || units >= 12 * sms) {
+    // (backward, CTAs of 4 warps: 12 warps an SM; of 16, with one buffer each: 16)
+    auto rounds = [&](int64_t an_sm) { return (units + an_sm * sms - 1) / (an_sm * sms) * an_sm; };
+    return {true, BACKWARD && seq > 2 * STEPS && rounds(16) * 20 < rounds(12) * 19 ? 16 : 4, 1};
+  }
+  // Else CTAs of `warps`, a cluster of them a sequence and tile: as many warps as the SMs hold at once, and no more than the
+  // longest sequence has stretches for.  An SM holds 16 warps of the forward pass, 12 of the backward pass.
+  Shape best{false, 4, 1};
+  int64_t most = 0;
+  for (const int warps : {4, BACKWARD ? 6 : 8}) {
+    const int an_sm = BACKWARD ? 12 / warps : 16 / warps;
+    for (int cluster = 1; cluster <= MAX_CLUSTER; cluster *= 2) {
+      if (cluster > 1 && (cluster / 2) * warps * STEPS >= seq) break;
+      if (cluster > 1 && units * cluster > (cluster == 16 ? 112 : sms) * an_sm) break;                // (seven GPCs have 16 SMs for a cluster of 16)
+      const int64_t held = units * cluster > sms * an_sm ? sms * an_sm * warps : units * cluster * warps;
+      if (held > most || (held == most && best.cluster > 2 && cluster < best.cluster)) { best = {false, warps, cluster}; most = held; }
+    }
+  }
+  return best;
+}
+
+template <bool BACKWARD, typename T>
+fax_status run(fax_ctx* ctx, RecurrenceParams p, bool complement) {
+  p.tiles = (p.d + CHANNELS - 1) / CHANNELS;
   const int64_t units = (int64_t)p.n_seq * p.tiles;
   if (units > 0x7fffffff / MAX_CLUSTER) return FAX_ERR_UNSUPPORTED_SHAPE;
   p.units = (int32_t)units;
-  // A warp for each sequence and channel tile where that is 8 warps an SM or a sequence is one stretch; else CTAs up to
-  // two an SM, as far as the longest sequence has stretches of 128 tokens for them.
-  const bool alone = units >= 8 * ctx->sm_count || p.seq <= STEPS;
-  int cluster = 1;
-  while (!alone && cluster < MAX_CLUSTER && cluster * WARPS * STEPS < p.seq && units * cluster < 2 * ctx->sm_count) cluster *= 2;
-  const int64_t grid = alone ? (units + WARPS - 1) / WARPS : units * cluster;
-  const bool gate = p.g != nullptr;
-  void (*kernel)(RecurrenceParams);
-  if (prec == FAX_PREC_BF16) {
-    if (pairs) kernel = alone ? pick<BACKWARD, bf16, 2, false>(gate, complement) : pick<BACKWARD, bf16, 2, true>(gate, complement);
-    else kernel = alone ? pick<BACKWARD, bf16, 1, false>(gate, complement) : pick<BACKWARD, bf16, 1, true>(gate, complement);
-  } else {
-    kernel = alone ? pick<BACKWARD, float, 1, false>(gate, complement) : pick<BACKWARD, float, 1, true>(gate, complement);
+  p.status = ctx->dev_status;
+  const Shape shape = shape_for<BACKWARD>(ctx, units, p.seq);
+  const bool alone = shape.alone;
+  const int cluster = shape.cluster;
+  p.warps = shape.warps;
+  const int span = (alone ? 1 : cluster * p.warps) * STEPS;
+  p.stages = p.seq > span ? 2 : 1;
+  const int64_t grid = alone ? (units + p.warps - 1) / p.warps : units * cluster;
+
+  // Pairs of channels: addresses and pitches of whole pairs (states: of 8 bytes).  Boxes: of 16 bytes.
+  const size_t es = sizeof(T);
+  const void* const ins[4] = {p.f, p.x, p.g, p.dy};
+  const int64_t in_ld[4] = {p.ldf, p.ldx, p.ldg, p.lddy};
+  const void* const outs[4] = {p.y, p.df, p.dx, p.dg};
+  const int64_t out_ld[4] = {p.ldy, p.lddf, p.lddx, p.lddg};
+  bool pairs = p.d % 2 == 0, boxes = p.rows > 0;
+  for (int i = 0; i < 4; ++i) {
+    pairs = pairs && (!ins[i] || fax_rows_aligned(ins[i], in_ld[i], es, 2 * es)) && (!outs[i] || fax_rows_aligned(outs[i], out_ld[i], es, 2 * es));
+    boxes = boxes && (!ins[i] || (fax_rows_aligned(ins[i], in_ld[i], es, 16) && in_ld[i] * (int64_t)es < (1ll << 40))) ;
   }
-  return launch(ctx, kernel, grid, cluster, p);
+  boxes = boxes && (BACKWARD || (fax_rows_aligned(p.y, p.ldy, es, 16) && p.ldy * (int64_t)es < (1ll << 40)));
+  pairs = pairs && fax_aligned(p.h0, 8) && fax_aligned(p.dh_last, 8) && fax_aligned(p.h_last, 8) && fax_aligned(p.dh0, 8) && fax_aligned(p.states, 8);
+  Maps maps = {};
+  if (p.seq > STEPS && pairs && boxes) {
+    int n = 0;
+    for (int i = 0; i < 4; ++i)
+      if (ins[i] && !make_map_rows(ctx, &maps.in[n++], ins[i], p.d, p.rows, in_ld[i], es == 4)) return FAX_ERR_INVALID_ARG;
+    if (!BACKWARD && !make_map_rows(ctx, &maps.out, p.y, p.d, p.rows, p.ldy, es == 4)) return FAX_ERR_INVALID_ARG;
+    return alone ? launch<BACKWARD, T, TILES, false>(ctx, complement, grid, 1, maps, p) : launch<BACKWARD, T, TILES, true>(ctx, complement, grid, cluster, maps, p);
+  }
+  if (!alone) return launch<BACKWARD, T, SINGLES, true>(ctx, complement, grid, cluster, maps, p);
+  return pairs ? launch<BACKWARD, T, PAIRS, false>(ctx, complement, grid, 1, maps, p) : launch<BACKWARD, T, SINGLES, false>(ctx, complement, grid, 1, maps, p);
 }
 
 // Sizes, sequences and inputs that both passes share; `ok` with rows = 0 as well.
@@ -438,9 +761,6 @@ RecurrenceParams params(const D* d) {
   return p;
 }
 
-// Two bf16 channels a lane: even widths and pitches, addresses of whole pairs.
-bool pair(const void* p, int64_t ld) { return !p || fax_rows_aligned(p, ld, 2, 4); }
-
 }  // namespace
 
 extern "C" fax_status fax_op_recurrence_states_floats(int32_t rows, int32_t n_seq, int32_t d, size_t* floats) {
@@ -458,8 +778,8 @@ extern "C" fax_status fax_op_recurrence_forward(fax_ctx* ctx, int32_t prec, cons
   p.y = d->y; p.ldy = d->ldy; p.h_last = d->h_last; p.states = d->states;
   const double n = (double)d->rows * d->d, es = (double)fax_elem_size(prec);
   FaxProfScope prof(ctx, KC_RECURRENCE, 4.0 * n, (3.0 + (d->g != nullptr)) * n * es + (d->states ? n / 4 : 0.0));
-  const bool pairs = prec == FAX_PREC_BF16 && d->d % 2 == 0 && pair(d->f, d->ldf) && pair(d->x, d->ldx) && pair(d->g, d->ldg) && pair(d->y, d->ldy);
-  return run<false>(ctx, prec, p, d->input == FAX_RECURRENCE_COMPLEMENT, pairs);
+  const bool complement = d->input == FAX_RECURRENCE_COMPLEMENT;
+  return prec == FAX_PREC_BF16 ? run<false, bf16>(ctx, p, complement) : run<false, float>(ctx, p, complement);
 }
 
 extern "C" fax_status fax_op_recurrence_backward(fax_ctx* ctx, int32_t prec, const fax_recurrence_backward_desc* d) {
@@ -477,7 +797,6 @@ extern "C" fax_status fax_op_recurrence_backward(fax_ctx* ctx, int32_t prec, con
   p.df = d->df; p.lddf = d->lddf; p.dx = d->dx; p.lddx = d->lddx; p.dg = d->dg; p.lddg = d->lddg;
   const double n = (double)d->rows * d->d, es = (double)esz;
   FaxProfScope prof(ctx, KC_RECURRENCE, 10.0 * n, (5.0 + 2.0 * (d->g != nullptr)) * n * es + n / 4);
-  const bool pairs = prec == FAX_PREC_BF16 && d->d % 2 == 0 && pair(d->f, d->ldf) && pair(d->x, d->ldx) && pair(d->g, d->ldg) && pair(d->dy, d->lddy) &&
-                     pair(d->df, d->lddf) && pair(d->dx, d->lddx) && (!d->g || pair(d->dg, d->lddg));
-  return run<true>(ctx, prec, p, d->input == FAX_RECURRENCE_COMPLEMENT, pairs);
+  const bool complement = d->input == FAX_RECURRENCE_COMPLEMENT;
+  return prec == FAX_PREC_BF16 ? run<true, bf16>(ctx, p, complement) : run<true, float>(ctx, p, complement);
 }
