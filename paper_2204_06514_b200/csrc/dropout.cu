@@ -1,9 +1,9 @@
 // Dropout whose mask is never stored: y = resid + (kept ? x / (1 - p) : 0) (see fax_ops.h for the bits).
 //
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
-// 32 x 32 -> 64 bit products over a counter of four words.  One counter gives the 16 bits of eight elements, which are one
-// 16-byte vector of bf16, so that a thread draws once for what it loads: about 6 integer instructions an element beside 4
-// to 6 bytes of traffic, which bound the kernel.
+// 32 x 32 -> 64 bit products over a counter of four words; the rounds' keys are the same for all and come with the launch.
+// One counter gives the 16 bits of eight elements, which are one 16-byte vector of bf16, so that a thread draws once for what
+// it loads.  Memory bounds it, the instructions come next: some 13 an element beside 4 to 6 bytes of traffic.
 #include <cmath>
 
 #include "stream_common.cuh"
@@ -12,94 +12,123 @@
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int UNITS = 2;           // groups of eight columns a thread has in flight
+constexpr int ROUNDS = 10;
 
 struct DropoutParams {
   const void* x; const void* resid; void* y;
   int64_t ldx, ldr, ldy;
   int64_t units;                   // rows * groups
   FastDiv groups;                  // of eight columns in a row
+  uint32_t step_rows, step_groups; // THREADS groups further
   int32_t cols;
   uint32_t limit;                  // dropped below it
+  uint32_t above;                  // 2^16 limit - 1
   float scale;
-  uint64_t seed, offset;
+  uint32_t k0[ROUNDS], k1[ROUNDS];
+  uint64_t offset;
   const uint64_t* offset_device;
 };
 
-__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, uint64_t offset, uint64_t key) {
+__device__ __forceinline__ uint4 philox(const DropoutParams& p, uint32_t c0, uint32_t c1, uint64_t offset) {
   uint32_t x0 = c0, x1 = c1, x2 = (uint32_t)offset, x3 = (uint32_t)(offset >> 32);
-  uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
 #pragma unroll
-  for (int r = 0; r < 10; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const uint64_t p0 = (uint64_t)x0 * 0xD2511F53u, p1 = (uint64_t)x2 * 0xCD9E8D57u;
-    x0 = (uint32_t)(p1 >> 32) ^ x1 ^ k0;
+    x0 = (uint32_t)(p1 >> 32) ^ x1 ^ p.k0[r];
     x1 = (uint32_t)p1;
-    x2 = (uint32_t)(p0 >> 32) ^ x3 ^ k1;
+    x2 = (uint32_t)(p0 >> 32) ^ x3 ^ p.k1[r];
     x3 = (uint32_t)p0;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
   }
   return make_uint4(x0, x1, x2, x3);
 }
 
-// VEC: rows and pitches are whole vectors; otherwise a group is handled element by element.
-template <typename T, bool RESID, bool VEC>
-__global__ void __launch_bounds__(THREADS) dropout_kernel(const DropoutParams p) {
+// How the rows lie.  FLAT: one after the other without gaps, in whole vectors; PITCHED: whole vectors a pitch apart (the last group may be short of
+// columns); LOOSE: anything, element by element.
+enum Rows { FLAT, PITCHED, LOOSE };
+
+constexpr int units_of(bool resid) { return resid ? 2 : 4; }       // groups of eight columns of a thread
+template <typename T, bool RESID, int ROWS>
+__global__ void __launch_bounds__(THREADS) dropout_kernel(const __grid_constant__ DropoutParams p) {
+  constexpr int UNITS = units_of(RESID);
   fax_grid_dependency_wait();
   const uint64_t offset = p.offset + (p.offset_device ? *p.offset_device : 0);
   const int64_t first = (int64_t)blockIdx.x * (THREADS * UNITS);
-  const uint32_t row0 = (uint32_t)(first / p.groups.d), group0 = (uint32_t)(first - (int64_t)row0 * p.groups.d);
-  Pack<T, 8> x[UNITS], r[UNITS];
   uint32_t row[UNITS], group[UNITS];
+  {
+    const uint32_t row0 = (uint32_t)(first / p.groups.d), at = (uint32_t)(first - (int64_t)row0 * p.groups.d) + threadIdx.x, down = p.groups.div(at);
+    row[0] = row0 + down;
+    group[0] = p.groups.mod(at, down);
+#pragma unroll
+    for (int k = 1; k < UNITS; ++k) {
+      row[k] = row[k - 1] + p.step_rows;
+      group[k] = group[k - 1] + p.step_groups;
+      if (group[k] >= p.groups.d) { group[k] -= p.groups.d; ++row[k]; }
+    }
+  }
+  auto place = [&](int k, int64_t ld) { return ROWS == FLAT ? (first + threadIdx.x + k * THREADS) * 8 : (int64_t)row[k] * ld + group[k] * 8; };
+  Pack<T, 8> x[UNITS], r[RESID ? UNITS : 1];
+  bool live[UNITS], whole[UNITS];
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
-    const uint32_t u = threadIdx.x + k * THREADS;
-    const uint32_t at = group0 + u, down = p.groups.div(at);
-    row[k] = row0 + down;
-    group[k] = p.groups.mod(at, down);
-    if (first + u < p.units) {
-      const int64_t in = (int64_t)row[k] * p.ldx + group[k] * 8, rin = (int64_t)row[k] * p.ldr + group[k] * 8;
-      if (VEC) {
-        x[k] = load_pack<T, 8>((const T*)p.x + in);
-        if (RESID) r[k] = load_pack<T, 8>((const T*)p.resid + rin);
-      } else {
+    live[k] = first + threadIdx.x + k * THREADS < p.units;
+    whole[k] = ROWS == FLAT || (ROWS == PITCHED && (int)group[k] * 8 + 8 <= p.cols);
+    if (!live[k]) continue;
+    const T* px = (const T*)p.x + place(k, p.ldx);
+    const T* pr = RESID ? (const T*)p.resid + place(k, p.ldr) : nullptr;
+    if (whole[k]) {
+      x[k] = load_pack<T, 8>(px);
+      if constexpr (RESID) r[k] = load_pack<T, 8>(pr);
+    } else if (ROWS != FLAT) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((int)group[k] * 8 + i < p.cols) {
-            x[k].e[i] = ((const T*)p.x)[in + i];
-            if (RESID) r[k].e[i] = ((const T*)p.resid)[rin + i];
-          }
-      }
+      for (int i = 0; i < 8; ++i)
+        if ((int)group[k] * 8 + i < p.cols) {
+          x[k].e[i] = px[i];
+          if constexpr (RESID) r[k].e[i] = pr[i];
+        }
     }
   }
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
-    const uint32_t u = threadIdx.x + k * THREADS;
-    if (first + u >= p.units) break;
-    const uint4 bits = philox(group[k], row[k], offset, p.seed);
+    if (!live[k]) continue;
+    // (a limit of 0 keeps everything: whatever is above 0)
+    const uint4 bits = p.limit ? philox(p, group[k], row[k], offset) : make_uint4(~0u, ~0u, ~0u, ~0u);
     const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
-    Pack<T, 8> y;
+    float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t draw = i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu;
-      const float kept = draw >= p.limit ? to_f32(x[k].e[i]) : 0.f;      // whatever x is
-      y.e[i] = from_f32<T>(RESID ? fmaf(kept, p.scale, to_f32(r[k].e[i])) : kept * p.scale);
+      const bool keep = (i % 2 ? w[i / 2] : w[i / 2] << 16) > p.above;       // the 16 bits against the limit, in the upper half of a word
+      const float kept = keep ? to_f32(x[k].e[i]) : 0.f;      // whatever x is
+      if constexpr (RESID) y[i] = fmaf(kept, p.scale, to_f32(r[k].e[i]));
+      else y[i] = kept * p.scale;
     }
-    T* out = (T*)p.y + (int64_t)row[k] * p.ldy + group[k] * 8;
-    if (VEC) {
-      store_pack<T, 8>(out, y);
+    Pack<T, 8> out;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) reinterpret_cast<__nv_bfloat162*>(out.e)[i / 2] = __floats2bfloat162_rn(y[i], y[i + 1]);
     } else {
 #pragma unroll
+      for (int i = 0; i < 8; ++i) out.e[i] = from_f32<T>(y[i]);
+    }
+    T* py = (T*)p.y + place(k, p.ldy);
+    if (whole[k]) {
+      store_pack<T, 8>(py, out);
+    } else if (ROWS != FLAT) {
+#pragma unroll
       for (int i = 0; i < 8; ++i)
-        if ((int)group[k] * 8 + i < p.cols) out[i] = y.e[i];
+        if ((int)group[k] * 8 + i < p.cols) py[i] = out.e[i];
     }
   }
 }
 
+template <typename T, int ROWS>
+void launch(fax_ctx* ctx, bool resid, int grid, const DropoutParams& p) {
+  fax_launch(ctx, resid ? dropout_kernel<T, true, ROWS> : dropout_kernel<T, false, ROWS>, dim3(grid), dim3(THREADS), 0, p);
+}
 template <typename T>
-void launch(fax_ctx* ctx, bool resid, bool vec, int grid, const DropoutParams& p) {
-  auto kernel = resid ? (vec ? dropout_kernel<T, true, true> : dropout_kernel<T, true, false>) : (vec ? dropout_kernel<T, false, true> : dropout_kernel<T, false, false>);
-  fax_launch(ctx, kernel, dim3(grid), dim3(THREADS), 0, p);
+void launch(fax_ctx* ctx, bool resid, Rows rows, int grid, const DropoutParams& p) {
+  if (rows == FLAT) launch<T, FLAT>(ctx, resid, grid, p);
+  else if (rows == PITCHED) launch<T, PITCHED>(ctx, resid, grid, p);
+  else launch<T, LOOSE>(ctx, resid, grid, p);
 }
 
 }  // namespace
@@ -115,20 +144,27 @@ extern "C" fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropo
   if (!fax_aligned(d->x, es) || !fax_aligned(d->y, es) || !fax_aligned(d->resid, es) || !fax_aligned(d->offset_device, 8)) return FAX_ERR_INVALID_ARG;
   if ((d->x == d->y && d->ldx != d->ldy) || (d->resid == d->y && d->ldr != d->ldy)) return FAX_ERR_INVALID_ARG;
   const uint32_t groups = ((uint32_t)d->cols + 7) / 8;
-  const int64_t units = (int64_t)d->rows * groups, blocks = (units + THREADS * UNITS - 1) / (THREADS * UNITS);
+  const int64_t units = (int64_t)d->rows * groups, per_block = THREADS * units_of(d->resid != nullptr), blocks = (units + per_block - 1) / per_block;
   if (blocks > 0x7fffffff) return FAX_ERR_UNSUPPORTED_SHAPE;
 
   DropoutParams p;
   p.x = d->x; p.resid = d->resid; p.y = d->y; p.ldx = d->ldx; p.ldr = d->ldr; p.ldy = d->ldy;
   p.units = units; p.groups = FastDiv(groups); p.cols = d->cols;
   p.limit = (uint32_t)std::rint((double)d->p * 65536.0);
+  p.above = p.limit ? (p.limit << 16) - 1u : 0u;            // (all ones for 65536: nothing is above)
   p.scale = p.limit < 65536 ? (float)(65536.0 / (65536.0 - p.limit)) : 0.f;
-  p.seed = d->seed; p.offset = d->offset; p.offset_device = d->offset_device;
-  const bool vec = d->cols % 8 == 0 && fax_rows_aligned(d->x, d->ldx, es, 16) && fax_rows_aligned(d->y, d->ldy, es, 16) &&
-                   (!d->resid || fax_rows_aligned(d->resid, d->ldr, es, 16));
+  for (int r = 0; r < ROUNDS; ++r) {
+    p.k0[r] = (uint32_t)d->seed + (uint32_t)r * 0x9E3779B9u;
+    p.k1[r] = (uint32_t)(d->seed >> 32) + (uint32_t)r * 0xBB67AE85u;
+  }
+  p.offset = d->offset; p.offset_device = d->offset_device;
+  p.step_rows = THREADS / groups; p.step_groups = THREADS % groups;
+  const bool vec = fax_rows_aligned(d->x, d->ldx, es, 16) && fax_rows_aligned(d->y, d->ldy, es, 16) && (!d->resid || fax_rows_aligned(d->resid, d->ldr, es, 16));
+  const bool flat = d->cols % 8 == 0 && d->ldx == d->cols && d->ldy == d->cols && (!d->resid || d->ldr == d->cols);
+  const Rows rows = !vec ? LOOSE : flat ? FLAT : PITCHED;
   const double n = (double)d->rows * d->cols;
   FaxProfScope prof(ctx, KC_DROPOUT, 2.0 * n, (d->resid ? 3.0 : 2.0) * n * es);
-  if (prec == FAX_PREC_BF16) launch<bf16>(ctx, d->resid != nullptr, vec, (int)blocks, p);
-  else launch<float>(ctx, d->resid != nullptr, vec, (int)blocks, p);
+  if (prec == FAX_PREC_BF16) launch<bf16>(ctx, d->resid != nullptr, rows, (int)blocks, p);
+  else launch<float>(ctx, d->resid != nullptr, rows, (int)blocks, p);
   return fax_after_launch(ctx);
 }

@@ -2,12 +2,12 @@
 //
 // The places: a counting sort that keeps the order, in one launch of one cluster.  Each CTA has a consecutive part of the choices,
 // each of its warps a consecutive part of that, and each warp counts its experts 32 choices at a time (the lanes with the same expert
-// find one another by match.any).  The counts are summed over warps in shared memory and over CTAs through distributed shared
+// find one another by a ballot for each bit of the expert's number).  The counts are summed over warps in shared memory and over CTAs through distributed shared
 // memory, which gives every warp the first slot of each expert for its own choices; a second walk over the (cached) ids hands the slots out.
 // Nothing is stored in between and nothing depends on an order of atomics.  Latency bounds it.
 //
 // The rows: memory bounds them.  A group of threads has a token: its row is read once and written to (or read from) the slots of all
-// its choices, a 16-byte vector at a time; groups behind the tokens look for empty slots and zero them.
+// its choices, a 16-byte vector at a time; groups before the tokens' look for empty slots and zero them.
 #include "stream_common.cuh"
 #include "../../include/fax_ops.h"
 
@@ -15,9 +15,9 @@ namespace {
 
 // ---- the places ----
 
-constexpr int SORT_THREADS = 1024;
-constexpr int SORT_WARPS = SORT_THREADS / 32;
-constexpr int SORT_CLUSTER = 8;
+constexpr int SORT_WARPS = 32;                  // of a CTA at most
+constexpr int SORT_CLUSTER = 16;
+constexpr int GROUPS = 4;                       // of 32 choices that a warp has in registers at a time
 
 struct SortParams {
   int32_t choices, experts, capacity, align, slots;
@@ -37,6 +37,16 @@ __device__ __forceinline__ void store_remote(const int32_t* here, uint32_t rank,
   asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(r), "r"(v) : "memory");
 }
 
+// The lanes with the same x as this one, x of `bits` bits: a ballot a bit (match.any takes longer the more values there are).
+__device__ __forceinline__ uint32_t alike(int x, int bits) {
+  uint32_t same = 0xffffffffu;
+  for (int b = 0; b < bits; ++b) {
+    const uint32_t ones = __ballot_sync(0xffffffffu, (x >> b) & 1);
+    same &= ((x >> b) & 1) ? ones : ~ones;
+  }
+  return same;
+}
+
 __device__ __forceinline__ int warp_inclusive(int v) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -46,38 +56,53 @@ __device__ __forceinline__ int warp_inclusive(int v) {
   return v;
 }
 
-// Shared memory: counts of each warp [SORT_WARPS][experts], of each CTA [SORT_CLUSTER][experts], first slots [experts].
-__global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(const SortParams p) {
+// Shared memory: counts of each warp [warps][experts], of each CTA [CTAs][experts], first slots [experts].
+__global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const SortParams p) {
   extern __shared__ int32_t mem[];
-  int32_t* const mine = mem;
-  int32_t* const ctas = mem + SORT_WARPS * p.experts;
-  int32_t* const first = ctas + SORT_CLUSTER * p.experts;
-  __shared__ int32_t sums[SORT_WARPS + 1];
   const uint32_t rank = cluster_rank(), n_ctas = cluster_size();
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int threads = blockDim.x, n_warps = threads / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  int32_t* const mine = mem;
+  int32_t* const ctas = mem + n_warps * p.experts;
+  int32_t* const first = ctas + n_ctas * p.experts;
+  __shared__ int32_t sums[SORT_WARPS + 1];
   const uint32_t before_me = (1u << lane) - 1;
-  for (int i = threadIdx.x; i < SORT_WARPS * p.experts; i += SORT_THREADS) mine[i] = 0;
+  for (int i = threadIdx.x; i < n_warps * p.experts; i += threads) mine[i] = 0;
   __syncthreads();
   if (n_ctas > 1) cluster_sync();                                   // the others run: their shared memory can be written
   fax_grid_dependency_wait();
 
-  // this warp's choices: whole groups of 32
-  const int64_t groups = ((int64_t)p.choices + 31) / 32, warps = (int64_t)n_ctas * SORT_WARPS, me = (int64_t)rank * SORT_WARPS + warp;
+  // this warp's choices: whole groups of 32, GROUPS of them read at a time; the first ones stay for the second walk
+  const int64_t groups = ((int64_t)p.choices + 31) / 32, warps = (int64_t)n_ctas * n_warps, me = (int64_t)rank * n_warps + warp;
   const int64_t lo = groups * me / warps * 32, hi = min(groups * (me + 1) / warps * 32, (int64_t)p.choices);
   int32_t* const count = mine + warp * p.experts;
-  for (int64_t c = lo; c < hi; c += 32) {
-    const int e = c + lane < hi ? p.ids[c + lane] : -1;
-    const bool live = (uint32_t)e < (uint32_t)p.experts;
-    const uint32_t same = __match_any_sync(0xffffffffu, live ? e : -1);
-    if (live && (same & before_me) == 0) count[e] += __popc(same);
-    __syncwarp();
+  const int bits = 32 - __clz(p.experts);         // of 0 to experts
+  int x[GROUPS];
+  auto read = [&](int64_t c) {
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      const int64_t at = c + 32 * k + lane;
+      x[k] = at < hi ? p.ids[at] : -1;
+      if ((uint32_t)x[k] >= (uint32_t)p.experts) x[k] = p.experts;                // none
+    }
+  };
+  // (from the end, so that the first ones are read last)
+  const int64_t last = lo < hi ? lo + (hi - lo - 1) / (32 * GROUPS) * (32 * GROUPS) : lo - 1;
+  for (int64_t c = last; c >= lo; c -= 32 * GROUPS) {
+    read(c);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      if (c + 32 * k >= hi) break;
+      const uint32_t same = alike(x[k], bits);
+      if (x[k] < p.experts && (same & before_me) == 0) count[x[k]] += __popc(same);
+      __syncwarp();
+    }
   }
   __syncthreads();
   // over the warps: what each starts from within the CTA, and the CTA's counts for everyone
-  for (int e = threadIdx.x; e < p.experts; e += SORT_THREADS) {
+  for (int e = threadIdx.x; e < p.experts; e += threads) {
     int sum = 0;
-#pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) {
+#pragma unroll 8
+    for (int w = 0; w < n_warps; ++w) {
       const int n = mine[w * p.experts + e];
       mine[w * p.experts + e] = sum;
       sum += n;
@@ -86,7 +111,7 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(const SortPar
     else for (uint32_t r = 0; r < n_ctas; ++r) store_remote(&ctas[rank * p.experts + e], r, sum);
   }
   if (n_ctas > 1) cluster_sync(); else __syncthreads();
-  // each expert's first slot: threads have one expert each (experts <= SORT_THREADS)
+  // each expert's first slot: a thread has one expert
   const int e = threadIdx.x;
   int total = 0, earlier = 0, room = 0;
   if (e < p.experts) {
@@ -99,14 +124,10 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(const SortPar
   const int through = warp_inclusive(room);
   if (lane == 31) sums[warp] = through;
   __syncthreads();
-  if (warp == 0) {
-    const int v = sums[lane], t = warp_inclusive(v);
-    __syncwarp();
-    sums[lane] = t - v;
-    if (lane == 31) sums[SORT_WARPS] = t;
-  }
-  __syncthreads();
-  const int slot0 = sums[warp] + through - room, end = sums[SORT_WARPS];
+  // (every warp adds up the warps before it)
+  const int v = warp_inclusive(lane < n_warps ? sums[lane] : 0);
+  const int before = __shfl_sync(0xffffffffu, v, (warp + 31) % 32), end = __shfl_sync(0xffffffffu, v, 31);
+  const int slot0 = (warp ? before : 0) + through - room;
   if (e < p.experts) {
     first[e] = (int)((uint32_t)slot0 + (uint32_t)earlier);
     if (rank == 0) {
@@ -116,43 +137,49 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(const SortPar
     }
   }
   __syncthreads();
+  // the slots
+  for (int64_t c = lo; c < hi; c += 32 * GROUPS) {
+    if (c > lo) read(c);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      if (c + 32 * k >= hi) break;
+      const uint32_t same = alike(x[k], bits);
+      int slot = -1;
+      if (x[k] < p.experts) {
+        const uint32_t next = (uint32_t)first[x[k]] + (uint32_t)count[x[k]] + __popc(same & before_me);     // below 2^32: slots and choices are below 2^31
+        slot = p.capacity && next >= (int64_t)(x[k] + 1) * p.capacity ? -1 : (int)next;
+      }
+      __syncwarp();
+      if (x[k] < p.experts && (same & before_me) == 0) count[x[k]] += __popc(same);
+      __syncwarp();
+      const int64_t at = c + 32 * k + lane;
+      if (at < hi) {
+        p.slot_of[at] = slot;
+        if (slot >= 0) p.source[slot] = (int32_t)at;
+      }
+    }
+  }
   // empty slots: behind an expert's choices (a warp an expert), and behind the last expert
-  for (int x = rank * SORT_WARPS + warp; x < p.experts; x += n_ctas * SORT_WARPS) {
-    int all = 0;
-    for (uint32_t r = 0; r < n_ctas; ++r) all += ctas[r * p.experts + x];
-    uint32_t start = (uint32_t)first[x];
-    for (uint32_t r = 0; r < rank; ++r) start -= (uint32_t)ctas[r * p.experts + x];
+  for (int q = rank * n_warps + warp; q < p.experts; q += n_ctas * n_warps) {
+    int all = 0, others = 0;
+    for (uint32_t r = 0; r < n_ctas; ++r) {
+      if (r == rank) others = all;
+      all += ctas[r * p.experts + q];
+    }
+    const uint32_t start = (uint32_t)first[q] - (uint32_t)others;
     const int64_t stop = (int64_t)start + (p.capacity ? p.capacity : (all + p.align - 1) / p.align * p.align);
     for (int64_t s = (int64_t)start + all + lane; s < stop; s += 32) p.source[s] = -1;
   }
-  for (int64_t s = end + (int64_t)rank * SORT_THREADS + threadIdx.x; s < p.slots; s += (int64_t)n_ctas * SORT_THREADS) p.source[s] = -1;
-  // the slots
-  for (int64_t c = lo; c < hi; c += 32) {
-    const int x = c + lane < hi ? p.ids[c + lane] : -1;
-    const bool live = (uint32_t)x < (uint32_t)p.experts;
-    const uint32_t same = __match_any_sync(0xffffffffu, live ? x : -1);
-    int slot = -1;
-    if (live) {
-      const uint32_t next = (uint32_t)first[x] + (uint32_t)count[x] + __popc(same & before_me);     // below 2^32: slots and choices are below 2^31
-      slot = p.capacity && next >= (int64_t)(x + 1) * p.capacity ? -1 : (int)next;
-    }
-    __syncwarp();
-    if (live && (same & before_me) == 0) count[x] += __popc(same);
-    __syncwarp();
-    if (c + lane < hi) {
-      p.slot_of[c + lane] = slot;
-      if (slot >= 0) p.source[slot] = (int32_t)(c + lane);
-    }
-  }
+  for (int64_t s = end + (int64_t)rank * threads + threadIdx.x; s < p.slots; s += (int64_t)n_ctas * threads) p.source[s] = -1;
 }
 
 // ---- the rows ----
 
 constexpr int ROW_THREADS = 256;
-constexpr int CHOICES = 8;          // of a token that a thread works on at a time
 
 struct RowParams {
   int32_t n_tokens, top_k, d, slots;
+  int64_t slot_groups;                // groups of threads that look for empty slots; those behind have a token each
   const int32_t* slot_of; const int32_t* source;
   const float* weights;
   const void *in, *resid, *z; void *out;
@@ -165,49 +192,64 @@ __device__ __forceinline__ int slot_at(const RowParams& p, int64_t token, int j)
   return (uint32_t)s < (uint32_t)p.slots ? s : -1;
 }
 
-// Zeros in slot s if it is empty.
+// Zeros in the empty ones of the 32 slots from s0 on: the group's warps look at them together and take a row in turn.
 template <typename T, int N, int GROUP>
-__device__ __forceinline__ void zero_slot(const RowParams& p, int64_t s, int lane) {
-  if (s >= p.slots || p.source[s] >= 0) return;
+__device__ __forceinline__ void zero_slots(const RowParams& p, int64_t s0) {
+  const int lane = threadIdx.x % 32, in_group = threadIdx.x % GROUP;
+  const int64_t s = s0 + lane;
+  uint32_t empty = __ballot_sync(0xffffffffu, s < p.slots && p.source[s] < 0);
   Pack<T, N> zero;
 #pragma unroll
   for (int i = 0; i < N; ++i) zero.e[i] = from_f32<T>(0.f);
-  T* row = (T*)p.out + s * p.ld_out;
-  for (int v = lane; v < p.d / N; v += GROUP) store_pack<T, N>(row + v * N, zero);
+  for (; empty; empty &= empty - 1) {
+    T* row = (T*)p.out + (s0 + __ffs(empty) - 1) * p.ld_out;
+    for (int v = in_group; v < p.d / N; v += GROUP) store_pack<T, N>(row + v * N, zero);
+  }
 }
 
-// A group of GROUP threads a token; tokens first, then one group for each slot.
-template <typename T, int N, int GROUP>
-__global__ void __launch_bounds__(ROW_THREADS) dispatch_kernel(const RowParams p) {
+// K: choices of a token that a thread works on at a time.  GROUP: threads of a token, a warp or the block.
+template <typename T, int N, int GROUP, int K>
+__global__ void __launch_bounds__(ROW_THREADS, 4) dispatch_kernel(const RowParams p) {
+  constexpr int U = 4;                            // vectors on their way together
   fax_grid_dependency_wait();
   const int lane = threadIdx.x % GROUP;
-  const int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
-  if (item >= p.n_tokens) { zero_slot<T, N, GROUP>(p, item - p.n_tokens, lane); return; }
+  int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
+  if (item < p.slot_groups) { zero_slots<T, N, GROUP>(p, item * 32); return; }
+  item -= p.slot_groups;
+  if (item >= p.n_tokens) return;
   const T* row = (const T*)p.in + item * p.ld_in;
-  for (int j0 = 0; j0 < p.top_k; j0 += CHOICES) {
-    int slot[CHOICES];
+  const int vectors = p.d / N;
+  for (int j0 = 0; j0 < p.top_k; j0 += K) {
+    int slot[K];
 #pragma unroll
-    for (int j = 0; j < CHOICES; ++j) slot[j] = slot_at(p, item, j0 + j);
-    for (int v = lane; v < p.d / N; v += GROUP) {
-      const Pack<T, N> x = load_pack<T, N>(row + v * N);
+    for (int j = 0; j < K; ++j) slot[j] = slot_at(p, item, j0 + j);
+    for (int v0 = lane; v0 < vectors; v0 += GROUP * U) {
+      Pack<T, N> x[U];
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j)
-        if (slot[j] >= 0) store_pack<T, N>((T*)p.out + (int64_t)slot[j] * p.ld_out + v * N, x);
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * GROUP < vectors) x[u] = load_pack<T, N>(row + (v0 + u * GROUP) * N);
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (slot[j] >= 0) {
+          T* out = (T*)p.out + (int64_t)slot[j] * p.ld_out + v0 * N;
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (v0 + u * GROUP < vectors) store_pack<T, N>(out + u * GROUP * N, x[u]);
+        }
     }
   }
 }
 
-template <typename T, int N, int GROUP>
-__global__ void __launch_bounds__(ROW_THREADS) combine_kernel(const RowParams p) {
+template <typename T, int N, int GROUP, int K>
+__global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_kernel(const RowParams p) {
   fax_grid_dependency_wait();
   const int lane = threadIdx.x % GROUP;
   const int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
   if (item >= p.n_tokens) return;
-  const int rounds = (p.top_k + CHOICES - 1) / CHOICES;
-  int slot[CHOICES]; float w[CHOICES];
+  int slot[K]; float w[K];
   auto fetch = [&](int j0) {
 #pragma unroll
-    for (int j = 0; j < CHOICES; ++j) {
+    for (int j = 0; j < K; ++j) {
       slot[j] = slot_at(p, item, j0 + j);
       w[j] = slot[j] >= 0 && p.weights ? p.weights[item * p.top_k + j0 + j] : 1.f;
     }
@@ -219,14 +261,14 @@ __global__ void __launch_bounds__(ROW_THREADS) combine_kernel(const RowParams p)
     for (int i = 0; i < N; ++i) sum[i] = 0.f;
     Pack<T, N> r;
     if (p.resid) r = load_pack<T, N>((const T*)p.resid + item * p.ld_resid + v * N);
-    for (int k = 0; k < rounds; ++k) {
-      if (rounds > 1) fetch(k * CHOICES);
-      Pack<T, N> z[CHOICES];
+    for (int j0 = 0; j0 < p.top_k; j0 += K) {
+      if (p.top_k > K) fetch(j0);
+      Pack<T, N> z[K];
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j)
+      for (int j = 0; j < K; ++j)
         if (slot[j] >= 0) z[j] = load_pack<T, N>((const T*)p.z + (int64_t)slot[j] * p.ld_z + v * N);
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j)
+      for (int j = 0; j < K; ++j)
         if (slot[j] >= 0) {
 #pragma unroll
           for (int i = 0; i < N; ++i) sum[i] = fmaf(w[j], to_f32(z[j].e[i]), sum[i]);
@@ -240,32 +282,34 @@ __global__ void __launch_bounds__(ROW_THREADS) combine_kernel(const RowParams p)
 }
 
 // in: dy; out: dz.  The products of a choice are summed over a thread's vectors, the group's lanes by halves, its warps in order.
-template <typename T, int N, int GROUP>
-__global__ void __launch_bounds__(ROW_THREADS) combine_backward_kernel(const RowParams p) {
-  __shared__ float sums[GROUP > 32 ? ROW_THREADS / 32 : 1][CHOICES];
+template <typename T, int N, int GROUP, int K>
+__global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_backward_kernel(const RowParams p) {
+  __shared__ float sums[GROUP > 32 ? ROW_THREADS / 32 : 1][K];
   fax_grid_dependency_wait();
   const int lane = threadIdx.x % GROUP;
-  const int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
-  if (item >= p.n_tokens) { zero_slot<T, N, GROUP>(p, item - p.n_tokens, lane); return; }
+  int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
+  if (item < p.slot_groups) { zero_slots<T, N, GROUP>(p, item * 32); return; }
+  item -= p.slot_groups;
+  if (item >= p.n_tokens) return;
   const T* row = (const T*)p.in + item * p.ld_in;
-  for (int j0 = 0; j0 < p.top_k; j0 += CHOICES) {
-    int slot[CHOICES]; float w[CHOICES], dot[CHOICES];
+  for (int j0 = 0; j0 < p.top_k; j0 += K) {
+    int slot[K]; float w[K], dot[K];
 #pragma unroll
-    for (int j = 0; j < CHOICES; ++j) {
+    for (int j = 0; j < K; ++j) {
       slot[j] = slot_at(p, item, j0 + j);
       w[j] = slot[j] >= 0 ? p.weights[item * p.top_k + j0 + j] : 0.f;
       dot[j] = 0.f;
     }
     for (int v = lane; v < p.d / N; v += GROUP) {
       const Pack<T, N> g = load_pack<T, N>(row + v * N);
-      Pack<T, N> z[CHOICES];
+      Pack<T, N> z[K];
       if (p.dw) {
 #pragma unroll
-        for (int j = 0; j < CHOICES; ++j)
+        for (int j = 0; j < K; ++j)
           if (slot[j] >= 0) z[j] = load_pack<T, N>((const T*)p.z + (int64_t)slot[j] * p.ld_z + v * N);
       }
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j)
+      for (int j = 0; j < K; ++j)
         if (slot[j] >= 0) {
           Pack<T, N> dz;
 #pragma unroll
@@ -279,16 +323,16 @@ __global__ void __launch_bounds__(ROW_THREADS) combine_backward_kernel(const Row
     }
     if (!p.dw) continue;
 #pragma unroll
-    for (int j = 0; j < CHOICES; ++j) dot[j] = warp_sum(dot[j]);
+    for (int j = 0; j < K; ++j) dot[j] = warp_sum(dot[j]);
     if (GROUP > 32) {
       __syncthreads();                            // GROUP is the block then: its threads are all here
       if (threadIdx.x % 32 == 0) {
 #pragma unroll
-        for (int j = 0; j < CHOICES; ++j) sums[threadIdx.x / 32][j] = dot[j];
+        for (int j = 0; j < K; ++j) sums[threadIdx.x / 32][j] = dot[j];
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j) {
+      for (int j = 0; j < K; ++j) {
         dot[j] = 0.f;
 #pragma unroll
         for (int q = 0; q < ROW_THREADS / 32; ++q) dot[j] += sums[q][j];
@@ -296,7 +340,7 @@ __global__ void __launch_bounds__(ROW_THREADS) combine_backward_kernel(const Row
     }
     if (lane == 0) {
 #pragma unroll
-      for (int j = 0; j < CHOICES; ++j)
+      for (int j = 0; j < K; ++j)
         if (j0 + j < p.top_k) p.dw[item * p.top_k + j0 + j] = slot[j] >= 0 ? dot[j] : 0.f;
     }
   }
@@ -304,14 +348,25 @@ __global__ void __launch_bounds__(ROW_THREADS) combine_backward_kernel(const Row
 
 enum RowOp { DISPATCH, COMBINE, COMBINE_BACKWARD };
 
+template <typename T, int N, int GROUP, int K>
+fax_status launch_rows(fax_ctx* ctx, RowOp op, RowParams p) {
+  constexpr int PER_BLOCK = ROW_THREADS / GROUP;
+  p.slot_groups = op == COMBINE ? 0 : (((int64_t)p.slots + 31) / 32 + PER_BLOCK - 1) / PER_BLOCK * PER_BLOCK;      // whole blocks, so that none has both kinds of work
+  const int64_t groups = p.slot_groups + p.n_tokens;
+  const dim3 grid((unsigned)((groups + PER_BLOCK - 1) / PER_BLOCK)), threads(ROW_THREADS);
+  if (op == DISPATCH) fax_launch(ctx, dispatch_kernel<T, N, GROUP, K>, grid, threads, 0, p);
+  else if (op == COMBINE) fax_launch(ctx, combine_kernel<T, N, GROUP, K>, grid, threads, 0, p);
+  else fax_launch(ctx, combine_backward_kernel<T, N, GROUP, K>, grid, threads, 0, p);
+  return fax_after_launch(ctx);
+}
+template <typename T, int N, int GROUP>
+fax_status launch_rows(fax_ctx* ctx, RowOp op, const RowParams& p) {
+  if (p.top_k <= 2) return launch_rows<T, N, GROUP, 2>(ctx, op, p);
+  return p.top_k <= 4 ? launch_rows<T, N, GROUP, 4>(ctx, op, p) : launch_rows<T, N, GROUP, 8>(ctx, op, p);
+}
 template <typename T, int N>
 fax_status launch_rows(fax_ctx* ctx, RowOp op, bool block, const RowParams& p) {
-  const int64_t items = (int64_t)p.n_tokens + (op == COMBINE ? 0 : p.slots), per_block = block ? 1 : ROW_THREADS / 32;
-  const dim3 grid((unsigned)((items + per_block - 1) / per_block)), threads(ROW_THREADS);
-  if (op == DISPATCH) fax_launch(ctx, block ? dispatch_kernel<T, N, ROW_THREADS> : dispatch_kernel<T, N, 32>, grid, threads, 0, p);
-  else if (op == COMBINE) fax_launch(ctx, block ? combine_kernel<T, N, ROW_THREADS> : combine_kernel<T, N, 32>, grid, threads, 0, p);
-  else fax_launch(ctx, block ? combine_backward_kernel<T, N, ROW_THREADS> : combine_backward_kernel<T, N, 32>, grid, threads, 0, p);
-  return fax_after_launch(ctx);
+  return block ? launch_rows<T, N, ROW_THREADS>(ctx, op, p) : launch_rows<T, N, 32>(ctx, op, p);
 }
 
 // Vectors of 16 bytes where every row is whole vectors, else single elements; a block a token where tokens are few.
@@ -354,14 +409,19 @@ extern "C" fax_status fax_op_expert_sort(fax_ctx* ctx, const fax_expert_sort_des
   SortParams p;
   p.choices = d->n_tokens * d->top_k; p.experts = d->n_experts; p.capacity = d->capacity; p.align = d->capacity ? 1 : d->align; p.slots = d->slots;
   p.ids = d->ids; p.slot_of = d->slot_of; p.source = d->source; p.offsets = d->offsets; p.counts = d->counts;
-  const int smem_max = (SORT_WARPS + SORT_CLUSTER + 1) * FAX_EXPERT_MAX * 4, smem = (SORT_WARPS + SORT_CLUSTER + 1) * p.experts * 4;
+  // Warps for every 64 choices, one CTA of them or a cluster's; threads for every expert.
+  const int cluster = p.choices <= SORT_WARPS * 32 * GROUPS ? 1 : p.choices <= 4 * SORT_WARPS * 32 * GROUPS ? 8 : SORT_CLUSTER;
+  int warps = (p.choices / cluster + 63) / 64;
+  if (warps < (p.experts + 31) / 32) warps = (p.experts + 31) / 32;
+  if (warps < 4) warps = 4;
+  if (warps > SORT_WARPS) warps = SORT_WARPS;
+  const int smem_max = (SORT_WARPS + SORT_CLUSTER + 1) * FAX_EXPERT_MAX * 4, smem = (warps + cluster + 1) * p.experts * 4;
   static bool done[FAX_MAX_DEVICES] = {};
   FAX_TRY(fax_opt_in_shared_memory(ctx, expert_sort_kernel, smem_max, done));
-  // One CTA as long as its warps have a few groups of 32 choices each, or all the cluster's.
-  const int cluster = p.choices <= 4 * SORT_THREADS ? 1 : SORT_CLUSTER;
+  if (cluster > 8) FAX_CUDA_TRY(ctx, cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   FaxProfScope prof(ctx, KC_EXPERT, 0.0, 4.0 * (2.0 * p.choices + p.slots + 2.0 * p.experts));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cluster); cfg.blockDim = dim3(SORT_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
+  cfg.gridDim = dim3(cluster); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

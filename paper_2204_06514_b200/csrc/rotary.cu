@@ -2,12 +2,13 @@
 //
 // The angle.  A frequency is held as turns in units of 2^-64, so that position * frequency modulo 2^64 is the angle modulo a
 // turn with no rounding at all: one 64-bit integer product, right at any position (a float32 angle is off by 0.06 rad at
-// position 10^6).  The nearest quarter turn is split off exactly, what is left (within an eighth of a turn, 34 bits behind the
-// point of the turn) goes through sincospif: the two factors are within 1e-7 of their values.
+// position 10^6).  The nearest quarter turn is split off exactly; sine and cosine of what is left (within an eighth of a turn, 34
+// bits behind the point of the turn) are the first five terms of their series each, within 2^-24 of their values.
 //
-// The work.  Each element is read and written once; memory bounds it.  The factors are the same for every head of a token, so
-// a block first works out those of its rows (rows * rot_dim / 2 of them) into shared memory and then goes over its rows' heads
-// 16 bytes a side at a time; the first loads are on their way while the factors are made.
+// The work.  Each element is read and written once; memory bounds it, the instructions come next (two pairs share one where the hardware has
+// it).  The factors are the same for every head of a token, so a thread works out those of one 16-byte vector of one token,
+// keeps them in registers and goes over the heads (or a part of them where tokens are few), several heads' loads on their way
+// together.  With HALVES the vector's partner lies half of rot_dim further: the lanes of a token cover whole lines of a head with both.
 #include <cmath>
 
 #include "stream_common.cuh"
@@ -16,104 +17,162 @@
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int UNITS = 4;                          // pairs of vectors that a thread holds at a time
-constexpr int TABLE_BYTES = 32 * 1024;
 
 struct RotaryParams {
   const void* x; void* y; int64_t ldx, ldy;
   const int32_t* positions;
   const uint64_t* freq;
-  int32_t rows, block_rows, half, head_dim, first, seq;
+  int32_t rows, heads, head_dim, half, first, seq;
   int32_t turned;                                 // units of a head that turn; those behind are copied
-  FastDiv row_units, head_units;                  // units of a row and of a head
+  int32_t per;                                    // heads of a thread
+  FastDiv units, tokens;                          // units of a head; rows
+  int64_t threads;
   float amplitude; int32_t backward;
 };
 
 // Cosine and sine of a turn's fraction held in units of 2^-64.
 __device__ __forceinline__ void turn(uint64_t angle, float* c, float* s) {
   const uint64_t quarter = (angle + (1ull << 61)) >> 62;
-  const int64_t rest = (int64_t)(angle - (quarter << 62));                     // [-2^61, 2^61)
-  float sn, cs;
-  sincospif((float)(int32_t)(rest >> 30) * 0x1p-33f, &sn, &cs);                // half turns
+  const int32_t rest = (int32_t)((int64_t)(angle - (quarter << 62)) >> 30);    // [-2^31, 2^31): units of 2^-34 turns
+  const float t = (float)rest * (6.28318531f * 0x1p-34f);                      // within pi / 4
+  const float q = t * t;
+  const float sn = fmaf(t * q, fmaf(q, fmaf(q, fmaf(q, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), t);
+  const float cs = fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.f / 40320, -1.f / 720), 1.f / 24), -0.5f), 1.f);
   const bool odd = quarter & 1;
   const float a = odd ? sn : cs, b = odd ? cs : sn;
   *c = (quarter == 1 || quarter == 2) ? -a : a;
   *s = (quarter >= 2) ? -b : b;
 }
 
-// NP: pairs of a unit.  A unit is two vectors of NP elements: HALVES: NP first and NP second elements; PAIRS: 2 NP elements in a row.
-template <typename T, int LAYOUT, int NP>
-__global__ void __launch_bounds__(THREADS) rotary_kernel(const RotaryParams p) {
-  extern __shared__ float table[];
-  float* const cosines = table;
-  float* const sines = table + p.block_rows * p.half;
-  fax_grid_dependency_wait();
-  const int row0 = blockIdx.x * p.block_rows;
-  const int rows = min(p.block_rows, p.rows - row0);
-  const uint32_t units = (uint32_t)rows * p.row_units.d;
-  const T* const x = (const T*)p.x;
-  T* const y = (T*)p.y;
-  for (uint32_t base = 0; base < units; base += THREADS * UNITS) {
-    Pack<T, NP> a[UNITS], b[UNITS];
-    int64_t at[UNITS]; int32_t entry[UNITS], second[UNITS];
+// N elements as floats.
+template <typename T, int N>
+__device__ __forceinline__ void widen(const Pack<T, N>& p, float* f) {
 #pragma unroll
-    for (int k = 0; k < UNITS; ++k) {
-      const uint32_t u = base + k * THREADS + threadIdx.x;
-      at[k] = -1;
-      if (u < units) {
-        const uint32_t r = p.row_units.div(u), in_row = p.row_units.mod(u, r);
-        const uint32_t head = p.head_units.div(in_row), j = p.head_units.mod(in_row, head);
-        const bool turns = (int)j < p.turned;
-        const int col = LAYOUT == FAX_ROTARY_HALVES && turns ? (int)j * NP : (int)j * 2 * NP;
-        second[k] = LAYOUT == FAX_ROTARY_HALVES && turns ? p.half : NP;
-        entry[k] = turns ? (int)(r * p.half + j * NP) : -1;
-        const int64_t row = row0 + (int)r;
-        const int64_t in = (int64_t)head * p.head_dim + col;
-        const T* src = x + row * p.ldx + in;
-        a[k] = load_pack<T, NP>(src);
-        b[k] = load_pack<T, NP>(src + second[k]);
-        at[k] = row * p.ldy + in;
-      }
-    }
-    if (base == 0) {
-      for (int i = threadIdx.x; i < rows * p.half; i += THREADS) {
-        const int r = i / p.half, f = i - r * p.half;
-        const int row = row0 + r;
-        const int64_t pos = p.positions ? (int64_t)p.positions[row] : (int64_t)p.first + (p.seq ? row % p.seq : row);
-        float c, s;
-        turn((uint64_t)pos * p.freq[f], &c, &s);
-        cosines[i] = p.amplitude * c;
-        sines[i] = p.backward ? -(p.amplitude * s) : p.amplitude * s;
-      }
-      __syncthreads();
-    }
+  for (int i = 0; i < N; ++i) f[i] = to_f32(p.e[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> narrow(const float* f) {
+  Pack<T, N> p;
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
 #pragma unroll
-    for (int k = 0; k < UNITS; ++k) {
-      if (at[k] < 0) continue;
-      if (entry[k] >= 0) {
-        const Pack<float, NP> c = load_pack<float, NP>(cosines + entry[k]), s = load_pack<float, NP>(sines + entry[k]);
-        float v[2 * NP], w[2 * NP];
+    for (int i = 0; i + 1 < N; i += 2) reinterpret_cast<__nv_bfloat162*>(p.e)[i / 2] = __floats2bfloat162_rn(f[i], f[i + 1]);
+  } else {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) { v[i] = to_f32(a[k].e[i]); v[NP + i] = to_f32(b[k].e[i]); }
+    for (int i = 0; i < N; ++i) p.e[i] = from_f32<T>(f[i]);
+  }
+  return p;
+}
+// VEC: one access; else element by element.
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ Pack<T, N> load(const T* p) {
+  Pack<T, N> v;
+  if constexpr (VEC) {
+    v = load_pack<T, N>(p);
+  } else {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int ia = LAYOUT == FAX_ROTARY_HALVES ? i : 2 * i, ib = LAYOUT == FAX_ROTARY_HALVES ? NP + i : 2 * i + 1;
-          w[ia] = v[ia] * c.e[i] - v[ib] * s.e[i];
-          w[ib] = v[ib] * c.e[i] + v[ia] * s.e[i];
-        }
+    for (int i = 0; i < N; ++i) v.e[i] = p[i];
+  }
+  return v;
+}
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ void store(T* p, const Pack<T, N>& v) {
+  if constexpr (VEC) {
+    store_pack<T, N>(p, v);
+  } else {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) { a[k].e[i] = from_f32<T>(w[i]); b[k].e[i] = from_f32<T>(w[NP + i]); }
-      }
-      store_pack<T, NP>(y + at[k], a[k]);
-      store_pack<T, NP>(y + at[k] + second[k], b[k]);
-    }
+    for (int i = 0; i < N; ++i) p[i] = v.e[i];
   }
 }
 
-template <typename T, int NP>
-void launch(fax_ctx* ctx, int layout, int grid, size_t smem, const RotaryParams& p) {
-  if (layout == FAX_ROTARY_HALVES) fax_launch(ctx, rotary_kernel<T, FAX_ROTARY_HALVES, NP>, dim3(grid), dim3(THREADS), smem, p);
-  else fax_launch(ctx, rotary_kernel<T, FAX_ROTARY_PAIRS, NP>, dim3(grid), dim3(THREADS), smem, p);
+// Two floats an instruction.
+typedef unsigned long long two;
+__device__ __forceinline__ two pack2(float a, float b) { two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(two v, float* f) { asm("mov.b64 {%0, %1}, %2;" : "=f"(f[0]), "=f"(f[1]) : "l"(v)); }
+__device__ __forceinline__ two mul2(two a, two b) { two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ two fma2(two a, two b, two c) { two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// A unit is N elements and, with HALVES, the N that turn with them; with PAIRS the N elements are N / 2 pairs.
+template <typename T, int LAYOUT, int N, bool VEC>
+__global__ void __launch_bounds__(THREADS, 3) rotary_kernel(const RotaryParams p) {
+  constexpr bool HALVES = LAYOUT == FAX_ROTARY_HALVES;
+  constexpr int PAIRS_ = HALVES ? N : N / 2;                                     // pairs of a unit
+  constexpr int HEADS = HALVES ? 2 : 4;                                          // on their way together: 80 registers, three blocks an SM
+  fax_grid_dependency_wait();
+  const int64_t id = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  if (id >= p.threads) return;
+  const uint32_t rest = p.units.div((uint32_t)id), j = p.units.mod((uint32_t)id, rest);
+  const uint32_t part = p.tokens.div(rest), row = p.tokens.mod(rest, part);
+  const int head0 = (int)part * p.per, heads = min(p.per, p.heads - head0);
+  const bool turns = (int)j < p.turned;
+  // (behind the turning elements a unit is 2 N elements with HALVES)
+  const int col = (int)j * (HALVES && !turns ? 2 * N : N), partner = turns ? p.half : N;
+  const T* x = (const T*)p.x + row * p.ldx + (int64_t)head0 * p.head_dim + col;
+  T* y = (T*)p.y + row * p.ldy + (int64_t)head0 * p.head_dim + col;
+
+  Pack<T, N> a[HEADS], b[HALVES ? HEADS : 1];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+      if (h0 + h < heads) {
+        a[h] = load<T, N, VEC>(x + h * p.head_dim);
+        if constexpr (HALVES) b[h] = load<T, N, VEC>(x + h * p.head_dim + partner);
+      }
+    x += HEADS * p.head_dim;
+  };
+  fetch(0);                                       // on its way while the factors are made
+  float c[PAIRS_], s[PAIRS_];
+  if (turns) {
+    const uint64_t pos = (uint64_t)(p.positions ? (int64_t)p.positions[row] : (int64_t)p.first + (p.seq ? row % (uint32_t)p.seq : row));
+    const float amplitude = p.amplitude, signed_amplitude = p.backward ? -p.amplitude : p.amplitude;
+#pragma unroll
+    for (int i = 0; i < PAIRS_; ++i) {
+      turn(pos * p.freq[j * PAIRS_ + i], &c[i], &s[i]);
+      c[i] *= amplitude;
+      s[i] *= signed_amplitude;
+    }
+  }
+  for (int h0 = 0; h0 < heads; h0 += HEADS) {
+    if (h0) fetch(h0);
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      if (h0 + h >= heads) break;
+      if (turns) {
+        float v[HALVES ? 2 * N : N];
+        widen<T, N>(a[h], v);
+        if constexpr (HALVES) widen<T, N>(b[h], v + N);
+        if constexpr (HALVES && N % 2 == 0) {
+#pragma unroll
+          for (int i = 0; i < N; i += 2) {
+            const two va = pack2(v[i], v[i + 1]), vb = pack2(v[N + i], v[N + i + 1]), cc = pack2(c[i], c[i + 1]), ss = pack2(s[i], s[i + 1]);
+            unpack2(fma2(vb, pack2(-s[i], -s[i + 1]), mul2(va, cc)), v + i);
+            unpack2(fma2(va, ss, mul2(vb, cc)), v + N + i);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < PAIRS_; ++i) {
+            const int ia = HALVES ? i : 2 * i, ib = HALVES ? N + i : 2 * i + 1;
+            const float va = v[ia], vb = v[ib];
+            v[ia] = fmaf(-vb, s[i], va * c[i]);
+            v[ib] = fmaf(va, s[i], vb * c[i]);
+          }
+        }
+        a[h] = narrow<T, N>(v);
+        if constexpr (HALVES) b[h] = narrow<T, N>(v + N);
+      }
+      store<T, N, VEC>(y + h * p.head_dim, a[h]);
+      if constexpr (HALVES) store<T, N, VEC>(y + h * p.head_dim + partner, b[h]);
+    }
+    y += HEADS * p.head_dim;
+  }
+}
+
+template <typename T, int N>
+void launch(fax_ctx* ctx, int layout, bool vec, int grid, const RotaryParams& p) {
+  void (*kernel)(RotaryParams);
+  if (layout == FAX_ROTARY_HALVES) kernel = rotary_kernel<T, FAX_ROTARY_HALVES, N, true>;
+  else if (vec) kernel = rotary_kernel<T, FAX_ROTARY_PAIRS, (N > 1 ? N : 2), true>;
+  else kernel = rotary_kernel<T, FAX_ROTARY_PAIRS, 2, false>;
+  fax_launch(ctx, kernel, dim3(grid), dim3(THREADS), 0, p);
 }
 
 }  // namespace
@@ -150,39 +209,46 @@ extern "C" fax_status fax_op_rotary(fax_ctx* ctx, int32_t prec, const fax_rotary
   const bool in_place = d->x == d->y;
   if (in_place && d->ldx != d->ldy) return FAX_ERR_INVALID_ARG;
 
-  // Elements a side of a unit: as many as fill 16 bytes, or 8 of them, where heads, pairs and rows divide into such vectors.
+  if (!in_place && d->head_dim % 2) return FAX_ERR_UNSUPPORTED_SHAPE;         // the copied rest has a last element without a partner
+
+  // Elements of a vector: as many as fill 16 bytes, or 8, where heads, pairs and rows divide into such vectors; else single
+  // elements (HALVES) or pairs (PAIRS).
   const int half = d->rot_dim / 2, moved = in_place ? d->rot_dim : d->head_dim;
-  auto fits = [&](int np) {
-    return half % np == 0 && moved % (2 * np) == 0 && d->head_dim % np == 0 && fax_rows_aligned(d->x, d->ldx, es, np * es) && fax_rows_aligned(d->y, d->ldy, es, np * es);
+  const bool halves = d->layout == FAX_ROTARY_HALVES;
+  auto fits = [&](int n) {
+    return (halves ? half % n == 0 && moved % (2 * n) == 0 : d->rot_dim % n == 0 && moved % n == 0) && d->head_dim % n == 0 && fax_rows_aligned(d->x, d->ldx, es, n * es) &&
+           fax_rows_aligned(d->y, d->ldy, es, n * es);
   };
-  const int np = es == 2 && fits(8) ? 8 : fits(4) ? 4 : 1;
-  // Odd head_dim: the copied rest has a last element without a partner.
-  if (moved % 2) return FAX_ERR_UNSUPPORTED_SHAPE;
+  const int full = (int)(16 / es), n = fits(full) ? full : fits(full / 2) ? full / 2 : halves ? 1 : 2;
+  const bool vec = n > 2 || halves || fits(n);
 
   RotaryParams p;
   p.x = d->x; p.y = d->y; p.ldx = d->ldx; p.ldy = d->ldy; p.positions = d->positions; p.freq = d->frequencies;
-  p.rows = d->rows; p.half = half; p.head_dim = d->head_dim; p.first = d->first; p.seq = d->seq;
-  p.turned = half / np;
-  p.head_units = FastDiv((uint32_t)(moved / (2 * np)));
-  p.row_units = FastDiv((uint32_t)d->heads * p.head_units.d);
+  p.rows = d->rows; p.heads = d->heads; p.half = half; p.head_dim = d->head_dim; p.first = d->first; p.seq = d->seq;
+  p.turned = halves ? half / n : d->rot_dim / n;
   p.amplitude = d->amplitude; p.backward = d->backward != 0;
-  // Rows of a block: about as many as its threads hold at a time, within the table, and no fewer blocks than SMs.
-  int64_t rows = (THREADS * UNITS + p.row_units.d - 1) / p.row_units.d;
-  rows = rows < 1 ? 1 : rows;
-  const int64_t table_rows = TABLE_BYTES / ((int64_t)half * 8), even = (d->rows + ctx->sm_count - 1) / ctx->sm_count;
-  if (rows > table_rows) rows = table_rows;
-  if (rows > even) rows = even;
-  p.block_rows = (int32_t)rows;
-  const int grid = (int)((d->rows + rows - 1) / rows);
-  const size_t smem = (size_t)rows * half * 8;
+  const int64_t units = halves ? moved / (2 * n) : moved / n;
+  // Heads of a thread: all of them, or so few that there are 32 warps an SM (16384 x 24 x 64 in place: 25 us with 16, 22 us with 32, 23 us
+  // with 48 of them; a thread's factors cost as much as a few heads).
+  const int64_t want = 32 * 32 * (int64_t)ctx->sm_count;
+  int64_t parts = (want + units * d->rows - 1) / (units * d->rows);
+  if (parts > d->heads) parts = d->heads;
+  p.per = (int32_t)((d->heads + parts - 1) / parts);
+  const int64_t all = units * d->rows * ((d->heads + p.per - 1) / p.per);
+  if (all > 0x7fffffff) return FAX_ERR_UNSUPPORTED_SHAPE;
+  p.threads = all;
+  p.units = FastDiv((uint32_t)units);
+  p.tokens = FastDiv((uint32_t)d->rows);
+  const int grid = (int)((all + THREADS - 1) / THREADS);
   FaxProfScope prof(ctx, KC_ROTARY, 3.0 * d->rows * d->heads * d->rot_dim, 2.0 * d->rows * d->heads * moved * es + (d->positions ? 4.0 * d->rows : 0.0));
   if (prec == FAX_PREC_BF16) {
-    if (np == 8) launch<bf16, 8>(ctx, d->layout, grid, smem, p);
-    else if (np == 4) launch<bf16, 4>(ctx, d->layout, grid, smem, p);
-    else launch<bf16, 1>(ctx, d->layout, grid, smem, p);
+    if (n == 8) launch<bf16, 8>(ctx, d->layout, vec, grid, p);
+    else if (n == 4) launch<bf16, 4>(ctx, d->layout, vec, grid, p);
+    else launch<bf16, 1>(ctx, d->layout, vec, grid, p);
   } else {
-    if (np == 4) launch<float, 4>(ctx, d->layout, grid, smem, p);
-    else launch<float, 1>(ctx, d->layout, grid, smem, p);
+    if (n == 4) launch<float, 4>(ctx, d->layout, vec, grid, p);
+    else if (n == 2 && vec) launch<float, 2>(ctx, d->layout, vec, grid, p);
+    else launch<float, 1>(ctx, d->layout, vec, grid, p);
   }
   return fax_after_launch(ctx);
 }
