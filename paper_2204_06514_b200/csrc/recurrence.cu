@@ -173,7 +173,7 @@ struct Place {
   uint32_t rank, ctas;
   int64_t lo, block0;                            // first row, first kept state
   int c0;                                        // first of the lane's channels
-  bool live0, live1;
+  bool live0, live1, whole;                      // channels there are; all of the warp's
   int span, rounds;                              // tokens of a round
   static constexpr int STEP = ROWS == SINGLES ? 32 : 1;          // from the first channel to the second
   __device__ __forceinline__ bool set(const RecurrenceParams& p) {
@@ -197,6 +197,7 @@ struct Place {
     c0 = tile * CHANNELS + (ROWS == SINGLES ? lane : 2 * lane);
     live0 = c0 < p.d;
     live1 = c0 + STEP < p.d;
+    whole = (tile + 1) * CHANNELS <= p.d;
     if (p.offsets) {
       const int a = min(max(p.offsets[seq], 0), p.rows), b = min(max(p.offsets[seq + 1], a), p.rows);
       lo = a; n = b - a;
@@ -215,8 +216,13 @@ struct Place {
     if (ROWS != SINGLES) { if (live0) *reinterpret_cast<float2*>(row + c0) = f; }
     else { if (live0) row[c0] = f.x; if (live1) row[c0 + STEP] = f.y; }
   }
-  template <typename T>
+  // ALL: rows and channels are all there.
+  template <bool ALL, typename T>
   __device__ __forceinline__ Raw<T> load(const T* at, bool row) const {      // at: the lane's first channel
+    if (ALL) {
+      if (ROWS != SINGLES) return *reinterpret_cast<const Raw<T>*>(at);
+      return Raw<T>::of(at[0], at[STEP]);
+    }
     if (ROWS != SINGLES) {
       Raw<T> r = Raw<T>::of(0ull);
       if (live0 && row) r = *reinterpret_cast<const Raw<T>*>(at);
@@ -241,38 +247,43 @@ __device__ __forceinline__ void join(const Exchange& ex, const P& at, int round,
   Link* const ctas = ex.ctas(parity) + at.lane;
   warps[me * 32] = mine;
   __syncthreads();
-  // the warps before this one; the last warp then knows the CTA's
+  // the links before this one's, and with them the state before it
   Link all{pack2(1.f, 1.f), pack2(0.f, 0.f)};
-  const int upto = at.ctas == 1 ? ex.n_warps : me;
-  two a0 = all.a, b0 = all.b;
 #pragma unroll 4
-  for (int i = 0; i < upto; ++i) {
-    if (i == me) { a0 = all.a; b0 = all.b; }
+  for (int i = 0; i < me; ++i) {
     const Link s = warps[i * 32];
     all.a = mul2(all.a, s.a);
     all.b = fma2(s.a, all.b, s.b);
   }
   if (at.ctas == 1) {
-    start = fma2(a0, carry, b0);
-    carry = fma2(all.a, carry, all.b);
+    start = fma2(all.a, carry, all.b);
+    carry = fma2(mine.a, start, mine.b);
+#pragma unroll 4
+    for (int i = me + 1; i < ex.n_warps; ++i) {
+      const Link s = warps[i * 32];
+      carry = fma2(s.a, carry, s.b);
+    }
     return;
   }
-  const uint32_t my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
+  const int my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
   const uint32_t bar = ex.bars + 8 * parity;
   if (threadIdx.x == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
-  if (me == ex.n_warps - 1) {
+  if (me == ex.n_warps - 1) {                    // which knows the CTA's
     const Link cta{mul2(all.a, mine.a), fma2(mine.a, all.b, mine.b)};
     for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, cta);
   }
   wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status);
-  two before = carry;
 #pragma unroll 4
-  for (uint32_t c = 0; c < at.ctas; ++c) {
-    if (c == my_cta) before = carry;
+  for (int c = 0; c < my_cta; ++c) {
     const Link s = ctas[c * 32];
     carry = fma2(s.a, carry, s.b);
   }
-  start = fma2(all.a, before, all.b);
+  start = fma2(all.a, carry, all.b);
+#pragma unroll 4
+  for (int c = my_cta; c < (int)at.ctas; ++c) {
+    const Link s = ctas[c * 32];
+    carry = fma2(s.a, carry, s.b);
+  }
 }
 
 // ---- rows coming in ----
@@ -287,28 +298,29 @@ struct Inputs {
   __device__ __forceinline__ Raw<T>* place(int i) const { return reinterpret_cast<Raw<T>*>(at + K * box_bytes<T>() + i * CHANNELS * (int)sizeof(T)); }
   __device__ __forceinline__ two get(int k, int i) const { return reinterpret_cast<const Raw<T>*>(at + k * box_bytes<T>() + i * CHANNELS * (int)sizeof(T))->wide(); }
   // PAIRS and SINGLES: through registers, R rows' loads on their way together.
-  template <int R, typename P>
-  __device__ __forceinline__ void fetch(const P& pl, const T* const (&src)[N], const int64_t (&ld)[N], int64_t row, int from, int count) const {
+  template <int R, bool ALL, typename P>
+  __device__ __forceinline__ void fetch(const P& pl, const T* const (&src)[N], const int64_t (&ld)[N], int64_t row, int count) const {
     Raw<T> r[N][R];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const T* q = src[k] + (row + from) * ld[k] + pl.c0;
+      const T* q = src[k] + row * ld[k] + pl.c0;
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        r[k][i] = pl.load(q, from + i < count);
+        r[k][i] = pl.template load<ALL>(q, i < count);
         q += ld[k];
       }
     }
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
-      for (int i = 0; i < R; ++i) *reinterpret_cast<Raw<T>*>(at + k * box_bytes<T>() + (from + i) * CHANNELS * (int)sizeof(T)) = r[k][i];
+      for (int i = 0; i < R; ++i) *reinterpret_cast<Raw<T>*>(at + k * box_bytes<T>() + i * CHANNELS * (int)sizeof(T)) = r[k][i];
   }
   template <typename P>
   __device__ __forceinline__ void fetch(const P& pl, const T* const (&src)[N], const int64_t (&ld)[N], int64_t row, int count) const {
-    if (count > 4) fetch<STEPS>(pl, src, ld, row, 0, count);
-    else if (count > 1) fetch<4>(pl, src, ld, row, 0, count);
-    else if (count == 1) fetch<1>(pl, src, ld, row, 0, count);
+    if (count == STEPS && pl.whole) fetch<STEPS, true>(pl, src, ld, row, count);
+    else if (count > 4) fetch<STEPS, false>(pl, src, ld, row, count);
+    else if (count > 1) fetch<4, false>(pl, src, ld, row, count);
+    else if (count == 1) fetch<1, false>(pl, src, ld, row, count);
   }
 };
 
