@@ -14,6 +14,12 @@ profiler.
   python -m paper_2204_06514_b200.opbench fp8_quantize --rows 8192 --d 4096 [--tile 1 --only straight|transposed]
   python -m paper_2204_06514_b200.opbench embed_fwd --rows 16384 --d 768 --vocab 50304
   python -m paper_2204_06514_b200.opbench embed_bwd --rows 16384 --d 768 --vocab 50304 [--acc 1]
+  python -m paper_2204_06514_b200.opbench rotary --rows 16384 --heads 24 --hd 64 [--rot 64 --layout halves|pairs]   # in place in a fused q | k | v
+  python -m paper_2204_06514_b200.opbench dropout --rows 16384 --d 768 [--resid 0]
+  python -m paper_2204_06514_b200.opbench recurrence_fwd --batch 16 --seq 1024 --d 768 [--gate 0]
+  python -m paper_2204_06514_b200.opbench recurrence_bwd --batch 16 --seq 1024 --d 768 [--gate 0]
+  python -m paper_2204_06514_b200.opbench expert_sort --rows 16384 --top-k 2 --experts 8 [--capacity 5120 | --align 128]
+  python -m paper_2204_06514_b200.opbench expert_dispatch | expert_combine | expert_combine_bwd --rows 16384 --d 768 (as above)
 """
 from __future__ import annotations
 
@@ -26,7 +32,7 @@ import torch
 from . import binding as fx
 from . import binding_ops as ops
 from . import build
-from .state import Session, hparams
+from .state import Session, hparams, rotary_frequencies
 
 
 def P(t):
@@ -36,7 +42,8 @@ def P(t):
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("op", choices=["gemm", "attn_fwd", "attn_bwd", "ln_fwd", "ln_bwd", "adamw", "adamw8", "fp8_gemm",
-                                   "fp8_quantize", "embed_fwd", "embed_bwd"])
+                                   "fp8_quantize", "embed_fwd", "embed_bwd", "rotary", "dropout", "recurrence_fwd", "recurrence_bwd",
+                                   "expert_sort", "expert_dispatch", "expert_combine", "expert_combine_bwd"])
     ap.add_argument("--m", type=int, default=8192); ap.add_argument("--n", type=int, default=4096)
     ap.add_argument("--k", type=int, default=4096)
     ap.add_argument("--a-mn", type=int, default=0); ap.add_argument("--b-mn", type=int, default=1)
@@ -47,6 +54,10 @@ def main():
     ap.add_argument("--b-tile", type=int, default=128, choices=[1, 128]); ap.add_argument("--acc", type=int, default=0)
     ap.add_argument("--tile", type=int, default=1, choices=[1, 128]); ap.add_argument("--only", choices=["straight", "transposed"])
     ap.add_argument("--vocab", type=int, default=50304)
+    ap.add_argument("--rot", type=int, default=0); ap.add_argument("--layout", choices=["halves", "pairs"], default="halves")
+    ap.add_argument("--resid", type=int, default=1); ap.add_argument("--gate", type=int, default=1)
+    ap.add_argument("--top-k", type=int, default=2); ap.add_argument("--experts", type=int, default=8)
+    ap.add_argument("--capacity", type=int, default=0); ap.add_argument("--align", type=int, default=128)
     ap.add_argument("--iters", type=int, default=20); ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--l2-budget-mb", type=float, default=-1.0, help="GEMM raster: L2 bytes for resident panels (0: fixed order)")
     a = ap.parse_args()
@@ -139,6 +150,63 @@ def main():
             scratch = s.arena(nb)
             fn = lambda: ops.fax_op_embedding_backward(s.ctx, 0, n, V, d, P(ids), P(x), d ** 0.5, a.acc, P(table), P(scratch), nb)
             bytes_ = 2.0 * n * d + 4.0 * n + 4.0 * d * (2 * int(ids.unique().numel()) if a.acc else V)
+    elif a.op == "rotary":
+        R, H, hd = a.rows, a.heads, a.hd
+        rot = a.rot or hd
+        qkv = rn(R, (H + H // 2) * hd)
+        table = rotary_frequencies(dev, rot)
+        desc = ops.RotaryDesc(R, H, hd, rot, int(a.layout == "pairs"), P(qkv), qkv.shape[1], P(qkv), qkv.shape[1], None, 0, a.seq, P(table), 1.0, 0)
+        fn = lambda: ops.fax_op_rotary(s.ctx, 0, desc)
+        bytes_ = 4.0 * R * H * rot
+    elif a.op == "dropout":
+        R, d = a.rows, a.d
+        x, r, y = rn(R, d), rn(R, d), rn(R, d)
+        desc = ops.DropoutDesc(R, d, P(x), d, P(r) if a.resid else None, d, P(y), d, 0.1, 1, 0, None)
+        fn = lambda: ops.fax_op_dropout(s.ctx, 0, desc)
+        bytes_ = (4.0 + 2 * (a.resid != 0)) * R * d
+    elif a.op in ("recurrence_fwd", "recurrence_bwd"):
+        B_, T, d = a.batch, a.seq, a.d
+        R, k = B_ * T, 2 + (a.gate != 0)
+        proj, dproj, y, dy = rn(R, k * d), rn(R, k * d), rn(R, d), rn(R, d)
+        h0 = torch.zeros((B_, d), device=dev)
+        states = torch.empty(ops.fax_op_recurrence_states_floats(R, B_, d), device=dev)
+        col = lambda t, i: C.c_void_p(t.data_ptr() + 2 * i * d) if i < k else None
+        shape = (R, d, B_, T, None, ops.FAX_RECURRENCE_COMPLEMENT, col(proj, 0), k * d, col(proj, 1), k * d, col(proj, 2), k * d, P(h0))
+        fwd = ops.RecurrenceDesc(*shape, P(y), d, None, P(states))
+        bwd = ops.RecurrenceBackwardDesc(*shape, P(states), P(dy), d, None, col(dproj, 0), k * d, col(dproj, 1), k * d, col(dproj, 2), k * d, None)
+        ops.fax_op_recurrence_forward(s.ctx, 0, fwd)
+        if a.op == "recurrence_fwd":
+            fn = lambda: ops.fax_op_recurrence_forward(s.ctx, 0, fwd)
+            bytes_ = 2.0 * (k + 1) * R * d + R * d / 4
+        else:
+            fn = lambda: ops.fax_op_recurrence_backward(s.ctx, 0, bwd)
+            bytes_ = 2.0 * (2 * k + 1) * R * d + R * d / 4
+    elif a.op.startswith("expert"):
+        R, d, K, E = a.rows, a.d, a.top_k, a.experts
+        slots = ops.fax_op_expert_slots(R, K, E, a.capacity, a.align)
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=dev)
+        ids = torch.rand((R, E), generator=g, device=dev).topk(K, dim=1).indices.int()
+        slot_of, source, offsets, counts = i32(R, K), i32(slots), i32(E + 1), i32(E)
+        plan = ops.ExpertSortDesc(R, K, E, a.capacity, a.align, slots, P(ids), P(slot_of), P(source), P(offsets), P(counts))
+        ops.fax_op_expert_sort(s.ctx, plan)
+        x, z, y = rn(R, d), rn(slots, d), rn(R, d)
+        w, dw = torch.rand((R, K), generator=g, device=dev), torch.empty((R, K), device=dev)
+        where = (R, K, d, slots, P(slot_of))
+        if a.op == "expert_sort":
+            fn = lambda: ops.fax_op_expert_sort(s.ctx, plan)
+            bytes_ = 4.0 * (2 * R * K + slots + 2 * E)
+        elif a.op == "expert_dispatch":
+            desc = ops.ExpertDispatchDesc(*where, P(source), P(x), d, P(z), d)
+            fn = lambda: ops.fax_op_expert_dispatch(s.ctx, 0, desc)
+            bytes_ = 2.0 * d * (R + slots)
+        elif a.op == "expert_combine":
+            desc = ops.ExpertCombineDesc(*where, P(w), P(z), d, P(x), d, P(y), d)
+            fn = lambda: ops.fax_op_expert_combine(s.ctx, 0, desc)
+            bytes_ = 2.0 * d * (R * K + 2 * R)
+        else:
+            desc = ops.ExpertCombineBackwardDesc(*where, P(source), P(w), P(z), d, P(x), d, P(z), d, P(dw))
+            fn = lambda: ops.fax_op_expert_combine_backward(s.ctx, 0, desc)
+            bytes_ = 2.0 * d * (R * K + slots + R)
     elif a.op == "adamw8":
         n = a.n if a.n > 4096 else 201379840
         w = torch.randn(n, generator=g, device=dev); gr = torch.randn(n, generator=g, device=dev)
