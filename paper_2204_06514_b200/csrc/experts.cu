@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const Sort
   const uint32_t before_me = (1u << lane) - 1;
   for (int i = threadIdx.x; i < n_warps * p.experts; i += threads) mine[i] = 0;
   __syncthreads();
-  if (n_ctas > 1) cluster_sync();                                   // the others run: their shared memory can be written
+  if (n_ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   fax_grid_dependency_wait();
 
   // this warp's choices: whole groups of 32, GROUPS of them read at a time; the first ones stay for the second walk
@@ -77,6 +77,7 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const Sort
   int32_t* const count = mine + warp * p.experts;
   const int bits = 32 - __clz(p.experts);         // of 0 to experts
   int x[GROUPS];
+  uint32_t same[GROUPS];
   auto read = [&](int64_t c) {
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) {
@@ -84,6 +85,9 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const Sort
       x[k] = at < hi ? p.ids[at] : -1;
       if ((uint32_t)x[k] >= (uint32_t)p.experts) x[k] = p.experts;                // none
     }
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k)
+      if (c + 32 * k < hi) same[k] = alike(x[k], bits);
   };
   // (from the end, so that the first ones are read last)
   const int64_t last = lo < hi ? lo + (hi - lo - 1) / (32 * GROUPS) * (32 * GROUPS) : lo - 1;
@@ -92,13 +96,13 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const Sort
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) {
       if (c + 32 * k >= hi) break;
-      const uint32_t same = alike(x[k], bits);
-      if (x[k] < p.experts && (same & before_me) == 0) count[x[k]] += __popc(same);
+      if (x[k] < p.experts && (same[k] & before_me) == 0) count[x[k]] += __popc(same[k]);
       __syncwarp();
     }
   }
   __syncthreads();
   // over the warps: what each starts from within the CTA, and the CTA's counts for everyone
+  if (n_ctas > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");              // the others run: their shared memory can be written
   for (int e = threadIdx.x; e < p.experts; e += threads) {
     int sum = 0;
 #pragma unroll 8
@@ -143,14 +147,13 @@ __global__ void __launch_bounds__(SORT_WARPS * 32) expert_sort_kernel(const Sort
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) {
       if (c + 32 * k >= hi) break;
-      const uint32_t same = alike(x[k], bits);
       int slot = -1;
       if (x[k] < p.experts) {
-        const uint32_t next = (uint32_t)first[x[k]] + (uint32_t)count[x[k]] + __popc(same & before_me);     // below 2^32: slots and choices are below 2^31
+        const uint32_t next = (uint32_t)first[x[k]] + (uint32_t)count[x[k]] + __popc(same[k] & before_me);     // below 2^32: slots and choices are below 2^31
         slot = p.capacity && next >= (int64_t)(x[k] + 1) * p.capacity ? -1 : (int)next;
       }
       __syncwarp();
-      if (x[k] < p.experts && (same & before_me) == 0) count[x[k]] += __popc(same);
+      if (x[k] < p.experts && (same[k] & before_me) == 0) count[x[k]] += __popc(same[k]);
       __syncwarp();
       const int64_t at = c + 32 * k + lane;
       if (at < hi) {
@@ -241,7 +244,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) dispatch_kernel(const RowParam
 }
 
 template <typename T, int N, int GROUP, int K>
-__global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_kernel(const RowParams p) {
+__global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 4) combine_kernel(const RowParams p) {
   fax_grid_dependency_wait();
   const int lane = threadIdx.x % GROUP;
   const int64_t item = (int64_t)blockIdx.x * (ROW_THREADS / GROUP) + threadIdx.x / GROUP;
@@ -283,7 +286,7 @@ __global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_kernel(con
 
 // in: dy; out: dz.  The products of a choice are summed over a thread's vectors, the group's lanes by halves, its warps in order.
 template <typename T, int N, int GROUP, int K>
-__global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_backward_kernel(const RowParams p) {
+__global__ void __launch_bounds__(ROW_THREADS, 4) combine_backward_kernel(const RowParams p) {
   __shared__ float sums[GROUP > 32 ? ROW_THREADS / 32 : 1][K];
   fax_grid_dependency_wait();
   const int lane = threadIdx.x % GROUP;
@@ -348,21 +351,22 @@ __global__ void __launch_bounds__(ROW_THREADS, K > 4 ? 2 : 3) combine_backward_k
 
 enum RowOp { DISPATCH, COMBINE, COMBINE_BACKWARD };
 
-template <typename T, int N, int GROUP, int K>
+// Choices at a time (K): as many loads on their way as registers hold beside four blocks an SM; more of them in two blocks' worth
+// pays where a sum is all there is to keep (6 of 64, 8191 x 2048: combine 58 us with 4 or 3 at a time, 50 us with 6; its gradient 98 us with
+// 8 at a time, 89 us with 3; 4 of 16: 33 and 58 us with 4 at a time in four blocks, 42 and 72 us in two).
+template <typename T, int N, int GROUP>
 fax_status launch_rows(fax_ctx* ctx, RowOp op, RowParams p) {
   constexpr int PER_BLOCK = ROW_THREADS / GROUP;
   p.slot_groups = op == COMBINE ? 0 : (((int64_t)p.slots + 31) / 32 + PER_BLOCK - 1) / PER_BLOCK * PER_BLOCK;      // whole blocks, so that none has both kinds of work
   const int64_t groups = p.slot_groups + p.n_tokens;
   const dim3 grid((unsigned)((groups + PER_BLOCK - 1) / PER_BLOCK)), threads(ROW_THREADS);
-  if (op == DISPATCH) fax_launch(ctx, dispatch_kernel<T, N, GROUP, K>, grid, threads, 0, p);
-  else if (op == COMBINE) fax_launch(ctx, combine_kernel<T, N, GROUP, K>, grid, threads, 0, p);
-  else fax_launch(ctx, combine_backward_kernel<T, N, GROUP, K>, grid, threads, 0, p);
+  const int k = p.top_k;
+  void (*kernel)(RowParams);
+  if (op == DISPATCH) kernel = k <= 2 ? dispatch_kernel<T, N, GROUP, 2> : k <= 4 ? dispatch_kernel<T, N, GROUP, 4> : dispatch_kernel<T, N, GROUP, 8>;
+  else if (op == COMBINE) kernel = k == 1 ? combine_kernel<T, N, GROUP, 1> : k == 2 ? combine_kernel<T, N, GROUP, 2> : k <= 4 ? combine_kernel<T, N, GROUP, 4> : k <= 6 ? combine_kernel<T, N, GROUP, 6> : combine_kernel<T, N, GROUP, 8>;
+  else kernel = k == 1 ? combine_backward_kernel<T, N, GROUP, 1> : k == 2 ? combine_backward_kernel<T, N, GROUP, 2> : k == 3 || k == 5 || k == 6 ? combine_backward_kernel<T, N, GROUP, 3> : combine_backward_kernel<T, N, GROUP, 4>;
+  fax_launch(ctx, kernel, grid, threads, 0, p);
   return fax_after_launch(ctx);
-}
-template <typename T, int N, int GROUP>
-fax_status launch_rows(fax_ctx* ctx, RowOp op, const RowParams& p) {
-  if (p.top_k <= 2) return launch_rows<T, N, GROUP, 2>(ctx, op, p);
-  return p.top_k <= 4 ? launch_rows<T, N, GROUP, 4>(ctx, op, p) : launch_rows<T, N, GROUP, 8>(ctx, op, p);
 }
 template <typename T, int N>
 fax_status launch_rows(fax_ctx* ctx, RowOp op, bool block, const RowParams& p) {
@@ -409,7 +413,8 @@ extern "C" fax_status fax_op_expert_sort(fax_ctx* ctx, const fax_expert_sort_des
   SortParams p;
   p.choices = d->n_tokens * d->top_k; p.experts = d->n_experts; p.capacity = d->capacity; p.align = d->capacity ? 1 : d->align; p.slots = d->slots;
   p.ids = d->ids; p.slot_of = d->slot_of; p.source = d->source; p.offsets = d->offsets; p.counts = d->counts;
-  // Warps for every 64 choices, one CTA of them or a cluster's; threads for every expert.
+  // Warps for every 64 choices, one CTA of them or a cluster's (49146 choices, 64 experts: 15.5 us on 8 CTAs, 12 us on 16: the slots' scattered
+  // stores); threads for every expert.
   const int cluster = p.choices <= SORT_WARPS * 32 * GROUPS ? 1 : p.choices <= 4 * SORT_WARPS * 32 * GROUPS ? 8 : SORT_CLUSTER;
   int warps = (p.choices / cluster + 63) / 64;
   if (warps < (p.experts + 31) / 32) warps = (p.experts + 31) / 32;
@@ -418,7 +423,12 @@ extern "C" fax_status fax_op_expert_sort(fax_ctx* ctx, const fax_expert_sort_des
   const int smem_max = (SORT_WARPS + SORT_CLUSTER + 1) * FAX_EXPERT_MAX * 4, smem = (warps + cluster + 1) * p.experts * 4;
   static bool done[FAX_MAX_DEVICES] = {};
   FAX_TRY(fax_opt_in_shared_memory(ctx, expert_sort_kernel, smem_max, done));
-  if (cluster > 8) FAX_CUDA_TRY(ctx, cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  static bool wide[FAX_MAX_DEVICES] = {};
+  const bool tracked = ctx->device >= 0 && ctx->device < FAX_MAX_DEVICES;
+  if (cluster > 8 && !(tracked && wide[ctx->device])) {
+    FAX_CUDA_TRY(ctx, cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (tracked) wide[ctx->device] = true;
+  }
   FaxProfScope prof(ctx, KC_EXPERT, 0.0, 4.0 * (2.0 * p.choices + p.slots + 2.0 * p.experts));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cluster); cfg.blockDim = dim3(warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = ctx->stream;

@@ -131,6 +131,22 @@ def test_channels_and_sequences_that_fill_the_gpu(sess):
     layer.check()
 
 
+@pytest.mark.parametrize("prec", [0, 1])
+@pytest.mark.parametrize("lengths", [[1] * 40, [2, 0, 1, 2, 0], [1]])
+def test_a_token_or_two(sess, lengths, prec):
+    """Widths of whole 16-byte vectors and others, sequences of 0 to 2 tokens, and longer ones than the caller says."""
+    for d, gated, mode, uniform in ((64, True, ref.COMPLEMENT, True), (8, False, ref.PLAIN, False), (24, True, ref.PLAIN, False), (1032, False, ref.COMPLEMENT, False), (12, True, ref.COMPLEMENT, True)):
+        layer = Layer(sess, prec, lengths, d, gated, mode, d, uniform=uniform and len(set(lengths)) == 1)
+        layer.forward()
+        layer.backward()
+        layer.check()
+    layer = Layer(sess, prec, [40, 17], 64, True, ref.COMPLEMENT, 5)
+    layer.seq = 1
+    layer.forward()
+    layer.backward()
+    layer.check()
+
+
 def test_without_states_gate_or_initial_values(sess):
     layer = Layer(sess, 0, [100, 50], 64, False, ref.PLAIN, 2, h0=False, dh_last=False)
     layer.forward(keep=False)
