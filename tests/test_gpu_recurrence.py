@@ -104,7 +104,8 @@ LENGTHS = {"one token": [1], "tokens of many": [1] * 70, "a stretch": [16, 16], 
 @pytest.mark.parametrize("lengths", list(LENGTHS))
 def test_sequences(sess, lengths, gated, mode, prec):
     n = LENGTHS[lengths]
-    for d, fused, pad in ((70, True, 0), (33, False, 3)):
+    # rows in boxes (72 and 136: pitches of whole 16 bytes, a last tile of 8 channels), pairs or single channels (70, 33)
+    for d, fused, pad in ((70, True, 0), (33, False, 3), (72, True, 0), (136, False, 8)):
         layer = Layer(sess, prec, n, d, gated, mode, len(n) + d, fused=fused, pad=pad, uniform=len(set(n)) == 1 and fused, rows=None if fused else sum(n) + 5)
         if layer.uniform:
             layer.rows = layer.n_seq * layer.seq
@@ -175,6 +176,31 @@ def test_a_sequence_continued(sess, prec):
     whole.check(backward=False)
 
 
+@pytest.mark.parametrize("prec", [0, 1])
+@pytest.mark.parametrize("d", [64, 65])
+@pytest.mark.parametrize("said", [0, 1, 16, 17, 20, 100000])
+def test_the_longest_length_is_only_a_hint(sess, d, said, prec):
+    layer = Layer(sess, prec, [300, 5, 700], d, True, ref.COMPLEMENT, 17)
+    layer.seq = said
+    layer.forward()
+    layer.backward()
+    layer.check()
+
+
+@pytest.mark.parametrize("d", [64, 63])
+def test_what_lies_behind_a_sequence_is_not_looked_at(sess, d):
+    """A sequence's last rows share boxes with its neighbour's: NaN there, and in rows of no sequence, change nothing."""
+    clean, dirty = (Layer(sess, 0, [37, 16, 40], d, True, ref.PLAIN, 18, rows=100) for _ in range(2))
+    for t in (dirty.tf, dirty.tx, dirty.tg, dirty.tdy):
+        t[37:53] = float("nan")
+        t[93:] = float("nan")
+    for layer in (clean, dirty):
+        layer.forward()
+        layer.backward()
+    for a, b in ((clean.y, dirty.y), (clean.df, dirty.df), (clean.dx, dirty.dx), (clean.dg, dirty.dg)):
+        assert torch.equal(a[:37], b[:37]) and torch.equal(a[53:93], b[53:93]) and bool((b[93:] == 7).all())
+
+
 def test_gradients_in_place_of_their_inputs(sess):
     a, b = (Layer(sess, 0, [300, 20], 64, True, ref.COMPLEMENT, 6, fused=True) for _ in range(2))
     a.forward()
@@ -188,9 +214,11 @@ def test_gradients_in_place_of_their_inputs(sess):
 
 
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
-def test_values_that_are_not_finite_stay_in_their_sequence_and_channel(sess, value):
+@pytest.mark.parametrize("d", [66, 64])
+@pytest.mark.parametrize("prec", [0, 1])
+def test_values_that_are_not_finite_stay_in_their_sequence_and_channel(sess, value, d, prec):
     for name in ("f", "x", "g"):
-        clean, dirty = (Layer(sess, 0, [200, 40, 1], 66, True, ref.COMPLEMENT, 9) for _ in range(2))
+        clean, dirty = (Layer(sess, prec, [200, 40, 1], d, True, ref.COMPLEMENT, 9) for _ in range(2))
         getattr(dirty, "t" + name)[90, 5] = value
         for layer in (clean, dirty):
             layer.forward()
