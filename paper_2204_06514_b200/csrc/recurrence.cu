@@ -9,8 +9,8 @@
 // instructions, so that two channels share one wherever the hardware has it (f32x2).
 //
 // A warp has 64 channels, two a lane, and 16 tokens at a time.  Where sequences are few, a cluster of CTAs shares one:
-// each CTA has 8 warps, one after the other in time, and the CTAs of a cluster follow one another; (A, B) of a CTA goes to
-// the others through distributed shared memory, one cluster barrier a round of (CTAs * 128) tokens.  Where channels and sequences
+// each CTA has 4 to 8 warps, one after the other in time, and the CTAs of a cluster follow one another; (A, B) of a CTA goes to
+// the others through distributed shared memory, once a round of (CTAs * warps * 16) tokens.  Where channels and sequences
 // alone fill the GPU, or sequences are one stretch, each warp takes a whole sequence by itself.
 // The order of joining is fixed by the sizes: the same inputs give the same bits.
 #include <type_traits>
@@ -154,16 +154,20 @@ __device__ __forceinline__ void wait_sent(uint32_t bar, uint32_t parity, volatil
   }
 }
 
-// What warps and CTAs tell one another, in the order of joining.  Two of each in turn: a place is written again two rounds
-// later, by a warp (or for a CTA) that has seen every warp of this CTA pass the barrier of the round between, after its reading.
+// What warps and CTAs tell one another, in the order of joining.  The CTAs' links have two places that take turns: one is written again two rounds
+// later, by a CTA that has received this CTA's link of the round between, which was sent after the reading of it.
 struct Exchange {
-  Link* mem;                                     // [2][warps][32] of the CTA's warps, then [2][CTAs][32]
+  Link* links;                                   // [warps][32] of the CTA's warps
+  Link* ctas;                                    // [2][CTAs][32]
+  two* starts;                                   // [warps][32]: the states before the warps' stretches
   int n_warps, n_ctas;
   uint32_t bars;                                 // two barriers, of what the CTAs send
   volatile int* gave_up;
   int32_t* status;
-  __device__ __forceinline__ Link* warps(int parity) const { return mem + parity * n_warps * 32; }
-  __device__ __forceinline__ Link* ctas(int parity) const { return mem + (2 * n_warps + parity * n_ctas) * 32; }
+  __device__ __forceinline__ Exchange(uint8_t* mem, int warps, int n, volatile int* flag, int32_t* s)
+      : links(reinterpret_cast<Link*>(mem)), ctas(links + warps * 32), starts(reinterpret_cast<two*>(ctas + 2 * n * 32)), n_warps(warps), n_ctas(n),
+        bars(tc::smem_u32(starts + warps * 32)), gave_up(flag), status(s) {}
+  static __host__ __device__ constexpr int bytes(int warps, int n) { return (warps + 2 * n) * 32 * (int)sizeof(Link) + warps * 32 * (int)sizeof(two); }      // then the barriers
 };
 
 // Which stretches of which sequence a warp works on.
@@ -237,53 +241,54 @@ struct Place {
   }
 };
 
-// Joins the stretches of a round: mine is this warp's; carry: the state before the round, afterwards the one behind it; start: the
-// state before this warp's stretch.  FORWARD: earlier slots come first; else later ones.
+// Joins the stretches of a round: mine is this warp's; carry (of the first warp): the state before the round, afterwards the one behind
+// it; returns the state before this warp's stretch.  The first warp does it for all: every warp reading every link is bound by shared
+// memory (16 CTAs of 8 warps: 2400 of a round's 5200 cycles that way).  FORWARD: earlier slots come first; else later ones.
 template <bool FORWARD, typename P>
-__device__ __forceinline__ void join(const Exchange& ex, const P& at, int round, const Link& mine, two& carry, two& start) {
-  const int parity = round & 1;
+__device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, const Link& mine, two& carry) {
   const int me = FORWARD ? at.warp : ex.n_warps - 1 - at.warp;
-  Link* const warps = ex.warps(parity) + at.lane;
-  Link* const ctas = ex.ctas(parity) + at.lane;
-  warps[me * 32] = mine;
+  Link* const links = ex.links + at.lane;
+  links[me * 32] = mine;
   __syncthreads();
-  // the links before this one's, and with them the state before it
-  Link all{pack2(1.f, 1.f), pack2(0.f, 0.f)};
+  if (at.warp == 0) {
+    two state = carry;
+    if (at.ctas > 1) {
+      Link all{pack2(1.f, 1.f), 0ull};
 #pragma unroll 4
-  for (int i = 0; i < me; ++i) {
-    const Link s = warps[i * 32];
-    all.a = mul2(all.a, s.a);
-    all.b = fma2(s.a, all.b, s.b);
-  }
-  if (at.ctas == 1) {
-    start = fma2(all.a, carry, all.b);
-    carry = fma2(mine.a, start, mine.b);
+      for (int i = 0; i < ex.n_warps; ++i) {
+        const Link s = links[i * 32];
+        all.a = mul2(all.a, s.a);
+        all.b = fma2(s.a, all.b, s.b);
+      }
+      const int my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
+      const uint32_t bar = ex.bars + 8 * (round & 1);
+      Link* const ctas = ex.ctas + ((round & 1) * ex.n_ctas) * 32 + at.lane;
+      if (at.lane == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
 #pragma unroll 4
-    for (int i = me + 1; i < ex.n_warps; ++i) {
-      const Link s = warps[i * 32];
-      carry = fma2(s.a, carry, s.b);
+      for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, all);
+      wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status);
+#pragma unroll 4
+      for (int c = 0; c < my_cta; ++c) {
+        const Link s = ctas[c * 32];
+        carry = fma2(s.a, carry, s.b);
+      }
+      state = carry;
+#pragma unroll 4
+      for (int c = my_cta; c < (int)at.ctas; ++c) {
+        const Link s = ctas[c * 32];
+        carry = fma2(s.a, carry, s.b);
+      }
     }
-    return;
-  }
-  const int my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
-  const uint32_t bar = ex.bars + 8 * parity;
-  if (threadIdx.x == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
-  if (me == ex.n_warps - 1) {                    // which knows the CTA's
-    const Link cta{mul2(all.a, mine.a), fma2(mine.a, all.b, mine.b)};
-    for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, cta);
-  }
-  wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status);
 #pragma unroll 4
-  for (int c = 0; c < my_cta; ++c) {
-    const Link s = ctas[c * 32];
-    carry = fma2(s.a, carry, s.b);
+    for (int i = 0; i < ex.n_warps; ++i) {
+      const Link s = links[i * 32];
+      ex.starts[i * 32 + at.lane] = state;
+      state = fma2(s.a, state, s.b);
+    }
+    if (at.ctas == 1) carry = state;
   }
-  start = fma2(all.a, carry, all.b);
-#pragma unroll 4
-  for (int c = my_cta; c < (int)at.ctas; ++c) {
-    const Link s = ctas[c * 32];
-    carry = fma2(s.a, carry, s.b);
-  }
+  __syncthreads();
+  return ex.starts[me * 32 + at.lane];
 }
 
 // ---- rows coming in ----
@@ -365,7 +370,7 @@ __device__ __forceinline__ void written() { tc::fence_proxy_async(); __syncwarp(
 
 __host__ __device__ constexpr int align128(int n) { return (n + 127) / 128 * 128; }
 // Shared memory: the exchange of a cluster (its bytes), its two barriers and each warp's, then the warps' buffers (their place).
-template <bool CLUSTER> __host__ __device__ constexpr int exchange_bytes(int warps, int ctas) { return CLUSTER ? 2 * (warps + ctas) * 32 * (int)sizeof(Link) : 0; }
+template <bool CLUSTER> __host__ __device__ constexpr int exchange_bytes(int warps, int ctas) { return CLUSTER ? Exchange::bytes(warps, ctas) : 0; }
 template <bool CLUSTER> __host__ __device__ constexpr int buffers_at(int warps, int ctas) { return align128(exchange_bytes<CLUSTER>(warps, ctas) + 16 + warps * 8 * MAX_STAGES); }
 
 template <typename T, int ROWS, bool GATE, bool COMPLEMENT, bool CLUSTER>
@@ -374,7 +379,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
   extern __shared__ __align__(128) uint8_t mem[];
   __shared__ int gave_up;
   const int ctas = CLUSTER ? (int)cluster_size() : 1;
-  const Exchange ex{reinterpret_cast<Link*>(mem), p.warps, ctas, tc::smem_u32(mem + exchange_bytes<CLUSTER>(p.warps, ctas)), &gave_up, p.status};
+  const Exchange ex(mem, p.warps, ctas, &gave_up, p.status);
   const int warp_buffer = p.stages * N * box_bytes<T>();
   if (threadIdx.x == 0) {
     gave_up = 0;
@@ -437,7 +442,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
         else at.store(out + i * p.ldy, Raw<T>::of(y));
       };
       if constexpr (CLUSTER) {
-        two a[STEPS], b[STEPS], h;
+        two a[STEPS], b[STEPS];
         Link mine{pack2(1.f, 1.f), pack2(0.f, 0.f)};
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
@@ -451,7 +456,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
           }
         }
         if (ROWS == TILES && ahead > 0) ask(round + ahead, ahead);
-        join<true>(ex, at, round, mine, carry, h);
+        two h = join<true>(ex, at, round, mine, carry);
         if (kept) at.store_state(kept, h);
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
@@ -521,7 +526,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
   extern __shared__ __align__(128) uint8_t mem[];
   __shared__ int gave_up;
   const int ctas = CLUSTER ? (int)cluster_size() : 1;
-  const Exchange ex{reinterpret_cast<Link*>(mem), p.warps, ctas, tc::smem_u32(mem + exchange_bytes<CLUSTER>(p.warps, ctas)), &gave_up, p.status};
+  const Exchange ex(mem, p.warps, ctas, &gave_up, p.status);
   const int warp_buffer = p.stages * N * box_bytes<T>();
   uint8_t* const buffer = mem + buffers_at<CLUSTER>(p.warps, ctas) + (threadIdx.x / 32) * warp_buffer;
   if (threadIdx.x == 0) {
@@ -608,7 +613,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
             mine.a = mul2(mine.a, a[i]);
             mine.b = mul2(a[i], add2(u_of(i), mine.b));
           }
-        join<false>(ex, at, round, mine, carry, e);
+        e = join<false>(ex, at, round, mine, carry);
       }
       const int last = (FULL ? STEPS : count) - 1;
       T* df = row_of(p.df, p.lddf, last);
