@@ -200,7 +200,7 @@ fax_status fax_op_fp8_gemm_tile(const fax_ctx* ctx, int32_t M, int32_t N, int32_
  * is positions[row] (int32, device), or without positions first + row % seq (seq = 0: first + row).  frequencies: device,
  * rot_dim / 2 words from fax_rotary_frequencies.  The angle is exact modulo a turn at any position (whole numbers
  * modulo 2^64); y is rounded once to T.  rows = 0 does nothing; rot_dim is even,
- * head_dim <= FAX_ROTARY_MAX_DIM and, where y is not x, even too. */
+ * head_dim <= FAX_ROTARY_MAX_DIM and, where y is not x, even too; rows <= 2^30, heads * head_dim <= 2^24. */
 enum { FAX_ROTARY_HALVES = 0, FAX_ROTARY_PAIRS = 1 };
 #define FAX_ROTARY_MAX_DIM 1024
 typedef struct {
@@ -251,7 +251,8 @@ fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropout_desc* de
  * rows offsets[s] to offsets[s + 1] - 1, with seq the longest one's length (a choice of kernel goes by it, no result); rows outside stay as
  * they were.  Offsets outside [0, rows] are taken as the nearest end, a falling one as an empty sequence.
  * states: NULL, or for the backward pass fax_op_recurrence_states_floats floats, which receive h before every 16th token.
- * y holds no element of f, x or g.  The same inputs give the same bits.  rows = 0 still writes h_last. */
+ * y holds no element of f, x or g.  The same inputs give the same bits.  rows = 0 still writes h_last.  rows <= 2^30,
+ * d <= 2^24, n_seq * ceil(d / 64) <= 2^27 - 1. */
 enum { FAX_RECURRENCE_PLAIN = 0, FAX_RECURRENCE_COMPLEMENT = 1 };
 #define FAX_RECURRENCE_BLOCK 16
 typedef struct {

@@ -22,7 +22,8 @@ struct RotaryParams {
   const void* x; void* y; int64_t ldx, ldy;
   const int32_t* positions;
   const uint64_t* freq;
-  int32_t rows, heads, head_dim, half, first, seq;
+  int32_t heads, head_dim, half, first, seq;
+  int64_t row0;                                   // of the launch's first row
   int32_t turned;                                 // units of a head that turn; those behind are copied
   int32_t per;                                    // heads of a thread
   FastDiv units, tokens;                          // units of a head; rows
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(THREADS, 3) rotary_kernel(const RotaryParams p
   fetch(0);                                       // on its way while the factors are made
   float c[PAIRS_], s[PAIRS_];
   if (turns) {
-    const uint64_t pos = (uint64_t)(p.positions ? (int64_t)p.positions[row] : (int64_t)p.first + (p.seq ? row % (uint32_t)p.seq : row));
+    const uint64_t pos = (uint64_t)(p.positions ? (int64_t)p.positions[row] : (int64_t)p.first + (p.seq ? (p.row0 + row) % p.seq : p.row0 + row));
     const float amplitude = p.amplitude, signed_amplitude = p.backward ? -p.amplitude : p.amplitude;
 #pragma unroll
     for (int i = 0; i < PAIRS_; ++i) {
@@ -223,8 +224,8 @@ extern "C" fax_status fax_op_rotary(fax_ctx* ctx, int32_t prec, const fax_rotary
   const bool vec = n > 2 || halves || fits(n);
 
   RotaryParams p;
-  p.x = d->x; p.y = d->y; p.ldx = d->ldx; p.ldy = d->ldy; p.positions = d->positions; p.freq = d->frequencies;
-  p.rows = d->rows; p.heads = d->heads; p.half = half; p.head_dim = d->head_dim; p.first = d->first; p.seq = d->seq;
+  p.ldx = d->ldx; p.ldy = d->ldy; p.freq = d->frequencies;
+  p.heads = d->heads; p.half = half; p.head_dim = d->head_dim; p.first = d->first; p.seq = d->seq;
   p.turned = halves ? half / n : d->rot_dim / n;
   p.amplitude = d->amplitude; p.backward = d->backward != 0;
   const int64_t units = halves ? moved / (2 * n) : moved / n;
@@ -234,21 +235,29 @@ extern "C" fax_status fax_op_rotary(fax_ctx* ctx, int32_t prec, const fax_rotary
   int64_t parts = (want + units * d->rows - 1) / (units * d->rows);
   if (parts > d->heads) parts = d->heads;
   p.per = (int32_t)((d->heads + parts - 1) / parts);
-  const int64_t all = units * d->rows * ((d->heads + p.per - 1) / p.per);
-  if (all > 0x7fffffff) return FAX_ERR_UNSUPPORTED_SHAPE;
-  p.threads = all;
+  const int64_t row_threads = units * ((d->heads + p.per - 1) / p.per);
   p.units = FastDiv((uint32_t)units);
-  p.tokens = FastDiv((uint32_t)d->rows);
-  const int grid = (int)((all + THREADS - 1) / THREADS);
   FaxProfScope prof(ctx, KC_ROTARY, 3.0 * d->rows * d->heads * d->rot_dim, 2.0 * d->rows * d->heads * moved * es + (d->positions ? 4.0 * d->rows : 0.0));
-  if (prec == FAX_PREC_BF16) {
-    if (n == 8) launch<bf16, 8>(ctx, d->layout, vec, grid, p);
-    else if (n == 4) launch<bf16, 4>(ctx, d->layout, vec, grid, p);
-    else launch<bf16, 1>(ctx, d->layout, vec, grid, p);
-  } else {
-    if (n == 4) launch<float, 4>(ctx, d->layout, vec, grid, p);
-    else if (n == 2 && vec) launch<float, 2>(ctx, d->layout, vec, grid, p);
-    else launch<float, 1>(ctx, d->layout, vec, grid, p);
+  // threads are counted in 31 bits
+  const int64_t most = 0x7fffff00 / row_threads;
+  for (int64_t r0 = 0; r0 < d->rows; r0 += most) {
+    const int64_t rows = d->rows - r0 < most ? d->rows - r0 : most;
+    p.x = (const char*)d->x + r0 * d->ldx * es; p.y = (char*)d->y + r0 * d->ldy * es;
+    p.positions = d->positions ? d->positions + r0 : nullptr;
+    p.row0 = r0;
+    p.threads = row_threads * rows;
+    p.tokens = FastDiv((uint32_t)rows);
+    const int grid = (int)((p.threads + THREADS - 1) / THREADS);
+    if (prec == FAX_PREC_BF16) {
+      if (n == 8) launch<bf16, 8>(ctx, d->layout, vec, grid, p);
+      else if (n == 4) launch<bf16, 4>(ctx, d->layout, vec, grid, p);
+      else launch<bf16, 1>(ctx, d->layout, vec, grid, p);
+    } else {
+      if (n == 4) launch<float, 4>(ctx, d->layout, vec, grid, p);
+      else if (n == 2 && vec) launch<float, 2>(ctx, d->layout, vec, grid, p);
+      else launch<float, 1>(ctx, d->layout, vec, grid, p);
+    }
+    FAX_TRY(fax_after_launch(ctx));
   }
-  return fax_after_launch(ctx);
+  return FAX_OK;
 }

@@ -191,3 +191,31 @@ def test_rows_behind_two_to_the_31_elements(sess):
     assert torch.equal(out[n // 2 - 32:n // 2], x[-63::2]) and torch.equal(out[-32:], x[-64::2])
     ops.fax_op_expert_combine(sess.ctx, 0, ops.ExpertCombineDesc(n, 1, d, n, ptr(slot_of), None, ptr(out), d, None, 0, ptr(back), d))
     assert torch.equal(back, x)
+
+
+@pytest.mark.parametrize("d", [64, 63])
+def test_pitches_of_their_own(sess, d):
+    """Every matrix with a pitch of its own: the same values as without gaps."""
+    rng = np.random.default_rng(8)
+    n, k, e = 37, 2, 3
+    slot_t, source_t, _, _ = sort(sess, choices(rng, n, k, e), e, 0, 8)
+    slots = source_t.numel()
+    w = torch.as_tensor(rng.random((n, k))).float().to(sess.device)
+
+    def run(pads):
+        make = lambda rows, i: pitched(sess, ref.rounded(np.random.default_rng(100 + i).standard_normal((rows, d)), 0), 0, pads[i])  # noqa: E731
+        x, z, r, dy, out, y, dz = make(n, 0), make(slots, 1), make(n, 2), make(n, 3), make(slots, 4), make(n, 5), make(slots, 6)
+        dw = torch.empty((n, k), device=sess.device)
+        ld = lambda t: t.stride(0)  # noqa: E731
+        ops.fax_op_expert_dispatch(sess.ctx, 0, ops.ExpertDispatchDesc(n, k, d, slots, ptr(slot_t), ptr(source_t), ptr(x), ld(x), ptr(out), ld(out)))
+        ops.fax_op_expert_combine(sess.ctx, 0, ops.ExpertCombineDesc(n, k, d, slots, ptr(slot_t), ptr(w), ptr(z), ld(z), ptr(r), ld(r), ptr(y), ld(y)))
+        ops.fax_op_expert_combine_backward(sess.ctx, 0, ops.ExpertCombineBackwardDesc(n, k, d, slots, ptr(slot_t), ptr(source_t), ptr(w), ptr(z), ld(z), ptr(dy), ld(dy), ptr(dz), ld(dz), ptr(dw)))
+        for t, p in zip((out, y, dz), (pads[4], pads[5], pads[6])):
+            assert p == 0 or bool((t[:, d:] == 7).all())
+        return out[:, :d].clone(), y[:, :d].clone(), dz[:, :d].clone(), dw
+    a, b = run([0] * 7), run([8, 16, 1, 8, 24, 3, 8])
+    c = run([8, 16, 24, 8, 24, 8, 40])
+    for x, y, z in zip(a[:3], b[:3], c[:3]):
+        assert torch.equal(x, y) and torch.equal(x, z)
+    # (the sums of dw run in another order where vectors are single elements)
+    assert float((a[3] - c[3]).abs().max()) <= 64 * 2.0 ** -24 * 64 and float((a[3] - b[3]).abs().max()) <= 64 * 2.0 ** -24 * 64

@@ -297,3 +297,32 @@ def test_rows_behind_two_to_the_31_elements(sess):
     ops.fax_op_recurrence_backward(sess.ctx, 0, ops.RecurrenceBackwardDesc(*shape, ptr(states), ptr(bufs[2]), pitch, ptr(small.tdh_last), ptr(bufs[0]), pitch, ptr(y), pitch, None, 0, ptr(dh0)))
     assert torch.equal(bufs[0][lo:, :d], small.df) and torch.equal(y[lo:, :d], small.dx) and torch.equal(dh0, small.dh0)
     assert float(y[:lo, :d].abs().max()) == 0 and float(y[:, d:d + 64].abs().max()) == 0
+
+
+@pytest.mark.parametrize("d", [64, 40, 31])
+def test_pitches_of_their_own(sess, d):
+    """Every matrix with a pitch of its own, whole 16 bytes or not: the same bits as without gaps where the rows come in alike, values in the bounds everywhere."""
+    for pads in ([8, 16, 24, 32, 40, 8, 16, 48], [1, 2, 3, 4, 5, 6, 7, 9]):
+        layer = Layer(sess, 0, [50, 0, 130], d, True, ref.COMPLEMENT, 21)
+        t = {}
+        for i, name in enumerate(("tf", "tx", "tg", "tdy", "y", "df", "dx", "dg")):
+            old = getattr(layer, name)
+            wide = torch.full((old.shape[0], d + pads[i]), 7.0, dtype=old.dtype, device=sess.device)
+            wide[:, :d] = old
+            t[name] = wide
+            setattr(layer, name, wide[:, :d])
+        layer.forward()
+        layer.backward()
+        layer.check()
+        for name, wide in t.items():
+            assert bool((wide[:, d:] == 7).all()), name
+
+
+def test_nothing_to_do(sess):
+    """No rows: the states pass through; no sequences: nothing is touched."""
+    for prec in (0, 1):
+        layer = Layer(sess, prec, [0, 0], 24, True, ref.PLAIN, 3)
+        layer.forward()
+        layer.backward()
+        assert torch.equal(layer.h_last, layer.th0) and torch.equal(layer.dh0, layer.tdh_last)
+        ops.fax_op_recurrence_forward(sess.ctx, prec, ops.RecurrenceDesc(0, 24, 0, 0, None, 0, None, 24, None, 24, None, 0, None, None, 24, None, None))

@@ -103,3 +103,36 @@ def test_rows_behind_two_to_the_31_elements(sess):
     want, bound = ref.rotary(v[last].double().cpu().numpy().reshape(50, 1, 64), np.arange(rows)[last], ref.frequencies(64), 64, ref.HALVES)
     check(x[last, 100:164].double().cpu().numpy().reshape(50, 1, 64), want, bound, 0)
     assert float(x[:, :100].abs().max()) == 0 and float(x[:, 164:300].abs().max()) == 0
+
+
+@pytest.mark.parametrize("layout", [ref.HALVES, ref.PAIRS])
+@pytest.mark.parametrize("pitches", [(128, 200), (131, 128), (136, 129)])
+def test_pitches_of_their_own(sess, pitches, layout):
+    """x and y with pitches (and so alignments) that differ, the rest of a head copied."""
+    rng = np.random.default_rng(6)
+    x = ref.rounded(rng.standard_normal((77, 2, 64)), 0)
+    bx, by = (torch.full((77, p), 7.0, dtype=torch.bfloat16, device=sess.device) for p in pitches)
+    bx[:, :128] = torch.as_tensor(x.reshape(77, 128)).to(bx)
+    table = rotary_frequencies(sess.device, 32)
+    ops.fax_op_rotary(sess.ctx, 0, ops.RotaryDesc(77, 2, 64, 32, layout, ptr(bx), pitches[0], ptr(by), pitches[1], None, 3, 0, ptr(table), 0.5, 0))
+    want, bound = ref.rotary(x, 3 + np.arange(77), ref.frequencies(32), 32, layout, 0.5)
+    check(by[:, :128].double().cpu().numpy().reshape(77, 2, 64), want, bound, 0)
+    assert bool((by[:, 128:] == 7).all()) and np.array_equal(by[:, :128].double().cpu().numpy().reshape(77, 2, 64)[..., 32:], x[..., 32:])
+
+
+def test_more_pairs_than_31_bits_count(sess):
+    """2^29 rows of four pairs, single elements because the rows begin at odd ones: several launches, one count of positions."""
+    rows, dev = 2**29 + 100, sess.device
+    buf = torch.zeros(rows * 8 + 1, dtype=torch.bfloat16, device=dev)
+    x = buf[1:].view(rows, 8)
+    spots = torch.tensor([0, 1, 2**29 - 64 - 1, 2**29 - 64, 2**29 - 1, 2**29 + 99], device=dev)
+    v = torch.randn((len(spots), 8), device=dev).to(torch.bfloat16)
+    x[spots] = v
+    table = rotary_frequencies(dev, 8)
+    for seq in (0, 1000):
+        x[spots] = v
+        ops.fax_op_rotary(sess.ctx, 0, ops.RotaryDesc(rows, 1, 8, 8, 0, x.data_ptr(), 8, x.data_ptr(), 8, None, 5, seq, ptr(table), 1.0, 0))
+        p = spots.cpu().numpy()
+        want, bound = ref.rotary(v.double().cpu().numpy().reshape(-1, 1, 8), 5 + (p % seq if seq else p), ref.frequencies(8), 8, ref.HALVES)
+        check(x[spots].double().cpu().numpy().reshape(-1, 1, 8), want, bound, 0)
+        assert float(x[2**29 - 5000:2**29 - 100].abs().max()) == 0
