@@ -249,7 +249,7 @@ __device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, 
   const int me = FORWARD ? at.warp : ex.n_warps - 1 - at.warp;
   Link* const links = ex.links + at.lane;
   links[me * 32] = mine;
-  __syncthreads();
+  tc::named_barrier_sync(1, ex.n_warps * 32);     // (warps with whole and with short stretches come here from different places)
   if (at.warp == 0) {
     two state = carry;
     if (at.ctas > 1) {
@@ -287,7 +287,7 @@ __device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, 
     }
     if (at.ctas == 1) carry = state;
   }
-  __syncthreads();
+  tc::named_barrier_sync(1, ex.n_warps * 32);
   return ex.starts[me * 32 + at.lane];
 }
 
