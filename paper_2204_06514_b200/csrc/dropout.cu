@@ -29,17 +29,23 @@ struct DropoutParams {
   const uint64_t* offset_device;
 };
 
-__device__ __forceinline__ uint4 philox(const DropoutParams& p, uint32_t c0, uint32_t c1, uint64_t offset) {
-  uint32_t x0 = c0, x1 = c1, x2 = (uint32_t)offset, x3 = (uint32_t)(offset >> 32);
+// N counters at once, so that a round's keys are fetched once for all.
+template <int N>
+__device__ __forceinline__ void philox(const DropoutParams& p, const uint32_t (&c0)[N], const uint32_t (&c1)[N], uint64_t offset, uint32_t (&w)[N][4]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) { w[n][0] = c0[n]; w[n][1] = c1[n]; w[n][2] = (uint32_t)offset; w[n][3] = (uint32_t)(offset >> 32); }
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
-    const uint64_t p0 = (uint64_t)x0 * 0xD2511F53u, p1 = (uint64_t)x2 * 0xCD9E8D57u;
-    x0 = (uint32_t)(p1 >> 32) ^ x1 ^ p.k0[r];
-    x1 = (uint32_t)p1;
-    x2 = (uint32_t)(p0 >> 32) ^ x3 ^ p.k1[r];
-    x3 = (uint32_t)p0;
+    const uint32_t k0 = p.k0[r], k1 = p.k1[r];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint64_t p0 = (uint64_t)w[n][0] * 0xD2511F53u, p1 = (uint64_t)w[n][2] * 0xCD9E8D57u;
+      w[n][0] = (uint32_t)(p1 >> 32) ^ w[n][1] ^ k0;
+      w[n][1] = (uint32_t)p1;
+      w[n][2] = (uint32_t)(p0 >> 32) ^ w[n][3] ^ k1;
+      w[n][3] = (uint32_t)p0;
+    }
   }
-  return make_uint4(x0, x1, x2, x3);
 }
 
 // How the rows lie.  FLAT: one after the other without gaps, in whole vectors; PITCHED: whole vectors a pitch apart (the last group may be short of
@@ -89,12 +95,17 @@ __global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) == 4 ? 5 : 1
         }
     }
   }
+  uint32_t bits[UNITS][4];
+  if (p.limit) {
+    philox<UNITS>(p, group, row, offset, bits);
+  } else {                                         // keeps everything: whatever is above 0
+#pragma unroll
+    for (int k = 0; k < UNITS; ++k) bits[k][0] = bits[k][1] = bits[k][2] = bits[k][3] = ~0u;
+  }
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
     if (!live[k]) continue;
-    // (a limit of 0 keeps everything: whatever is above 0)
-    const uint4 bits = p.limit ? philox(p, group[k], row[k], offset) : make_uint4(~0u, ~0u, ~0u, ~0u);
-    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
+    const uint32_t (&w)[4] = bits[k];
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
