@@ -3,7 +3,7 @@
 // Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
 // 32 x 32 -> 64 bit products over a counter of four words; the rounds' keys are the same for all and come with the launch.
 // One counter gives the 16 bits of eight elements, which are one 16-byte vector of bf16, so that a thread draws once for what
-// it loads.  Memory bounds it, the instructions come next: some 13 an element beside 4 to 6 bytes of traffic.
+// it loads.  Memory bounds it, the instructions come next: some 15 an element beside 4 to 6 bytes of traffic.
 #include <cmath>
 
 #include "stream_common.cuh"
@@ -52,11 +52,12 @@ __device__ __forceinline__ void philox(const DropoutParams& p, const uint32_t (&
 // columns); LOOSE: anything, element by element.
 enum Rows { FLAT, PITCHED, LOOSE };
 
-// Groups of eight columns of a thread: one (more warps hide the loads better: 16384 x 768 with residual 13.7 us, with two groups 15.7 us), but
-// four where a thread has little in hand and no places to work out (8192 x 4096 bf16: 27.1 against 29 us).
-template <typename T> constexpr int units_of(bool resid, int rows) { return !resid && rows == FLAT && sizeof(T) == 2 ? 4 : 1; }
+// Groups of eight columns of a thread: several of bf16 in flat rows share the fetching of keys (8192 x 4096: 28.6 us with one, 24.3 with two, 23.1
+// with four; with residual 16384 x 768: 14.0, 13.4, 13.4 us); else one, with more warps to hide the loads (float 22.1 against 22.7 us,
+// pitched rows 33.6 against 36.9 us).
+template <typename T> constexpr int units_of(bool resid, int rows) { return rows == FLAT && sizeof(T) == 2 ? (resid ? 2 : 4) : 1; }
 template <typename T, bool RESID, int ROWS>
-__global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) == 4 ? 5 : 1) dropout_kernel(const __grid_constant__ DropoutParams p) {
+__global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) > 1 ? 4 : 1) dropout_kernel(const __grid_constant__ DropoutParams p) {
   constexpr int UNITS = units_of<T>(RESID, ROWS);
   fax_grid_dependency_wait();
   const uint64_t offset = p.offset + (p.offset_device ? *p.offset_device : 0);
