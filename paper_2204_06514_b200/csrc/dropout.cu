@@ -48,14 +48,14 @@ __device__ __forceinline__ void philox(const DropoutParams& p, const uint32_t (&
   }
 }
 
-// How the rows lie.  FLAT: one after the other without gaps, in whole vectors; PITCHED: whole vectors a pitch apart (the last group may be short of
-// columns); LOOSE: anything, element by element.
-enum Rows { FLAT, PITCHED, LOOSE };
+// How the rows lie.  FLAT: one after the other without gaps, in whole vectors; PITCHED: whole vectors a pitch apart; SHORT: the same with a last
+// group that is short of columns; LOOSE: anything, element by element.
+enum Rows { FLAT, PITCHED, SHORT, LOOSE };
 
 // Groups of eight columns of a thread: several of bf16 in flat rows share the fetching of keys (8192 x 4096: 28.6 us with one, 24.3 with two, 23.1
 // with four; with residual 16384 x 768: 14.0, 13.4, 13.4 us); else one, with more warps to hide the loads (float 22.1 against 22.7 us,
 // pitched rows 33.6 against 36.9 us).
-template <typename T> constexpr int units_of(bool resid, int rows) { return rows == FLAT && sizeof(T) == 2 ? (resid ? 2 : 4) : 1; }
+template <typename T> constexpr int units_of(bool resid, int rows) { return (rows == FLAT || rows == PITCHED) && sizeof(T) == 2 ? (resid ? 2 : 4) : 1; }
 template <typename T, bool RESID, int ROWS>
 __global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) > 1 ? 4 : 1) dropout_kernel(const __grid_constant__ DropoutParams p) {
   constexpr int UNITS = units_of<T>(RESID, ROWS);
@@ -80,14 +80,20 @@ __global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) > 1 ? 4 : 1)
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
     live[k] = first + threadIdx.x + k * THREADS < p.units;
-    whole[k] = ROWS == FLAT || (ROWS == PITCHED && (int)group[k] * 8 + 8 <= p.cols);
+    whole[k] = ROWS == FLAT || ROWS == PITCHED || (ROWS == SHORT && (int)group[k] * 8 + 8 <= p.cols);
     if (!live[k]) continue;
     const T* px = (const T*)p.x + place(k, p.ldx);
     const T* pr = RESID ? (const T*)p.resid + place(k, p.ldr) : nullptr;
     if (whole[k]) {
       x[k] = load_pack<T, 8>(px);
       if constexpr (RESID) r[k] = load_pack<T, 8>(pr);
-    } else if (ROWS != FLAT) {
+    } else if (ROWS == LOOSE && (int)group[k] * 8 + 8 <= p.cols) {               // no branches between the loads
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[k].e[i] = px[i];
+        if constexpr (RESID) r[k].e[i] = pr[i];
+      }
+    } else if (ROWS == SHORT || ROWS == LOOSE) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if ((int)group[k] * 8 + i < p.cols) {
@@ -126,7 +132,10 @@ __global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) > 1 ? 4 : 1)
     T* py = (T*)p.y + place(k, p.ldy);
     if (whole[k]) {
       store_pack<T, 8>(py, out);
-    } else if (ROWS != FLAT) {
+    } else if (ROWS == LOOSE && (int)group[k] * 8 + 8 <= p.cols) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) py[i] = out.e[i];
+    } else if (ROWS == SHORT || ROWS == LOOSE) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if ((int)group[k] * 8 + i < p.cols) py[i] = out.e[i];
@@ -143,6 +152,7 @@ template <typename T>
 void launch(fax_ctx* ctx, bool resid, Rows rows, const DropoutParams& p) {
   if (rows == FLAT) launch<T, FLAT>(ctx, resid, p);
   else if (rows == PITCHED) launch<T, PITCHED>(ctx, resid, p);
+  else if (rows == SHORT) launch<T, SHORT>(ctx, resid, p);
   else launch<T, LOOSE>(ctx, resid, p);
 }
 
@@ -176,7 +186,7 @@ extern "C" fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropo
   p.step_rows = THREADS / groups; p.step_groups = THREADS % groups;
   const bool vec = fax_rows_aligned(d->x, d->ldx, es, 16) && fax_rows_aligned(d->y, d->ldy, es, 16) && (!d->resid || fax_rows_aligned(d->resid, d->ldr, es, 16));
   const bool flat = d->cols % 8 == 0 && d->ldx == d->cols && d->ldy == d->cols && (!d->resid || d->ldr == d->cols);
-  const Rows rows = !vec ? LOOSE : flat ? FLAT : PITCHED;
+  const Rows rows = !vec ? LOOSE : flat ? FLAT : d->cols % 8 == 0 ? PITCHED : SHORT;
   const double n = (double)d->rows * d->cols;
   FaxProfScope prof(ctx, KC_DROPOUT, 2.0 * n, (d->resid ? 3.0 : 2.0) * n * es);
   if (prec == FAX_PREC_BF16) launch<bf16>(ctx, d->resid != nullptr, rows, p);
