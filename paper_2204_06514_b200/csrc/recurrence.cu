@@ -25,13 +25,13 @@ constexpr int MAX_WARPS = 16;                    // of a CTA: 128 registers a th
 constexpr int STEPS = FAX_RECURRENCE_BLOCK;      // tokens of a stretch
 constexpr int CHANNELS = 64;                     // of a warp
 constexpr int MAX_CLUSTER = 16;
-constexpr int MAX_STAGES = 3;
+constexpr int MAX_STAGES = 2;
 constexpr int SMEM_MAX = 226 * 1024;
 
-// How rows come in and go out.  TILES: 16 x 64 boxes by TMA through shared memory, those of the next rounds under the
-// current one's work (the backward pass, which has no room for its outputs, and a sequence's last rows, fewer than 16,
-// are stored row by row).  PAIRS: straight to registers, a lane's two channels side by side in one access.  SINGLES: a lane has channels c and
-// c + 32, an access each, for widths, pitches and addresses of any kind.
+// How rows come in and go out.  TILES: 16 x 64 boxes by TMA through shared memory, the next round's under the current
+// one's work (the backward pass, which has no room for its outputs, and a sequence's last rows, fewer than 16, are
+// stored row by row).  PAIRS: the same boxes filled by the lanes, a lane's two channels side by side in one access.
+// SINGLES: a lane has channels c and c + 32, an access each, for widths, pitches and addresses of any kind.
 enum Rows { TILES, PAIRS, SINGLES };
 
 struct RecurrenceParams {
@@ -44,7 +44,7 @@ struct RecurrenceParams {
   float *h_last, *states, *dh0;
   int32_t units;                                 // sequences * tiles of channels
   int32_t warps;                                 // of a CTA
-  int32_t stages;                                // TILES: buffers of a warp, 1 to MAX_STAGES
+  int32_t stages;                                // buffers of a warp (TILES: up to MAX_STAGES; else 1)
   int32_t* status;
 };
 struct Maps { CUtensorMap in[4], out; };          // f, x, (g), (dy); y
@@ -329,8 +329,8 @@ struct Inputs {
   }
 };
 
-// A warp's buffers, in turn, and the barriers that say they are full.  Rows are asked for as many rounds ahead as there are other
-// buffers; a buffer is asked for again when every lane has read it and what was stored from it has left.
+// A warp's buffers, in turn, and the barriers that say they are full.  With two, rows are asked for a round ahead; a buffer
+// is asked for again when every lane has read it and what was stored from it has left.
 template <typename T, int N>
 struct Tiles {
   uint32_t bar, phase;                           // barriers, their phases

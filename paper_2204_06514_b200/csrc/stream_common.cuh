@@ -26,7 +26,7 @@ __device__ __forceinline__ Pack<T, N> load_pack(const T* p) { return *reinterpre
 template <typename T, int N>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, N>& v) { *reinterpret_cast<Pack<T, N>*>(p) = v; }
 
-// The largest of 16, 8, .. bytes' worth of elements (a power of two, at most `most`) that every given count and pitch is a multiple of.
+// Whether rows that start at p, ld elements of `elem` bytes apart, all start at a multiple of `bytes`.
 static inline bool fax_rows_aligned(const void* p, int64_t ld, size_t elem, size_t bytes) {
   return fax_aligned(p, bytes) && (ld * (int64_t)elem) % (int64_t)bytes == 0;
 }
