@@ -52,9 +52,9 @@ __device__ __forceinline__ void philox(const DropoutParams& p, const uint32_t (&
 // group that is short of columns; LOOSE: anything, element by element.
 enum Rows { FLAT, PITCHED, SHORT, LOOSE };
 
-// Groups of eight columns of a thread: several of bf16 in flat rows share the fetching of keys (8192 x 4096: 28.6 us with one, 24.3 with two, 23.1
-// with four; with residual 16384 x 768: 14.0, 13.4, 13.4 us); else one, with more warps to hide the loads (float 22.1 against 22.7 us,
-// pitched rows 33.6 against 36.9 us).
+// Groups of eight columns of a thread: several of bf16 in whole vectors share the fetching of keys (8192 x 4096: 28.6 us with one, 24.3 with two, 23.1
+// with four; with residual 16384 x 768: 14.0, 13.4, 13.4 us; a pitch of 4104: 25.1 us with four, 33.6 with one and branches between its loads); else
+// one, with more warps to hide the loads (float 22.1 against 22.7 us).
 template <typename T> constexpr int units_of(bool resid, int rows) { return (rows == FLAT || rows == PITCHED) && sizeof(T) == 2 ? (resid ? 2 : 4) : 1; }
 template <typename T, bool RESID, int ROWS>
 __global__ void __launch_bounds__(THREADS, units_of<T>(RESID, ROWS) > 1 ? 4 : 1) dropout_kernel(const __grid_constant__ DropoutParams p) {

@@ -314,7 +314,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 4) combine_backward_kernel(const 
         if (p.dw) {
 #pragma unroll
           for (int j = 0; j < K; ++j)
-            // (one choice: a row in any case, so that no branch stands before the load: 16384 x 2048 45 -> 36 us; with more choices it costs)
+            // (one choice: a row in any case, so that no branch stands before the load: 16384 x 2048 45 -> 36 us; with more choices it
+            // costs.  What is read for a choice without a slot is not looked at, whoever writes there where dz is z.)
             if (K == 1 ? p.slots > 0 : slot[j] >= 0) z[u][j] = load_pack<T, N>((const T*)p.z + (int64_t)max(slot[j], 0) * p.ld_z + (v0 + u * GROUP) * N);
         }
       }

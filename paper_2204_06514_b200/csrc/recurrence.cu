@@ -123,6 +123,10 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// Where a state is written in the place of the one it began with: no CTA writes it before all have read theirs.
+__device__ __forceinline__ void cluster_has_read() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_read() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 // (A, B) of a lane's two channels.
 struct alignas(16) Link { two a, b; };
 // To the same place of CTA `rank`, whose barrier at the place of `bar` counts the bytes: nothing else is waited for or flushed.
@@ -401,6 +405,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
   if (!at.set(p)) return;
   const int64_t seq_row = (int64_t)at.seq * p.d;
   two carry = p.h0 ? at.load_state(p.h0 + seq_row) : 0ull;
+  const bool in_place = CLUSTER && ctas > 1 && p.h_last && p.h_last == p.h0;
+  if (in_place) cluster_has_read();
   const T* src[N]; int64_t ld[N];
   src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
   if constexpr (GATE) { src[2] = (const T*)p.g; ld[2] = p.ldg; }
@@ -492,6 +498,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
     }
   }
   if (ROWS == TILES && at.lane == 0) tc::bulk_wait_all();
+  if (in_place) cluster_wait_read();
   if (p.h_last && at.slot == 0) at.store_state(p.h_last + seq_row, carry);
 }
 
@@ -546,6 +553,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
   if (!at.set(p)) return;
   const int64_t seq_row = (int64_t)at.seq * p.d;
   two carry = p.dh_last ? at.load_state(p.dh_last + seq_row) : 0ull;          // e behind the round: what its last token receives
+  const bool in_place = CLUSTER && ctas > 1 && p.dh0 && p.dh0 == p.dh_last;
+  if (in_place) cluster_has_read();
   const T* src[N]; int64_t ld[N];
   src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
   if constexpr (GATE) { src[2] = (const T*)p.g; ld[2] = p.ldg; }
@@ -637,6 +646,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
       tiles.next();
     }
   }
+  if (in_place) cluster_wait_read();
   if (p.dh0 && at.slot == 0) at.store_state(p.dh0 + seq_row, carry);
 }
 

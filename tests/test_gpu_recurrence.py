@@ -213,6 +213,19 @@ def test_gradients_in_place_of_their_inputs(sess):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("d", [64, 63, 129])
+def test_states_in_place_where_a_cluster_shares_a_sequence(sess, d):
+    """h_last in the place of h0, dh0 in that of dh_last, with many CTAs a sequence, a short and an empty sequence among them."""
+    for seed in range(4):
+        a, b = (Layer(sess, 0, [5000, 3, 0, 2100], d, True, ref.COMPLEMENT, 30 + seed) for _ in range(2))
+        b.h_last, b.dh0 = b.th0, b.tdh_last
+        for layer in (a, b):
+            layer.forward()
+            layer.backward()
+        for x, y in ((a.y, b.y), (a.h_last, b.h_last), (a.df, b.df), (a.dx, b.dx), (a.dg, b.dg), (a.dh0, b.dh0)):
+            assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("d", [66, 64])
 @pytest.mark.parametrize("prec", [0, 1])
