@@ -365,7 +365,7 @@ enum RowOp { DISPATCH, COMBINE, COMBINE_BACKWARD };
 
 // Choices at a time (K): as many loads on their way as registers hold beside four blocks an SM; more of them in two blocks' worth
 // pays where a sum is all there is to keep (6 of 64, 8191 x 2048: combine 58 us with 4 or 3 at a time, 50 us with 6; its gradient 98 us with
-// 8 at a time, 89 us with 3; 4 of 16: 33 and 58 us with 4 at a time in four blocks, 42 and 72 us in two).
+// 8 at a time, 82 us with 3; 4 of 16, 8192 x 2048: 33 and 60 us with 4 at a time in four blocks, 42 and 72 us in two).
 template <typename T, int N, int GROUP>
 fax_status launch_rows(fax_ctx* ctx, RowOp op, RowParams p) {
   constexpr int PER_BLOCK = ROW_THREADS / GROUP;
