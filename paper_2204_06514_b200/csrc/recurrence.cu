@@ -746,16 +746,18 @@ bool make_map_rows(fax_ctx* ctx, CUtensorMap* map, const void* base, int64_t col
                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How warps share the work.
+// How warps share the work.  warp_bytes: one of a warp's buffers.
 struct Shape { bool alone; int warps, cluster; };
 template <bool BACKWARD>
-Shape shape_for(const fax_ctx* ctx, int64_t units, int seq) {
+Shape shape_for(const fax_ctx* ctx, int64_t units, int seq, int warp_bytes) {
   const int64_t sms = ctx->sm_count;
   // A warp a sequence and tile: sequences of one stretch, or 12 warps an SM and more of them.
   if (seq <= STEPS || units >= 12 * sms) {
-    // (backward, CTAs of 4 warps: 12 warps an SM; of 16, with one buffer each: 16)
+    // (backward, CTAs of 4 warps: 12 warps an SM; of 16, with one buffer each: 16, where shared memory holds them: floats with a gate are 4 boxes of
+    // 4 KB a warp, 16 of which would be 256 KB)
     auto rounds = [&](int64_t an_sm) { return (units + an_sm * sms - 1) / (an_sm * sms) * an_sm; };
-    return {true, BACKWARD && seq > 2 * STEPS && rounds(16) * 20 < rounds(12) * 19 ? 16 : 4, 1};
+    const bool fits = buffers_at<false>(MAX_WARPS, 1) + MAX_WARPS * warp_bytes <= SMEM_MAX;
+    return {true, BACKWARD && fits && seq > 2 * STEPS && rounds(16) * 20 < rounds(12) * 19 ? MAX_WARPS : 4, 1};
   }
   // Else CTAs of `warps`, a cluster of them a sequence and tile: as many warps as the SMs hold at once, and no more than the
   // longest sequence has stretches for.  An SM holds 16 warps of the forward pass, 12 of the backward pass.
@@ -792,7 +794,7 @@ fax_status run(fax_ctx* ctx, RecurrenceParams p, bool complement) {
   if (units > 0x7fffffff / MAX_CLUSTER) return FAX_ERR_UNSUPPORTED_SHAPE;
   p.units = (int32_t)units;
   p.status = ctx->dev_status;
-  const Shape shape = shape_for<BACKWARD>(ctx, units, p.seq);
+  const Shape shape = shape_for<BACKWARD>(ctx, units, p.seq, (2 + (p.g != nullptr) + BACKWARD) * box_bytes<T>());
   const bool alone = shape.alone;
   const int cluster = shape.cluster;
   p.warps = shape.warps;
