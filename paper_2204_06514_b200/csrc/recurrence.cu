@@ -604,7 +604,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
             two s, r;
             gates<T>(g, &s, &r);
             const two gs = mul2(g, s);
-            at.store(dg, Raw<T>::of(mul2(mul2(dy, h), fma2(gs, r, s))));
+            at.store(dg, Raw<T>::of(mul2(mul2(dy, fma2(gs, r, s)), h)));         // (in this order: see df)
             dg += p.lddg;
             kept.put_u(i, mul2(dy, gs));
           }
@@ -631,7 +631,8 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
       for (int i = STEPS - 1; i >= 0; --i)
         if (FULL || i < count) {
           const two dh = add2(u_of(i), e);
-          at.store(df, Raw<T>::of(mul2(mul2(dh, kept.get_w(i)), mul2(a[i], rest[i]))));
+          // (dh by the gate's derivative first: dh times a state may pass float's range where a shut gate leaves nothing of it)
+          at.store(df, Raw<T>::of(mul2(mul2(dh, mul2(a[i], rest[i])), kept.get_w(i))));
           at.store(dx, Raw<T>::of(COMPLEMENT ? mul2(dh, rest[i]) : dh));
           df -= p.lddf;
           dx -= p.lddx;
