@@ -83,23 +83,25 @@ template <> struct Raw<float> {
 
 // sigmoid(f) and sigmoid(-f), both with a small relative error (where a is close to 1, 1 - a is what a channel forgets): with
 // e = exp(-f) they are 1 / (1 + e) and e / (1 + e).  bf16 inputs take the hardware's exponential and reciprocal (within 2^-21 + |f| 2^-23
-// of their values, against the 2^-8 of f's and the outputs' own rounding) and cut -f at 87, where a is 2^-126 and the other one 1;
-// min keeps a NaN.  Float inputs take the library's functions of |f|.
+// of their values, against the 2^-8 of f's and the outputs' own rounding) and cut e at 2^126, whose reciprocal is still normal, so that
+// the second one is 1 from there on.  The first one would stay at 2^-126, which times the lowest bf16 as a gate is -4: it is taken 2^-126 lower,
+// 0 from there on and elsewhere off by no more than what a float flushes.  min keeps a NaN.  Float inputs take the library's functions of |f|.
 template <typename T>
 __device__ __forceinline__ void gates(two f, two* a, two* rest) {
   if constexpr (sizeof(T) == 2) {
     const float2 t = unpack2(mul2(f, pack2(-1.4426950408889634f, -1.4426950408889634f)));
-    float t0, t1, e0, e1, r0, r1;
-    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t0) : "f"(t.x));               // 126
-    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(t1) : "f"(t.y));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t0));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t1));
+    float e0, e1, r0, r1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(t.y));
+    asm("min.NaN.f32 %0, %0, 0f7E800000;" : "+f"(e0));                          // 2^126
+    asm("min.NaN.f32 %0, %0, 0f7E800000;" : "+f"(e1));
     const two e = pack2(e0, e1);
     const float2 s = unpack2(add2(e, pack2(1.f, 1.f)));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(s.x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(s.y));
-    *a = pack2(r0, r1);
-    *rest = mul2(e, *a);
+    const two r = pack2(r0, r1);
+    *a = add2(r, pack2(-0x1p-126f, -0x1p-126f));
+    *rest = mul2(e, r);
   } else {
     const float2 v = unpack2(f);
     float big[2], small[2];

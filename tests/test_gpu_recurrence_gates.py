@@ -24,7 +24,20 @@ def fill(layer, name, values):
     getattr(layer, "t" + name).copy_(torch.as_tensor(v))
 
 
-@pytest.mark.parametrize("prec", [1])
+@pytest.mark.parametrize("prec", [0, 1])
+@pytest.mark.parametrize("mode", [ref.PLAIN, ref.COMPLEMENT])
+@pytest.mark.parametrize("lengths,d", SHAPES)
+def test_a_shut_output_gate(sess, lengths, d, mode, prec):  # noqa: F811
+    """g sigmoid(g) and its derivative are 0 for a g this low: no output, and no gradient but dh_last's."""
+    layer = Layer(sess, prec, lengths, d, True, mode, 1, dh_last=False)
+    fill(layer, "g", shut(prec))
+    layer.forward()
+    layer.backward()
+    for t in (layer.y, layer.df, layer.dx, layer.dg, layer.dh0):
+        assert float(t.abs().max()) == 0
+
+
+@pytest.mark.parametrize("prec", [0, 1])
 @pytest.mark.parametrize("lengths,d", SHAPES)
 def test_a_state_that_is_forgotten(sess, lengths, d, prec):  # noqa: F811
     """a is 0: a large state leaves nothing behind, a large gradient hands nothing back."""
@@ -45,7 +58,7 @@ def test_a_state_that_is_forgotten(sess, lengths, d, prec):  # noqa: F811
     assert float(layer.dh0.abs().max()) == 0
 
 
-@pytest.mark.parametrize("prec", [1])
+@pytest.mark.parametrize("prec", [0, 1])
 @pytest.mark.parametrize("lengths,d", SHAPES)
 def test_a_shut_output_gate_beside_a_large_state(sess, lengths, d, prec):  # noqa: F811
     """The products of a large state with a large gradient pass float's range; what the gate's derivative, 0, makes of them does not."""
@@ -60,3 +73,23 @@ def test_a_shut_output_gate_beside_a_large_state(sess, lengths, d, prec):  # noq
     assert bool((layer.h_last == layer.th0).all())
     for t in (layer.y, layer.df, layer.dx, layer.dg, layer.dh0):
         assert float(t.abs().max()) == 0
+
+
+@pytest.mark.parametrize("prec", [0, 1])
+@pytest.mark.parametrize("length", [1, 5])
+def test_gates_along_their_range(sess, length, prec):  # noqa: F811
+    """sigmoid(f) and 1 - sigmoid(f) of a token from -100 to 100: within their relative error, and 2^-126, below which a float is flushed."""
+    f = ref.rounded(np.linspace(-100, 100, 1001), prec)
+    for mode, h0, x in ((ref.PLAIN, 1.0, 0.0), (ref.COMPLEMENT, 0.0, 1.0)):
+        # the gates are the last token's; the ones before it keep the state (f = inf), and add nothing
+        layer = Layer(sess, prec, [length], len(f), False, mode, 3)
+        v = np.full((length, len(f)), np.inf)
+        v[-1] = f
+        layer.tf.copy_(torch.as_tensor(v))
+        layer.tx.fill_(0.0)
+        layer.tx[-1] = x
+        layer.th0.fill_(h0)
+        layer.forward()
+        want = ref.sigmoid(f) if mode == ref.PLAIN else ref.sigmoid(-f)
+        got = layer.h_last[0].double().cpu().numpy()
+        assert np.all(np.abs(got - want) <= (ref.gate_error(f) + 8 * ref.F32) * want + 2.0 ** -126)
