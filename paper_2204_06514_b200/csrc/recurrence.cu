@@ -601,16 +601,16 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
           const two x = in.get(1, i);
           const two h = fma2(a[i], before, COMPLEMENT ? mul2(rest[i], x) : x);
           const two w = COMPLEMENT ? fma2(x, pack2(-1.f, -1.f), before) : before;
+          kept.put_w(i, mul2(w, mul2(a[i], rest[i])));              // (before dh: dh times a state may pass float's range where a shut gate leaves nothing of it)
           if constexpr (GATE) {
             const two g = in.get(2, i), dy = in.get(DY, i);
             two s, r;
             gates<T>(g, &s, &r);
             const two gs = mul2(g, s);
-            at.store(dg, Raw<T>::of(mul2(mul2(dy, fma2(gs, r, s)), h)));         // (in this order: see df)
+            at.store(dg, Raw<T>::of(mul2(mul2(dy, fma2(gs, r, s)), h)));         // (in this order: see w)
             dg += p.lddg;
             kept.put_u(i, mul2(dy, gs));
           }
-          kept.put_w(i, w);
           before = h;
         }
       }
@@ -633,8 +633,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
       for (int i = STEPS - 1; i >= 0; --i)
         if (FULL || i < count) {
           const two dh = add2(u_of(i), e);
-          // (dh by the gate's derivative first: dh times a state may pass float's range where a shut gate leaves nothing of it)
-          at.store(df, Raw<T>::of(mul2(mul2(dh, mul2(a[i], rest[i])), kept.get_w(i))));
+          at.store(df, Raw<T>::of(mul2(dh, kept.get_w(i))));
           at.store(dx, Raw<T>::of(COMPLEMENT ? mul2(dh, rest[i]) : dh));
           df -= p.lddf;
           dx -= p.lddx;
