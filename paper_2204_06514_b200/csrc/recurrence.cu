@@ -128,6 +128,16 @@ __device__ __forceinline__ void cluster_sync() {
 // Where a state is written in the place of the one it began with: no CTA writes it before all have read theirs.
 __device__ __forceinline__ void cluster_has_read() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait_read() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// The CTAs of a cluster go together: none leaves while another one may still send to it.  (Where no wait ran out everything sent has been
+// received by then, so that nothing has to be ordered.)
+__device__ __forceinline__ void cluster_arrive_end() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait_end() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// Where a wait ran out, rows asked for and other CTAs' links may still be on their way into this CTA's memory: they get as long again as the wait had.
+__device__ __forceinline__ void let_arrive(volatile int* gave_up) {
+  if (!*gave_up) return;
+  const long long t0 = clock64();
+  while (clock64() - t0 < tc::WAIT_CYCLES) {}
+}
 
 // (A, B) of a lane's two channels.
 struct alignas(16) Link { two a, b; };
@@ -138,8 +148,8 @@ __device__ __forceinline__ void send(const Link* here, uint32_t bar, uint32_t ra
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote_bar) : "r"(bar), "r"(rank));
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(at), "l"(v.a), "l"(v.b), "r"(remote_bar) : "memory");
 }
-// Bounded wait for what other CTAs sent.
-__device__ __forceinline__ void wait_sent(uint32_t bar, uint32_t parity, volatile int* gave_up, int32_t* status) {
+// Bounded wait for what other CTAs sent; false where it ran out.
+__device__ __forceinline__ bool wait_sent(uint32_t bar, uint32_t parity, volatile int* gave_up, int32_t* status) {
   const long long t0 = clock64();
   for (int spins = 0;; ++spins) {
     uint32_t ok;
@@ -148,17 +158,19 @@ __device__ __forceinline__ void wait_sent(uint32_t bar, uint32_t parity, volatil
         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    if (ok) return;
+    if (ok) return true;
     if ((spins & 255) == 255) {
-      if (*gave_up) return;
+      if (*gave_up) return false;
       if (clock64() - t0 > tc::WAIT_CYCLES) {
         *gave_up = 1;
         if (atomicCAS(status, 0, 1) == 0) status[1] = 602;
-        return;
+        return false;
       }
     }
   }
 }
+
+constexpr uint32_t RAN_OUT = 1u << 31;            // a wait of this warp has run out: it asks and waits for nothing any more
 
 // What warps and CTAs tell one another, in the order of joining.  The CTAs' links have two places that take turns: one is written again two rounds
 // later, by a CTA that has received this CTA's link of the round between, which was sent after the reading of it.
@@ -248,10 +260,10 @@ struct Place {
 };
 
 // Joins the stretches of a round: mine is this warp's; carry (of the first warp): the state before the round, afterwards the one behind
-// it; returns the state before this warp's stretch.  The first warp does it for all: every warp reading every link is bound by shared
+// it; waits: RAN_OUT in it when a wait of the first warp has run out; returns the state before this warp's stretch.  The first warp does it for all: every warp reading every link is bound by shared
 // memory (16 CTAs of 8 warps: 2400 of a round's 5200 cycles that way).  FORWARD: earlier slots come first; else later ones.
 template <bool FORWARD, typename P>
-__device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, const Link& mine, two& carry) {
+__device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, const Link& mine, two& carry, uint32_t& waits) {
   const int me = FORWARD ? at.warp : ex.n_warps - 1 - at.warp;
   Link* const links = ex.links + at.lane;
   links[me * 32] = mine;
@@ -269,10 +281,13 @@ __device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, 
       const int my_cta = FORWARD ? at.rank : at.ctas - 1 - at.rank;
       const uint32_t bar = ex.bars + 8 * (round & 1);
       Link* const ctas = ex.ctas + ((round & 1) * ex.n_ctas) * 32 + at.lane;
-      if (at.lane == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
+      // (where a wait ran out this CTA takes no further part, its barriers may be behind; the others' waits run out in their turn)
+      if (waits < RAN_OUT) {
+        if (at.lane == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
 #pragma unroll 4
-      for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, all);
-      wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status);
+        for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, all);
+        if (!__all_sync(0xffffffffu, wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status))) waits |= RAN_OUT;
+      }
 #pragma unroll 4
       for (int c = 0; c < my_cta; ++c) {
         const Link s = ctas[c * 32];
@@ -339,11 +354,11 @@ struct Inputs {
 // is asked for again when every lane has read it and what was stored from it has left.
 template <typename T, int N>
 struct Tiles {
-  uint32_t bar, phase;                           // barriers, their phases
+  uint32_t bar, phase = 0;                       // barriers, their phases and RAN_OUT
   uint8_t* buf;
   int stages, now;                               // buffers, the current round's one
   __device__ __forceinline__ void init(uint8_t* buffers, uint64_t* bars, int n, int lane) {
-    buf = buffers; bar = tc::smem_u32(bars); phase = 0; stages = n; now = 0;
+    buf = buffers; bar = tc::smem_u32(bars); stages = n; now = 0;
     if (lane == 0) {
 #pragma unroll
       for (int i = 0; i < MAX_STAGES; ++i) tc::mbar_init(bar + 8 * i, 1);
@@ -353,20 +368,21 @@ struct Tiles {
   }
   __device__ __forceinline__ uint8_t* current() const { return buf + now * N * box_bytes<T>(); }
   // The rows of `ahead` rounds from now, when lane 0's stores have left their buffers.
+  // (None when a wait has run out: the buffer may be one that is still waited for.)
   __device__ __forceinline__ void ask(const Maps& maps, int ahead, int col, int64_t row, int lane) {
     int s = now + ahead;
     s = s >= stages ? s - stages : s;
     __syncwarp();
-    if (lane == 0) {
+    if (lane == 0 && phase < RAN_OUT) {
       tc::bulk_wait_read_all();
       tc::mbar_expect_tx(bar + 8 * s, N * box_bytes<T>());
 #pragma unroll
       for (int k = 0; k < N; ++k) tc::tma_load_2d(tc::smem_u32(buf + (s * N + k) * box_bytes<T>()), &maps.in[k], bar + 8 * s, col, (int)row);
     }
   }
-  // Bounded; a wait that runs out sets the context's status, and the work goes on with what is there so that nobody waits for this warp.
+  // Bounded; a wait that runs out sets the context's status, and the work goes on with what is there, without further waits, so that nobody waits for this warp.
   __device__ __forceinline__ void wait(volatile int* gave_up, int32_t* status) {
-    tc::mbar_wait_warp(bar + 8 * now, (phase >> now) & 1, gave_up, status, 601);
+    if (phase < RAN_OUT && !tc::mbar_wait_warp(bar + 8 * now, (phase >> now) & 1, gave_up, status, 601)) phase |= RAN_OUT;
     phase ^= 1u << now;
   }
   __device__ __forceinline__ void next() { now = now + 1 == stages ? 0 : now + 1; }
@@ -407,7 +423,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
   if (!at.set(p)) return;
   const int64_t seq_row = (int64_t)at.seq * p.d;
   two carry = p.h0 ? at.load_state(p.h0 + seq_row) : 0ull;
-  const bool in_place = CLUSTER && ctas > 1 && p.h_last && p.h_last == p.h0;
+  const bool in_place = CLUSTER && p.h_last && p.h_last == p.h0;
   if (in_place) cluster_has_read();
   const T* src[N]; int64_t ld[N];
   src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
@@ -464,7 +480,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
           }
         }
         if (ROWS == TILES && ahead > 0) ask(round + ahead, ahead);
-        two h = join<true>(ex, at, round, mine, carry);
+        two h = join<true>(ex, at, round, mine, carry, tiles.phase);
         if (kept) at.store_state(kept, h);
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
@@ -499,8 +515,11 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_forward_kernel(c
       tiles.next();
     }
   }
-  if (ROWS == TILES && at.lane == 0) tc::bulk_wait_all();
   if (in_place) cluster_wait_read();
+  if (CLUSTER) cluster_arrive_end();
+  if (ROWS == TILES && at.lane == 0) tc::bulk_wait_all();
+  if (CLUSTER) cluster_wait_end();
+  let_arrive(&gave_up);
   if (p.h_last && at.slot == 0) at.store_state(p.h_last + seq_row, carry);
 }
 
@@ -555,7 +574,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
   if (!at.set(p)) return;
   const int64_t seq_row = (int64_t)at.seq * p.d;
   two carry = p.dh_last ? at.load_state(p.dh_last + seq_row) : 0ull;          // e behind the round: what its last token receives
-  const bool in_place = CLUSTER && ctas > 1 && p.dh0 && p.dh0 == p.dh_last;
+  const bool in_place = CLUSTER && p.dh0 && p.dh0 == p.dh_last;
   if (in_place) cluster_has_read();
   const T* src[N]; int64_t ld[N];
   src[0] = (const T*)p.f; ld[0] = p.ldf; src[1] = (const T*)p.x; ld[1] = p.ldx;
@@ -624,7 +643,7 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
             mine.a = mul2(mine.a, a[i]);
             mine.b = mul2(a[i], add2(u_of(i), mine.b));
           }
-        e = join<false>(ex, at, round, mine, carry);
+        e = join<false>(ex, at, round, mine, carry, tiles.phase);
       }
       const int last = (FULL ? STEPS : count) - 1;
       T* df = row_of(p.df, p.lddf, last);
@@ -649,6 +668,9 @@ __global__ void __launch_bounds__(MAX_WARPS * 32, 1) recurrence_backward_kernel(
     }
   }
   if (in_place) cluster_wait_read();
+  if (CLUSTER) cluster_arrive_end();
+  if (CLUSTER) cluster_wait_end();
+  let_arrive(&gave_up);
   if (p.dh0 && at.slot == 0) at.store_state(p.dh0 + seq_row, carry);
 }
 
