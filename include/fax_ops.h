@@ -248,10 +248,12 @@ fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropout_desc* de
  * (NULL: zeros) and ends in h_last [n_seq, d] float (NULL: not wanted; may be h0), so that a sequence can be continued, a
  * token at a time too.  f, x, g (NULL: none), y are [rows, d] T with pitches (columns of one fused projection, e.g.).
  * Sequences are `seq` rows each (rows = n_seq * seq), or with offsets (device, [n_seq + 1] int32, not falling, within 0 to rows) sequence s is
- * rows offsets[s] to offsets[s + 1] - 1, with seq the longest one's length (a choice of kernel goes by it, no result); rows outside stay as
- * they were.  Offsets outside [0, rows] are taken as the nearest end, a falling one as an empty sequence.
+ * rows offsets[s] to offsets[s + 1] - 1, with seq the longest one's length (a choice of kernel goes by it, and with it the
+ * order of roundings); rows outside stay as they were.  Offsets outside [0, rows] are taken as the nearest end, a falling one
+ * as an empty sequence.  Where a sequence behind a falling offset begins before the end of an earlier one, nothing but the arrays is
+ * touched, but y of rows that both have, and whatever the backward pass makes of the call, have no meaning (each writes, in no order).
  * states: NULL, or for the backward pass fax_op_recurrence_states_floats floats, which receive h before every 16th token.
- * y holds no element of f, x or g.  The same inputs give the same bits.  rows = 0 still writes h_last.  rows <= 2^30,
+ * y holds no element of f, x or g.  The same call on the same device gives the same bits.  rows = 0 still writes h_last.  rows <= 2^30,
  * d <= 2^24, n_seq * ceil(d / 64) <= 2^27 - 1. */
 enum { FAX_RECURRENCE_PLAIN = 0, FAX_RECURRENCE_COMPLEMENT = 1 };
 #define FAX_RECURRENCE_BLOCK 16
