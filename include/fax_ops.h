@@ -244,7 +244,9 @@ fax_status fax_op_dropout(fax_ctx* ctx, int32_t prec, const fax_dropout_desc* de
 /* ---- gated linear recurrence ----
  * For each channel c of d and the tokens t of a sequence, in float32:
  *   a_t = 1 / (1 + exp(-f_t))      h_t = a_t h_{t-1} + b_t      y_t = h_t, or with g: h_t g_t / (1 + exp(-g_t))
- * with b_t = x_t (FAX_RECURRENCE_PLAIN) or (1 - a_t) x_t (FAX_RECURRENCE_COMPLEMENT).  h starts at h0 [n_seq, d] float
+ * with b_t = x_t (FAX_RECURRENCE_PLAIN) or (1 - a_t) x_t (FAX_RECURRENCE_COMPLEMENT).  With bf16
+ * inputs the exponentials and reciprocals are the hardware's approximations: a sigmoid of f, and 1 less it, is off by
+ * (2^-21 + 2^-23 |f|) of itself and 2^-126 at most, which h_last, states and dh0 inherit.  h starts at h0 [n_seq, d] float
  * (NULL: zeros) and ends in h_last [n_seq, d] float (NULL: not wanted; may be h0), so that a sequence can be continued, a
  * token at a time too.  f, x, g (NULL: none), y are [rows, d] T with pitches (columns of one fused projection, e.g.).
  * Sequences are `seq` rows each (rows = n_seq * seq), or with offsets (device, [n_seq + 1] int32, not falling, within 0 to rows) sequence s is
