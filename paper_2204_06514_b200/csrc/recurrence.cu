@@ -286,7 +286,7 @@ __device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, 
         if (at.lane == 0) tc::mbar_expect_tx(bar, at.ctas * 32 * sizeof(Link));
 #pragma unroll 4
         for (uint32_t r = 0; r < at.ctas; ++r) send(ctas + my_cta * 32, bar, r, all);
-        if (!__all_sync(0xffffffffu, wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status))) waits |= RAN_OUT;
+        if (!wait_sent(bar, (round >> 1) & 1, ex.gave_up, ex.status)) waits |= RAN_OUT;
       }
 #pragma unroll 4
       for (int c = 0; c < my_cta; ++c) {
@@ -307,6 +307,7 @@ __device__ __forceinline__ two join(const Exchange& ex, const P& at, int round, 
       state = fma2(s.a, state, s.b);
     }
     if (at.ctas == 1) carry = state;
+    else if (__any_sync(0xffffffffu, waits >= RAN_OUT)) waits |= RAN_OUT;                  // (one lane for all, not right behind the wait: 93.2 -> 91.1 us at 1 x 65536 x 768)
   }
   tc::named_barrier_sync(1, ex.n_warps * 32);
   return ex.starts[me * 32 + at.lane];
@@ -784,7 +785,8 @@ Shape shape_for(const fax_ctx* ctx, int64_t units, int seq, int warp_bytes) {
     return {true, BACKWARD && fits && seq > 2 * STEPS && rounds(16) * 20 < rounds(12) * 19 ? MAX_WARPS : 4, 1};
   }
   // Else CTAs of `warps`, a cluster of them a sequence and tile: as many warps as the SMs hold at once, and no more than the
-  // longest sequence has stretches for.  An SM holds 16 warps of the forward pass, 12 of the backward pass.
+  // longest sequence has stretches for.  By its registers an SM holds 16 warps of the forward pass, 12 of the backward pass; where shared memory holds fewer (float
+  // boxes, a gate in a cluster of 16 CTAs) some CTAs come in a second wave, which the rule does not weigh.
   Shape best{false, 4, 1};
   int64_t most = 0;
   for (const int warps : {4, BACKWARD ? 6 : 8}) {

@@ -4,7 +4,7 @@
 // turn with no rounding at all: one 64-bit integer product, right at any position (a float32 angle is off by 0.06 rad at
 // position 10^6).  The nearest quarter turn is split off exactly; sine and cosine of what is left (within an eighth of a turn, 34
 // bits behind the point of the turn) are the first five terms of their series each, whose remainder is below 2^-24; with the roundings of
-// the angle and of the terms they are within 2^-22 of their values (3.2 and 2.2 times 2^-24, over all angles).
+// the angle and of the terms they are within 2^-22 of their values (3.2 and 2.2 times 2^-24 over millions of angles).
 //
 // The work.  Each element is read and written once; memory bounds it, the instructions come next (two pairs share one where the hardware has
 // it).  The factors are the same for every head of a token, so a thread works out those of one 16-byte vector of one token,
