@@ -425,7 +425,7 @@ extern "C" fax_status fax_op_expert_sort(fax_ctx* ctx, const fax_expert_sort_des
   SortParams p;
   p.choices = d->n_tokens * d->top_k; p.experts = d->n_experts; p.capacity = d->capacity; p.align = d->capacity ? 1 : d->align; p.slots = d->slots;
   p.ids = d->ids; p.slot_of = d->slot_of; p.source = d->source; p.offsets = d->offsets; p.counts = d->counts;
-  // Warps for every 64 choices, threads for every expert; one CTA of them, 8 or 16 (4000 choices, 128 experts: 9.9 us on one CTA, 4.6 us on 8;
+  // Warps for every 64 choices, threads for every expert; one CTA of them, 8 or 16 (4000 choices, 128 experts: 9.9 us on one CTA, 5.1 us on 8;
   // 49146 choices, 64 experts: 15.5 us on 8, 11.4 us on 16: the slots' scattered stores).
   const int cluster = p.choices <= 1024 ? 1 : p.choices <= 8192 ? 8 : SORT_CLUSTER;
   int warps = (p.choices / cluster + 63) / 64;
